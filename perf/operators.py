@@ -42,9 +42,7 @@ def _rope(direction, B, N, H, D, **kw):
 
 
 def _linear(direction, M, N, K, **kw):
-    c = {"op": "linear", "direction": direction, "M": M, "N": N, "K": K, "out_type": "bf16"}
-    c.update(kw)
-    return c
+    return {"op": "linear", "direction": direction, "M": M, "N": N, "K": K, **kw}
 
 
 def listed():
@@ -73,8 +71,8 @@ def listed():
         _linear("fwd", 32760, 5120, 5120, name="linear_480p"),
         # Both gradients of a projection over a clip of 9 frames of 1560 tokens.
         _linear("bwd", 14040, 5120, 5120, name="linear_train_clip"),
-        # Sizes that fit no tile, into 32 bits.
-        _linear("fwd", 1237, 1961, 1000, name="linear_ragged", out_type="f32"),
+        # Sizes that fit no tile.
+        _linear("fwd", 1237, 1961, 1000, name="linear_ragged"),
     ]
 
 
@@ -121,7 +119,7 @@ def draw(rng):
         N, K = max(128, N // 128 * 128), max(128, K // 128 * 128)
     while M * N * K * (2 if direction == "bwd" else 1) > 32760 * 5120 * 5120:
         M = max(1, M * 2 // 3)
-    return _linear(direction, M, N, K, out_type=rng.choice(["bf16", "f32"]))
+    return _linear(direction, M, N, K)
 
 
 # ---- inputs ---------------------------------------------------------------------------------
@@ -246,7 +244,6 @@ def _prepare_rope(case, rand):
 
 def _prepare_linear(case, rand):
     M, N, K = case["M"], case["N"], case["K"]
-    out = _type(case["out_type"])
     channel = torch.exp(rand(K, size=0.7))
     s = {"x": (rand(M, K) * channel).to(torch.bfloat16)}
     # codes [rows, columns rounded up to 128] and scales [128-column groups, 128-row blocks] of the weight, and of its transpose
@@ -258,13 +255,13 @@ def _prepare_linear(case, rand):
     codes = (blocks / scale[:, None, :, None]).view(padded.shape).to(torch.float8_e4m3fn).view(torch.uint8)
     if case["direction"] == "fwd":
         s["w_codes"], s["w_scales"] = codes[:N].contiguous(), scale.t().contiguous()
-        s["out"] = torch.empty(M, N, dtype=out, device=DEVICE)
+        s["out"] = torch.empty(M, N, dtype=torch.bfloat16, device=DEVICE)
         kept = [("x", M, K)]
     else:
         s["wt_codes"], s["wt_scales"] = codes.t()[:K].contiguous(), scale.contiguous()
         s["dout"] = rand(M, N, size=0.02, dtype=torch.bfloat16)
         s["dx"] = torch.empty(M, K, dtype=torch.bfloat16, device=DEVICE)
-        s["dw"] = torch.empty(N, K, dtype=torch.float32, device=DEVICE)
+        s["dw"] = torch.empty(N, K, dtype=torch.bfloat16, device=DEVICE)
         kept = [("dout", M, N), ("dout_t", N, M), ("x_t", K, M)]
     for name, rows, columns in kept:   # buffers of the quantised activations
         groups = -(-columns // GROUP)
@@ -492,10 +489,9 @@ def work(case):
         table = sum(size * dims for size, dims in _axes(case)) * 4
         return {"bytes": 2 * n * (4 if case["type"] == "f32" else 2) + min(table, case["B"] * case["N"] * case["D"] * 4), "flops": 3 * n}
     M, N, K = case["M"], case["N"], case["K"]
-    out = 4 if case["out_type"] == "f32" else 2
     if case["direction"] == "fwd":
-        return {"bytes": 2 * M * K + N * K + out * M * N, "flops": 2 * M * N * K}
-    return {"bytes": 2 * M * K + 2 * M * N + N * K + 2 * M * K + 4 * N * K, "flops": 4 * M * N * K}
+        return {"bytes": 2 * M * K + N * K + 2 * M * N, "flops": 2 * M * N * K}
+    return {"bytes": 2 * M * K + 2 * M * N + N * K + 2 * M * K + 2 * N * K, "flops": 4 * M * N * K}
 
 
 # ---- 64 bits ----------------------------------------------------------------------------------
