@@ -1,0 +1,738 @@
+// Gated residual and norms for gfx950, forward and backward.  For a token (row) of C channels, with a conditioning row shared by `group` tokens:
+//     u = N_post(y) w_post,   r = a x + g u,   z = N_pre(r) w (1 + s) + t
+//     N(v) = (v - mean) / sqrt(var + eps)   or   v / sqrt(mean(v^2) + eps)
+// and, with n = N_pre(r), m = N_post(y), 1/size the two norms' factors, and D the whole gradient of r:
+//     d = dz w (1 + s),   D = dr + (d - mean(d) - n mean(d n)) / size,   dx = a D      (mean(d) for layer norms only)
+//     e = D g w_post,     dy = (e - mean(e) - m mean(e m)) / size_y                    (dy = e without a norm)
+//     P = sum dz n, T = sum dz, Q = sum D m over a group's tokens:
+//     ds = P w,  dt = T,  dg = Q w_post,  dw = sum over groups P (1 + s),  dw_post = sum over groups Q g.
+//
+// Both passes are bound by memory: each tensor is read or written once and a row stays in registers between its statistics and its results.
+// A team of lanes takes a row: 16, 32 or 64 lanes with eight channels each up to 512 channels, from there all waves of the workgroup.  A thread
+// has the same channels in all rows of its workgroup, so that it loads the conditioning row once and keeps the sums over tokens in registers; a
+// workgroup's rows are of one group.  The backward writes a workgroup's sums to the workspace, where a second kernel adds them up
+// in a fixed order (no atomics).
+#include <math.h>
+
+#include "radial_layer_common.h"
+
+namespace radial {
+namespace {
+
+constexpr int kMaxChannels = 16384;
+
+struct RowsArg {
+  char* ptr;
+  int64_t sb, sn;  // elements
+};
+
+struct NormArgs {
+  RowsArg x, y, r, z;        // forward; backward: r, y read, z = dz
+  RowsArg dr, dx, dy;        // backward
+  const float *gate, *post_weight, *weight, *scale, *shift;
+  float* partial;            // backward: [groups][chunks][3][C] sums P, T, Q of a workgroup's rows
+  int32_t N, C, group, groups_of_batch;
+  int32_t chunks, rows;      // workgroups that share a group, tokens of each
+  int32_t post, pre;
+  float eps, residual_scale;
+  int64_t mod_stride;
+  int32_t wants;             // backward: bits of the sums that are wanted: 1 P, 2 T, 4 Q
+};
+
+// Sum over a team that is the whole workgroup: each wave's sum through LDS.  kCount sums at once; `turn` alternates between two places, so
+// that one barrier does for each call (who writes a place again has passed the barrier of the call between, behind all reads of it).
+constexpr int kMaxWaves = 16;
+struct Meeting {
+  float place[2][kMaxWaves][4];
+};
+
+// The channels of a thread: 8 V of them.  Vectors: eight in a row, V times, a workgroup's width apart; single elements: each a
+// width apart (rows that are not 16-byte aligned).
+template <bool kVec, int V>
+struct Channels {
+  int32_t first, width, C;
+  __device__ __forceinline__ int32_t at(int v, int e) const { return kVec ? (v * width + first) * 8 + e : (v * 8 + e) * width + first; }
+  __device__ __forceinline__ bool has(int v, int e) const { return at(v, e) < C; }
+  __device__ __forceinline__ int32_t count() const {
+    int32_t n = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) n += has(v, e);
+    return n;
+  }
+};
+
+// A thread's channels of a row, as they lie in memory.
+template <class T, bool kVec, int V>
+struct Held {
+  Eight<T> piece[kVec ? V : 1];
+  T single[kVec ? 1 : 8 * V];
+  __device__ __forceinline__ void load(const T* row, const Channels<kVec, V>& ch) {
+    if constexpr (kVec) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if (ch.has(v, 0)) piece[v].load(row + ch.at(v, 0));
+        else piece[v].clear();
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8 * V; ++i) single[i] = ch.has(i / 8, i % 8) ? row[ch.at(i / 8, i % 8)] : (T)0.f;
+    }
+  }
+  __device__ __forceinline__ void get(float (&out)[8 * V]) const {
+    if constexpr (kVec) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float e8[8];
+        piece[v].get(e8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[8 * v + e] = e8[e];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8 * V; ++i) out[i] = (float)single[i];
+    }
+  }
+};
+
+template <class T, bool kVec, int V>
+__device__ __forceinline__ void store_row(T* row, const float (&val)[8 * V], const Channels<kVec, V>& ch) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    if constexpr (kVec) {
+      float e8[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) e8[e] = val[8 * v + e];
+      if (ch.has(v, 0)) Eight<T>::store(row + ch.at(v, 0), e8);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (ch.has(v, e)) row[ch.at(v, e)] = (T)val[8 * v + e];
+    }
+  }
+}
+
+// A conditioning row or a weight, `missing` where it is not given.
+template <bool kVec, int V>
+__device__ __forceinline__ void load_mod(float (&out)[8 * V], const float* row, float missing, const Channels<kVec, V>& ch) {
+  if (row) {
+    Held<float, kVec, V> h;
+    h.load(row, ch);
+    h.get(out);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8 * V; ++i) out[i] = missing;
+  }
+}
+
+// Rows of a team and its sums.  kWide: the team is the workgroup; otherwise L lanes.
+template <bool kWide, int L>
+struct Team {
+  Meeting* meet;
+  int32_t turn, wave, waves;
+  float C;
+  float own;       // channels of this wave (wide) or of the row
+  __device__ __forceinline__ float lanes(float x) const { return lane_sum<kWide ? 64 : L>(x); }
+  // Every wave's `k` values to every wave.
+  template <int kCount>
+  __device__ __forceinline__ void exchange(const float (&mine)[kCount]) {
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int i = 0; i < kCount; ++i) meet->place[turn][wave][i] = mine[i];
+    }
+    __syncthreads();
+  }
+  __device__ __forceinline__ float theirs(int w, int i) const { return meet->place[turn][w][i]; }
+};
+
+// Mean and 1/size of the row, from `val` (zero beyond the channels).  A layer norm's variance is taken about the mean of the wave's own channels and then
+// moved to the row's (sum (v - m)^2 = sum (v - m_w)^2 + n_w (m_w - m)^2 per wave): no cancellation where the mean is large, and one exchange instead of two.
+template <bool kVec, int V>
+__device__ __forceinline__ float sum_of(const float (&val)[8 * V]) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8 * V; ++i) s += val[i];
+  return s;
+}
+template <bool kVec, int V>
+__device__ __forceinline__ float squares_about(const float (&val)[8 * V], float mean, const Channels<kVec, V>& ch) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8 * V; ++i) {
+    const float d = ch.has(i / 8, i % 8) ? val[i] - mean : 0.f;
+    s += d * d;
+  }
+  return s;
+}
+
+template <bool kVec, int V, bool kWide, int L>
+__device__ __forceinline__ void statistics(const float (&val)[8 * V], int32_t kind, float eps, Team<kWide, L>& team, const Channels<kVec, V>& ch, float own_count,
+                                           float& mean, float& inverse) {
+  mean = 0.f;
+  float about = 0.f;
+  if (kind == RADIAL_NORM_LAYER) about = team.lanes(sum_of<kVec, V>(val)) / fmaxf(own_count, 1.f);
+  float squares = team.lanes(squares_about<kVec, V>(val, about, ch));
+  if constexpr (kWide) {
+    const float mine[3] = {about, squares, own_count};
+    team.exchange(mine);
+    squares = 0.f;
+    if (kind == RADIAL_NORM_LAYER) {
+      float total = 0.f;
+      for (int w = 0; w < team.waves; ++w) total += team.theirs(w, 0) * team.theirs(w, 2);
+      mean = total / team.C;
+      for (int w = 0; w < team.waves; ++w) {
+        const float d = team.theirs(w, 0) - mean;
+        squares += team.theirs(w, 1) + team.theirs(w, 2) * d * d;
+      }
+    } else {
+      for (int w = 0; w < team.waves; ++w) squares += team.theirs(w, 1);
+    }
+  } else {
+    mean = about;
+  }
+  inverse = 1.f / sqrtf(squares / team.C + eps);
+}
+
+// Two sums over the row at once.
+template <bool kWide, int L>
+__device__ __forceinline__ void two_sums(float& a, float& b, Team<kWide, L>& team) {
+  a = team.lanes(a);
+  b = team.lanes(b);
+  if constexpr (kWide) {
+    const float mine[2] = {a, b};
+    team.exchange(mine);
+    a = b = 0.f;
+    for (int w = 0; w < team.waves; ++w) {
+      a += team.theirs(w, 0);
+      b += team.theirs(w, 1);
+    }
+  }
+}
+
+// What a workgroup works on.
+template <bool kVec, int V, bool kWide, int L>
+struct Share {
+  Channels<kVec, V> ch;
+  Team<kWide, L> team;
+  int32_t teams, first, last;  // rows first, first + teams, ... below last, of batch b
+  int32_t b, group;            // group: b * groups_of_batch + g
+  float own_count;
+  __device__ __forceinline__ Share(const NormArgs& a, Meeting* meet) {
+    group = blockIdx.x / a.chunks;
+    const int32_t chunk = blockIdx.x % a.chunks;
+    b = group / a.groups_of_batch;
+    const int32_t g = group % a.groups_of_batch;
+    const int64_t begin = (int64_t)g * a.group + (int64_t)chunk * a.rows;
+    const int64_t end = min(min(begin + a.rows, (int64_t)(g + 1) * a.group), (int64_t)a.N);
+    teams = kWide ? 1 : blockDim.x / L;
+    first = (int32_t)min(begin, (int64_t)a.N) + (kWide ? 0 : threadIdx.x / L);
+    last = (int32_t)max(end, (int64_t)0);
+    ch.first = kWide ? threadIdx.x : threadIdx.x % L;
+    ch.width = kWide ? blockDim.x : L;
+    ch.C = a.C;
+    team.meet = meet;
+    team.turn = 0;
+    team.wave = threadIdx.x >> 6;
+    team.waves = (blockDim.x + 63) >> 6;
+    team.C = (float)a.C;
+    own_count = team.lanes((float)ch.count());
+  }
+};
+
+template <class T>
+__device__ __forceinline__ T* row_of(const RowsArg& t, int32_t b, int32_t n) {
+  return (T*)t.ptr + (int64_t)b * t.sb + (int64_t)n * t.sn;
+}
+
+template <class XT, class YT, bool kVec, int V, bool kWide, int L>
+__global__ void __launch_bounds__(kWide ? 1024 : 256) norm_fwd_kernel(NormArgs a) {
+  __shared__ Meeting meet;
+  Share<kVec, V, kWide, L> s(a, &meet);
+  constexpr int E = 8 * V;
+  const int64_t mod = (int64_t)s.group * a.mod_stride;
+  float gate[E], factor[E], shift[E];
+  {
+    float w[E];
+    load_mod<kVec, V>(gate, a.gate ? a.gate + mod : nullptr, 1.f, s.ch);
+    load_mod<kVec, V>(w, a.post_weight, 1.f, s.ch);
+#pragma unroll
+    for (int i = 0; i < E; ++i) gate[i] *= w[i];
+    load_mod<kVec, V>(factor, a.scale ? a.scale + mod : nullptr, 0.f, s.ch);
+    load_mod<kVec, V>(w, a.weight, 1.f, s.ch);
+#pragma unroll
+    for (int i = 0; i < E; ++i) factor[i] = (1.f + factor[i]) * w[i];
+    load_mod<kVec, V>(shift, a.shift ? a.shift + mod : nullptr, 0.f, s.ch);
+  }
+  Held<XT, kVec, V> x;
+  Held<YT, kVec, V> y;
+  // Teams of a wave end together: lanes without a row work on the last one and store nothing.
+  for (int32_t n = s.first; kWide ? n < s.last : __any(n < s.last); n += s.teams) {
+    const bool live = kWide || n < s.last;
+    const int32_t row = live ? n : s.last - 1;
+    x.load(row_of<XT>(a.x, s.b, row), s.ch);
+    if (a.y.ptr) y.load(row_of<YT>(a.y, s.b, row), s.ch);
+    float r[E];
+    x.get(r);
+    if (a.y.ptr) {
+      float u[E];
+      y.get(u);
+      if (a.post != RADIAL_NORM_NONE) {
+        float mean, inverse;
+        statistics<kVec, V>(u, a.post, a.eps, s.team, s.ch, s.own_count, mean, inverse);
+#pragma unroll
+        for (int i = 0; i < E; ++i) u[i] = (u[i] - mean) * inverse;
+      }
+#pragma unroll
+      for (int i = 0; i < E; ++i) r[i] = s.ch.has(i / 8, i % 8) ? a.residual_scale * r[i] + gate[i] * u[i] : 0.f;
+      if (live) store_row<XT, kVec, V>(row_of<XT>(a.r, s.b, row), r, s.ch);
+    }
+    if (a.pre != RADIAL_NORM_NONE) {
+      float mean, inverse;
+      statistics<kVec, V>(r, a.pre, a.eps, s.team, s.ch, s.own_count, mean, inverse);
+#pragma unroll
+      for (int i = 0; i < E; ++i) r[i] = (r[i] - mean) * inverse * factor[i] + shift[i];
+      if (live) store_row<YT, kVec, V>(row_of<YT>(a.z, s.b, row), r, s.ch);
+    }
+  }
+}
+
+template <class XT, class YT, bool kVec, int V, bool kWide, int L>
+__global__ void __launch_bounds__(kWide ? 1024 : 256) norm_bwd_kernel(NormArgs a) {
+  __shared__ Meeting meet;
+  __shared__ float merged[kWide ? 1 : 3][kWide ? 1 : 256 * 8];
+  Share<kVec, V, kWide, L> s(a, &meet);
+  constexpr int E = 8 * V;
+  const int64_t mod = (int64_t)s.group * a.mod_stride;
+  const bool has_y = a.y.ptr != nullptr, has_z = a.z.ptr != nullptr;
+  float gate[E], factor[E];
+  {
+    float w[E];
+    load_mod<kVec, V>(gate, a.gate ? a.gate + mod : nullptr, 1.f, s.ch);
+    load_mod<kVec, V>(w, a.post_weight, 1.f, s.ch);
+#pragma unroll
+    for (int i = 0; i < E; ++i) gate[i] *= w[i];
+    load_mod<kVec, V>(factor, a.scale ? a.scale + mod : nullptr, 0.f, s.ch);
+    load_mod<kVec, V>(w, a.weight, 1.f, s.ch);
+#pragma unroll
+    for (int i = 0; i < E; ++i) factor[i] = (1.f + factor[i]) * w[i];
+  }
+  float P[E], T[E], Q[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) P[i] = T[i] = Q[i] = 0.f;
+  Held<XT, kVec, V> r_held, dr_held;
+  Held<YT, kVec, V> y_held, dz_held;
+  for (int32_t row_n = s.first; kWide ? row_n < s.last : __any(row_n < s.last); row_n += s.teams) {
+    const bool live = kWide || row_n < s.last;
+    const int32_t row = live ? row_n : s.last - 1;
+    if (has_z) {
+      r_held.load(row_of<XT>(a.r, s.b, row), s.ch);
+      dz_held.load(row_of<YT>(a.z, s.b, row), s.ch);
+    }
+    if (a.dr.ptr) dr_held.load(row_of<XT>(a.dr, s.b, row), s.ch);
+    if (has_y) y_held.load(row_of<YT>(a.y, s.b, row), s.ch);
+    float D[E];
+    if (a.dr.ptr) {
+      dr_held.get(D);
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i) D[i] = 0.f;
+    }
+    if (has_z) {
+      float n[E], d[E];
+      r_held.get(n);
+      dz_held.get(d);
+      float mean, inverse;
+      statistics<kVec, V>(n, a.pre, a.eps, s.team, s.ch, s.own_count, mean, inverse);
+      float along = 0.f, flat = 0.f;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        n[i] = s.ch.has(i / 8, i % 8) ? (n[i] - mean) * inverse : 0.f;
+        if (live) {
+          P[i] += d[i] * n[i];
+          T[i] += d[i];
+        }
+        d[i] *= factor[i];
+        flat += d[i];
+        along += d[i] * n[i];
+      }
+      two_sums(flat, along, s.team);
+      flat = a.pre == RADIAL_NORM_LAYER ? flat / s.team.C : 0.f;
+      along /= s.team.C;
+#pragma unroll
+      for (int i = 0; i < E; ++i) D[i] += inverse * (d[i] - flat - n[i] * along);
+    }
+    {
+      float dx[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) dx[i] = a.residual_scale * D[i];
+      if (live) store_row<XT, kVec, V>(row_of<XT>(a.dx, s.b, row), dx, s.ch);
+    }
+    if (has_y) {
+      float m[E];
+      y_held.get(m);
+      float inverse = 1.f;
+      if (a.post != RADIAL_NORM_NONE) {
+        float mean;
+        statistics<kVec, V>(m, a.post, a.eps, s.team, s.ch, s.own_count, mean, inverse);
+#pragma unroll
+        for (int i = 0; i < E; ++i) m[i] = s.ch.has(i / 8, i % 8) ? (m[i] - mean) * inverse : 0.f;
+      }
+      float along = 0.f, flat = 0.f;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        D[i] = s.ch.has(i / 8, i % 8) ? D[i] : 0.f;
+        if (live) Q[i] += D[i] * m[i];
+        D[i] *= gate[i];
+        flat += D[i];
+        along += D[i] * m[i];
+      }
+      if (a.post != RADIAL_NORM_NONE) {
+        two_sums(flat, along, s.team);
+        flat = a.post == RADIAL_NORM_LAYER ? flat / s.team.C : 0.f;
+        along /= s.team.C;
+#pragma unroll
+        for (int i = 0; i < E; ++i) D[i] = inverse * (D[i] - flat - m[i] * along);
+      }
+      if (live) store_row<YT, kVec, V>(row_of<YT>(a.dy, s.b, row), D, s.ch);
+    }
+  }
+  if (!a.wants) return;
+  float* out = a.partial + (int64_t)blockIdx.x * 3 * a.C;
+  if constexpr (kWide) {
+    if (a.wants & 1) store_row<float, kVec, V>(out, P, s.ch);
+    if (a.wants & 2) store_row<float, kVec, V>(out + a.C, T, s.ch);
+    if (a.wants & 4) store_row<float, kVec, V>(out + 2 * (int64_t)a.C, Q, s.ch);
+  } else {
+    // the teams' sums meet in LDS: [team][lane * 8 + element]
+    const int32_t at = threadIdx.x * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      merged[0][at + i] = P[i];
+      merged[1][at + i] = T[i];
+      merged[2][at + i] = Q[i];
+    }
+    __syncthreads();
+    for (int32_t c = threadIdx.x; c < a.C; c += blockDim.x) {
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        if (!(a.wants >> k & 1)) continue;
+        float sum = 0.f;
+        for (int t = 0; t < s.teams; ++t) sum += merged[k][t * L * 8 + c];
+        out[(int64_t)k * a.C + c] = sum;
+      }
+    }
+  }
+}
+
+struct GradArgs {
+  const float* partial;  // [groups][chunks][3][C]
+  float* of_group;       // [groups][2][C]: P and Q of each group, or null
+  const float *gate, *post_weight, *weight, *scale;
+  float *dgate, *dscale, *dshift, *dpost_weight, *dweight;
+  int32_t C, chunks, groups, wants;
+  int64_t mod_stride, dmod_stride;
+};
+
+constexpr int kGradSlices = 16;
+
+// 64 channels of a group: 16 slices of its workgroups' sums each, then the slices' sums.
+__global__ void __launch_bounds__(64 * kGradSlices) norm_grad_kernel(GradArgs a) {
+  __shared__ float sums[kGradSlices][3][64];
+  const int32_t lane = threadIdx.x, slice = threadIdx.y;
+  const int32_t c = blockIdx.x * 64 + lane;
+  const int64_t group = blockIdx.y + (int64_t)blockIdx.z * 32768;
+  if (group >= a.groups) return;
+  float sum[3] = {0.f, 0.f, 0.f};
+  if (c < a.C) {
+    for (int32_t i = slice; i < a.chunks; i += kGradSlices) {
+      const float* p = a.partial + (group * a.chunks + i) * 3 * a.C + c;
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        if (a.wants >> k & 1) sum[k] += p[(int64_t)k * a.C];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) sums[slice][k][lane] = sum[k];
+  __syncthreads();
+  if (slice != 0 || c >= a.C) return;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    sum[k] = 0.f;
+    for (int i = 0; i < kGradSlices; ++i) sum[k] += sums[i][k][lane];
+  }
+  const int64_t mod = group * a.dmod_stride + c;
+  if (a.dscale) a.dscale[mod] = a.weight ? sum[0] * a.weight[c] : sum[0];
+  if (a.dshift) a.dshift[mod] = sum[1];
+  if (a.dgate) a.dgate[mod] = a.post_weight ? sum[2] * a.post_weight[c] : sum[2];
+  if (a.of_group) {
+    a.of_group[(group * 2) * a.C + c] = sum[0];
+    a.of_group[(group * 2 + 1) * a.C + c] = sum[2];
+  }
+}
+
+// dw and dw_post: sums over the groups, each times its conditioning.
+__global__ void __launch_bounds__(64 * kGradSlices) norm_weight_grad_kernel(GradArgs a) {
+  __shared__ float sums[kGradSlices][2][64];
+  const int32_t lane = threadIdx.x, slice = threadIdx.y;
+  const int32_t c = blockIdx.x * 64 + lane;
+  float dw = 0.f, dw_post = 0.f;
+  if (c < a.C) {
+    for (int64_t g = slice; g < a.groups; g += kGradSlices) {
+      if (a.dweight) dw += a.of_group[g * 2 * a.C + c] * (a.scale ? 1.f + a.scale[g * a.mod_stride + c] : 1.f);
+      if (a.dpost_weight) dw_post += a.of_group[(g * 2 + 1) * a.C + c] * (a.gate ? a.gate[g * a.mod_stride + c] : 1.f);
+    }
+  }
+  sums[slice][0][lane] = dw;
+  sums[slice][1][lane] = dw_post;
+  __syncthreads();
+  if (slice != 0 || c >= a.C) return;
+  dw = dw_post = 0.f;
+  for (int i = 0; i < kGradSlices; ++i) {
+    dw += sums[i][0][lane];
+    dw_post += sums[i][1][lane];
+  }
+  if (a.dweight) a.dweight[c] = dw;
+  if (a.dpost_weight) a.dpost_weight[c] = dw_post;
+}
+
+// ---- launches -----------------------------------------------------------------------------------
+
+// How a call is laid out; goes by the sizes alone, so that the workspace does too.
+struct Layout {
+  int32_t groups_of_batch;
+  int64_t groups;
+  int32_t chunks, rows;
+};
+
+Layout make_layout(const radial_norm_params& p, int64_t workgroups, int32_t least_rows) {
+  Layout l;
+  l.groups_of_batch = (int32_t)(((int64_t)p.N + p.group - 1) / p.group);
+  l.groups = (int64_t)p.B * l.groups_of_batch;
+  const int32_t of_group = p.group < p.N ? p.group : p.N;
+  int64_t chunks = (workgroups + l.groups - 1) / l.groups;
+  const int64_t most = ((int64_t)of_group + least_rows - 1) / least_rows;
+  if (chunks > most) chunks = most;
+  if (chunks < 1) chunks = 1;
+  l.rows = (int32_t)((of_group + chunks - 1) / chunks);
+  l.chunks = (int32_t)(((int64_t)of_group + l.rows - 1) / l.rows);
+  return l;
+}
+
+constexpr int32_t kNarrow = 512;  // channels up to which a row is a wave's or less
+
+Layout fwd_layout(const radial_norm_params& p) { return make_layout(p, 4096, p.C <= kNarrow ? 16 : 1); }
+Layout bwd_layout(const radial_norm_params& p) { return make_layout(p, 1024, p.C <= kNarrow ? 16 : 1); }
+
+bool aligned(const void* ptr, int64_t sb, int64_t sn, int size) {
+  return ((uintptr_t)ptr & 15u) == 0 && sb * size % 16 == 0 && sn * size % 16 == 0;
+}
+
+template <class XT, class YT, bool kVec, int V, bool kWide, int L>
+int launch_one(const NormArgs& a, bool backward, int64_t grid, hipStream_t stream) {
+  int threads = 256;
+  if (kWide) threads = ((a.C + 8 * V - 1) / (8 * V) + 63) / 64 * 64;
+  if (backward) norm_bwd_kernel<XT, YT, kVec, V, kWide, L><<<dim3((unsigned)grid), dim3(threads), 0, stream>>>(a);
+  else norm_fwd_kernel<XT, YT, kVec, V, kWide, L><<<dim3((unsigned)grid), dim3(threads), 0, stream>>>(a);
+  RADIAL_HIP_TRY(hipGetLastError());
+  return RADIAL_OK;
+}
+
+template <class XT, class YT>
+int launch_types(const NormArgs& a, bool vec, bool backward, int64_t grid, hipStream_t stream) {
+  if (!vec) return a.C <= 8192 ? launch_one<XT, YT, false, 1, true, 64>(a, backward, grid, stream) : launch_one<XT, YT, false, 2, true, 64>(a, backward, grid, stream);
+  if (a.C <= 128) return launch_one<XT, YT, true, 1, false, 16>(a, backward, grid, stream);
+  if (a.C <= 256) return launch_one<XT, YT, true, 1, false, 32>(a, backward, grid, stream);
+  if (a.C <= kNarrow) return launch_one<XT, YT, true, 1, false, 64>(a, backward, grid, stream);
+  if (a.C <= 8192) return launch_one<XT, YT, true, 1, true, 64>(a, backward, grid, stream);
+  return launch_one<XT, YT, true, 2, true, 64>(a, backward, grid, stream);
+}
+
+int launch(const NormArgs& a, int32_t x_type, int32_t y_type, bool vec, bool backward, int64_t grid, hipStream_t stream) {
+  if (x_type == RADIAL_F32)
+    return y_type == RADIAL_F32 ? launch_types<float, float>(a, vec, backward, grid, stream) : launch_types<float, __bf16>(a, vec, backward, grid, stream);
+  return y_type == RADIAL_F32 ? launch_types<__bf16, float>(a, vec, backward, grid, stream) : launch_types<__bf16, __bf16>(a, vec, backward, grid, stream);
+}
+
+// ---- checks -------------------------------------------------------------------------------------
+
+bool is_norm(int32_t kind) { return kind == RADIAL_NORM_LAYER || kind == RADIAL_NORM_RMS; }
+
+int check_params(const radial_norm_params* p) {
+  if (!p) return fail(RADIAL_EINVAL, "params is NULL");
+  if (p->B < 1 || p->N < 1 || p->C < 1 || p->group < 1) return fail(RADIAL_EINVAL, "B, N, C, group must be >= 1");
+  if ((int64_t)p->B * p->N > 0x7fffffffLL) return fail(RADIAL_EINVAL, "B*N must be below 2^31");
+  if (p->C > kMaxChannels) return fail(RADIAL_EUNSUPPORTED, "C must be at most %d (got %d)", kMaxChannels, p->C);
+  if (p->post != RADIAL_NORM_NONE && !is_norm(p->post)) return fail(RADIAL_EINVAL, "post must be a RADIAL_NORM_ value (got %d)", p->post);
+  if (p->pre != RADIAL_NORM_NONE && !is_norm(p->pre)) return fail(RADIAL_EINVAL, "pre must be a RADIAL_NORM_ value (got %d)", p->pre);
+  if (!(p->eps > 0.f) || !isfinite(p->eps)) return fail(RADIAL_EINVAL, "eps must be positive and finite");
+  if (!isfinite(p->residual_scale)) return fail(RADIAL_EINVAL, "residual_scale must be finite");
+  return RADIAL_OK;
+}
+
+int check_rows(const char* name, const radial_rows& t, const radial_norm_params& p) {
+  if (!t.ptr) return fail(RADIAL_EINVAL, "%s.ptr is NULL", name);
+  if (!is_type(t.type)) return fail(RADIAL_EINVAL, "%s.type must be RADIAL_BF16 or RADIAL_F32 (got %d)", name, t.type);
+  if ((uintptr_t)t.ptr % size_of(t.type)) return fail(RADIAL_ESHAPE, "%s.ptr is not aligned to its elements", name);
+  if ((p.N > 1 && t.stride_n < p.C) || t.stride_n < 0 || t.stride_b < 0)
+    return fail(RADIAL_ESHAPE, "%s strides must not be negative, and stride_n not below C", name);
+  return RADIAL_OK;
+}
+
+int check_mod(const char* name, const float* mod, int64_t stride, const radial_norm_params& p) {
+  if (!mod) return RADIAL_OK;
+  if ((uintptr_t)mod & 3u) return fail(RADIAL_ESHAPE, "%s is not aligned to its elements", name);
+  if (stride < p.C) return fail(RADIAL_ESHAPE, "the stride of %s must not be below C", name);
+  return RADIAL_OK;
+}
+
+int same_type(const char* x, int32_t of_x, const char* y, int32_t of_y) {
+  return of_x == of_y ? RADIAL_OK : fail(RADIAL_EINVAL, "%s and %s must have one type", x, y);
+}
+
+RowsArg arg(const radial_rows& t) { return RowsArg{(char*)t.ptr, t.stride_b, t.stride_n}; }
+
+NormArgs common_args(const radial_norm_params& p, const Layout& l) {
+  NormArgs a = {};
+  a.N = p.N; a.C = p.C; a.group = p.group; a.groups_of_batch = l.groups_of_batch;
+  a.chunks = l.chunks; a.rows = l.rows;
+  a.post = p.post; a.pre = p.pre;
+  a.eps = p.eps; a.residual_scale = p.residual_scale;
+  a.mod_stride = p.mod_stride;
+  return a;
+}
+
+int check_grid(const Layout& l) {
+  return l.groups * l.chunks <= 0x7fffffffLL ? RADIAL_OK : fail(RADIAL_ESHAPE, "too many groups for one launch");
+}
+
+}  // namespace
+}  // namespace radial
+
+using namespace radial;
+
+extern "C" int radial_norm_fwd(const radial_norm_params* params, radial_rows x, radial_rows y, const float* gate, const float* post_weight,
+                               const float* weight, const float* scale, const float* shift, radial_rows r, radial_rows z, void* hip_stream) {
+  if (int rc = check_params(params)) return rc;
+  const radial_norm_params& p = *params;
+  if (int rc = check_rows("x", x, p)) return rc;
+  const bool has_y = y.ptr != nullptr, has_z = p.pre != RADIAL_NORM_NONE;
+  if (has_y) {
+    if (int rc = check_rows("y", y, p)) return rc;
+    if (int rc = check_rows("r", r, p)) return rc;
+    if (int rc = same_type("x", x.type, "r", r.type)) return rc;
+  } else if (r.ptr || gate || post_weight || p.post != RADIAL_NORM_NONE || p.residual_scale != 1.f) {
+    return fail(RADIAL_EINVAL, "without y there is no r, gate, post norm or residual_scale");
+  }
+  if (has_z) {
+    if (int rc = check_rows("z", z, p)) return rc;
+    if (has_y)
+      if (int rc = same_type("y", y.type, "z", z.type)) return rc;
+  } else if (z.ptr || weight || scale || shift) {
+    return fail(RADIAL_EINVAL, "z, weight, scale and shift need a norm (pre)");
+  }
+  if (!has_y && !has_z) return fail(RADIAL_EINVAL, "neither y nor z is given");
+  if (post_weight && p.post == RADIAL_NORM_NONE) return fail(RADIAL_EINVAL, "post_weight needs a norm (post)");
+  const struct { const char* name; const float* ptr; int64_t stride; } mods[] = {
+      {"gate", gate, p.mod_stride}, {"scale", scale, p.mod_stride}, {"shift", shift, p.mod_stride}, {"post_weight", post_weight, p.C}, {"weight", weight, p.C}};
+  for (const auto& m : mods)
+    if (int rc = check_mod(m.name, m.ptr, m.stride, p)) return rc;
+  const Layout l = fwd_layout(p);
+  if (int rc = check_grid(l)) return rc;
+  NormArgs a = common_args(p, l);
+  a.x = arg(x);
+  if (has_y) { a.y = arg(y); a.r = arg(r); }
+  if (has_z) a.z = arg(z);
+  a.gate = gate; a.post_weight = post_weight; a.weight = weight; a.scale = scale; a.shift = shift;
+  bool vec = p.C % 8 == 0 && p.mod_stride % 4 == 0;
+  for (const radial_rows* t : {&x, &y, &r, &z})
+    if (t->ptr) vec = vec && aligned(t->ptr, t->stride_b, t->stride_n, size_of(t->type));
+  for (const auto& m : mods) vec = vec && ((uintptr_t)m.ptr & 15u) == 0;
+  return launch(a, x.type, has_y ? y.type : z.type, vec, false, l.groups * l.chunks, (hipStream_t)hip_stream);
+}
+
+extern "C" size_t radial_norm_bwd_workspace(const radial_norm_params* params) {
+  if (check_params(params) != RADIAL_OK) return 0;
+  const Layout l = bwd_layout(*params);
+  if (check_grid(l) != RADIAL_OK) return 0;
+  // the workgroups' sums, then the groups'
+  const size_t raw = ((size_t)l.groups * l.chunks * 3 + (size_t)l.groups * 2) * params->C * sizeof(float);
+  return (raw + 255) & ~(size_t)255;
+}
+
+extern "C" int radial_norm_bwd(const radial_norm_params* params, radial_rows r, radial_rows y, radial_rows dz, radial_rows dr, const float* gate,
+                               const float* post_weight, const float* weight, const float* scale, radial_rows dx, radial_rows dy, float* dgate,
+                               float* dscale, float* dshift, float* dpost_weight, float* dweight, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (int rc = check_params(params)) return rc;
+  const radial_norm_params& p = *params;
+  const bool has_y = y.ptr != nullptr, has_z = p.pre != RADIAL_NORM_NONE;
+  if (int rc = check_rows("dx", dx, p)) return rc;
+  if (dr.ptr) {
+    if (int rc = check_rows("dr", dr, p)) return rc;
+    if (int rc = same_type("dr", dr.type, "dx", dx.type)) return rc;
+  }
+  if (has_z) {
+    if (int rc = check_rows("r", r, p)) return rc;
+    if (int rc = check_rows("dz", dz, p)) return rc;
+    if (int rc = same_type("r", r.type, "dx", dx.type)) return rc;
+  } else if (dz.ptr || weight || scale || dscale || dshift || dweight) {
+    return fail(RADIAL_EINVAL, "dz, weight, scale and their gradients need a norm (pre)");
+  } else if (!dr.ptr) {
+    return fail(RADIAL_EINVAL, "dr.ptr is NULL, and there is no dz");
+  }
+  if (has_y) {
+    if (int rc = check_rows("y", y, p)) return rc;
+    if (int rc = check_rows("dy", dy, p)) return rc;
+    if (int rc = same_type("y", y.type, "dy", dy.type)) return rc;
+    if (has_z)
+      if (int rc = same_type("y", y.type, "dz", dz.type)) return rc;
+  } else if (dy.ptr || gate || post_weight || dgate || dpost_weight || p.post != RADIAL_NORM_NONE || p.residual_scale != 1.f) {
+    return fail(RADIAL_EINVAL, "without y there is no dy, gate, post norm or residual_scale");
+  }
+  if (!has_y && !has_z) return fail(RADIAL_EINVAL, "neither y nor dz is given");
+  if ((post_weight || dpost_weight) && p.post == RADIAL_NORM_NONE) return fail(RADIAL_EINVAL, "post_weight needs a norm (post)");
+  const struct { const char* name; const float* ptr; int64_t stride; } mods[] = {
+      {"gate", gate, p.mod_stride}, {"scale", scale, p.mod_stride}, {"post_weight", post_weight, p.C}, {"weight", weight, p.C},
+      {"dgate", dgate, p.dmod_stride}, {"dscale", dscale, p.dmod_stride}, {"dshift", dshift, p.dmod_stride}, {"dpost_weight", dpost_weight, p.C}, {"dweight", dweight, p.C}};
+  for (const auto& m : mods)
+    if (int rc = check_mod(m.name, m.ptr, m.stride, p)) return rc;
+  const size_t need = radial_norm_bwd_workspace(params);
+  if (!need) return fail(RADIAL_ESHAPE, "too many groups for one launch");
+  if (!workspace || ((uintptr_t)workspace & 255u)) return fail(RADIAL_ESHAPE, "workspace must be a 256-byte aligned device pointer");
+  if (workspace_bytes < need) return fail(RADIAL_ESHAPE, "workspace holds %zu bytes, %zu needed", workspace_bytes, need);
+
+  const Layout l = bwd_layout(p);
+  NormArgs a = common_args(p, l);
+  if (has_z) { a.r = arg(r); a.z = arg(dz); }
+  if (has_y) { a.y = arg(y); a.dy = arg(dy); }
+  if (dr.ptr) a.dr = arg(dr);
+  a.dx = arg(dx);
+  a.gate = gate; a.post_weight = post_weight; a.weight = weight; a.scale = scale;
+  a.partial = (float*)workspace;
+  a.wants = (dscale || dweight ? 1 : 0) | (dshift ? 2 : 0) | (dgate || dpost_weight ? 4 : 0);
+  bool vec = p.C % 8 == 0 && p.mod_stride % 4 == 0;
+  for (const radial_rows* t : {&r, &y, &dz, &dr, &dx, &dy})
+    if (t->ptr) vec = vec && aligned(t->ptr, t->stride_b, t->stride_n, size_of(t->type));
+  for (int i = 0; i < 4; ++i) vec = vec && ((uintptr_t)mods[i].ptr & 15u) == 0;
+  if (int rc = launch(a, dx.type, has_y ? y.type : dz.type, vec, true, l.groups * l.chunks, (hipStream_t)hip_stream)) return rc;
+  if (!a.wants) return RADIAL_OK;
+
+  GradArgs g = {};
+  g.partial = a.partial;
+  g.of_group = dweight || dpost_weight ? a.partial + (size_t)l.groups * l.chunks * 3 * p.C : nullptr;
+  g.gate = gate; g.post_weight = post_weight; g.weight = weight; g.scale = scale;
+  g.dgate = dgate; g.dscale = dscale; g.dshift = dshift; g.dpost_weight = dpost_weight; g.dweight = dweight;
+  g.C = p.C; g.chunks = l.chunks; g.groups = (int32_t)l.groups; g.wants = a.wants;
+  g.mod_stride = p.mod_stride; g.dmod_stride = p.dmod_stride;
+  const unsigned columns = (unsigned)((p.C + 63) / 64);
+  const dim3 block(64, kGradSlices);
+  const unsigned in_y = l.groups < 32768 ? (unsigned)l.groups : 32768u, in_z = (unsigned)((l.groups + 32767) / 32768);
+  norm_grad_kernel<<<dim3(columns, in_y, in_z), block, 0, (hipStream_t)hip_stream>>>(g);
+  RADIAL_HIP_TRY(hipGetLastError());
+  if (g.of_group) {
+    norm_weight_grad_kernel<<<dim3(columns), block, 0, (hipStream_t)hip_stream>>>(g);
+    RADIAL_HIP_TRY(hipGetLastError());
+  }
+  return RADIAL_OK;
+}

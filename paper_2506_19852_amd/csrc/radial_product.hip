@@ -1,0 +1,310 @@
+// 8-bit products for gfx950: matrices as E4M3 codes with a float32 scale for each 128 columns of a row, or for each block of 128 x 128, made by
+// quantize_groups_kernel, and their product
+//     C[m, n] = sum over groups g of  sa[g, m] sb[g, n] (A_g[m, :] . B_g[n, :]).
+// One group is the depth of one v_mfma_f32_16x16x128_f8f6f4, so a group's sum comes out of the matrix pipe whole and is scaled in float32.
+// The tile is computed transposed (matrix A operand = rows of B, B operand = rows of A): a lane then holds one row m of C and four
+// neighbouring columns n, so that sa is one value per lane and with blocks sa sb is one factor for all of a lane's sums.
+#include <math.h>
+
+#include "radial_layer_common.h"
+
+namespace radial {
+namespace {
+
+constexpr int kGroup = 128;
+constexpr float kLargest = 448.f;                  // of E4M3
+constexpr float kSmallestScale = 1.17549435e-38f;  // 2^-126
+
+// ---- codes and scales -----------------------------------------------------------------------------
+
+struct QuantArgs {
+  const void* x;
+  int64_t stride;
+  int32_t rows, cols;
+  uint8_t *codes, *codes_t;
+  float *scales, *scales_t;
+  int32_t col_tiles, row_tiles;
+  int32_t vec;  // rows start 16-byte aligned
+};
+
+// x / scale as float32: the product with the inverse, and what it leaves, once more; off by half a unit and 2^-46 of the value.  (A division
+// proper takes three times the instructions, twice per element.)  Infinite scales give NaN.
+struct Quotient {
+  float scale, inverse;
+  __device__ __forceinline__ explicit Quotient(float amax) {
+    scale = fmaxf(amax / kLargest, kSmallestScale);
+    inverse = 1.f / scale;
+  }
+  __device__ __forceinline__ float operator()(float x) const {
+    const float q = x * inverse;
+    return __builtin_fmaf(__builtin_fmaf(-q, scale, x), inverse, q);
+  }
+};
+
+__device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d) {
+  int v = 0;  // v_cvt_pk_fp8_f32 rounds to nearest even; no quotient rounds beyond 448
+  v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, v, false);
+  v = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
+  return (uint32_t)v;
+}
+
+// One workgroup per 128 x 128 tile; a thread holds eight rows of eight columns.  Codes along the rows go out as they are (16 lanes, 128 bytes); those of the
+// transpose pass through LDS in pieces of eight rows, exchanged by column so that the pieces of one write lie in different banks.
+template <class T, bool kBlocks, bool kRows, bool kCols>
+__global__ void __launch_bounds__(256) quantize_groups_kernel(QuantArgs a) {
+  __shared__ float wave_amax[4][kGroup];
+  __shared__ __align__(16) u32x2 turned[kCols ? kGroup * 16 : 1];
+  const int32_t row0 = blockIdx.x / a.col_tiles * kGroup, col0 = blockIdx.x % a.col_tiles * kGroup;
+  const int32_t tr = threadIdx.x >> 4, tc = threadIdx.x & 15, wave = threadIdx.x >> 6;
+  const int32_t r0 = row0 + tr * 8, c0 = col0 + tc * 8;
+  float v[8][8];
+  {
+    Eight<T> raw[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const T* p = (const T*)a.x + (int64_t)(r0 + i) * a.stride + c0;
+      if (r0 + i < a.rows && a.vec && c0 + 8 <= a.cols) {
+        raw[i].load(p);
+      } else {
+        T e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = r0 + i < a.rows && c0 + j < a.cols ? p[j] : (T)0.f;
+        raw[i] = __builtin_bit_cast(Eight<T>, e);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) raw[i].get(v[i]);
+  }
+  float of_row[8], of_col[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    of_row[i] = of_col[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      of_row[i] = fmaxf(of_row[i], fabsf(v[i][j]));
+      of_col[i] = fmaxf(of_col[i], fabsf(v[j][i]));
+    }
+  }
+  if constexpr (kBlocks || kRows) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      of_row[i] = max_dpp<kSwapOnes>(of_row[i]);
+      of_row[i] = max_dpp<kSwapTwos>(of_row[i]);
+      of_row[i] = max_dpp<kHalfRowMirror>(of_row[i]);
+      of_row[i] = max_dpp<kRowMirror>(of_row[i]);
+    }
+  }
+  if constexpr (kBlocks) {
+    float amax = of_row[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) amax = fmaxf(amax, of_row[i]);
+    if (tc == 0) wave_amax[0][tr] = amax;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) amax = fmaxf(amax, wave_amax[0][i]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) of_row[i] = of_col[i] = amax;
+  } else if constexpr (kCols) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      of_col[i] = fmaxf(of_col[i], __shfl_xor(of_col[i], 16));
+      of_col[i] = fmaxf(of_col[i], __shfl_xor(of_col[i], 32));
+    }
+    if ((threadIdx.x & 63) < 16) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) wave_amax[wave][tc * 8 + i] = of_col[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      of_col[i] = fmaxf(fmaxf(wave_amax[0][tc * 8 + i], wave_amax[1][tc * 8 + i]), fmaxf(wave_amax[2][tc * 8 + i], wave_amax[3][tc * 8 + i]));
+  }
+
+  const int32_t row_tile = row0 / kGroup, col_tile = col0 / kGroup;
+  u32x2 along[8];  // codes of a row's eight columns (blocks: the transpose's codes are these)
+  if constexpr (kRows) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const Quotient q(of_row[i]);
+      along[i] = u32x2{four_codes(q(v[i][0]), q(v[i][1]), q(v[i][2]), q(v[i][3])), four_codes(q(v[i][4]), q(v[i][5]), q(v[i][6]), q(v[i][7]))};
+      if (r0 + i < a.rows) {
+        *(u32x2*)(a.codes + ((int64_t)(r0 + i) * a.col_tiles + col_tile) * kGroup + tc * 8) = along[i];
+        if (!kBlocks && tc == 0) a.scales[(int64_t)col_tile * a.rows + r0 + i] = q.scale;
+        if (kBlocks && threadIdx.x == 0 && i == 0) a.scales[(int64_t)col_tile * a.row_tiles + row_tile] = q.scale;
+      }
+    }
+  }
+  if constexpr (kCols) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const Quotient q(of_col[j]);
+      const int32_t c = tc * 8 + j;
+      turned[c * 16 + (tr ^ tc)] =
+          u32x2{four_codes(q(v[0][j]), q(v[1][j]), q(v[2][j]), q(v[3][j])), four_codes(q(v[4][j]), q(v[5][j]), q(v[6][j]), q(v[7][j]))};
+      if (!kBlocks && tr == 0 && col0 + c < a.cols) a.scales_t[(int64_t)row_tile * a.cols + col0 + c] = q.scale;
+      if (kBlocks && threadIdx.x == 0 && j == 0) a.scales_t[(int64_t)row_tile * a.col_tiles + col_tile] = q.scale;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int32_t c = i * 32 + (threadIdx.x >> 3), piece = threadIdx.x & 7;
+      const u32x2 lo = turned[c * 16 + ((2 * piece) ^ (c >> 3))], hi = turned[c * 16 + ((2 * piece + 1) ^ (c >> 3))];
+      if (col0 + c < a.cols) *(u32x4*)(a.codes_t + ((int64_t)(col0 + c) * a.row_tiles + row_tile) * kGroup + piece * 16) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+    }
+  }
+}
+
+template <class T, bool kBlocks>
+void launch_quantize(const QuantArgs& a, unsigned grid, hipStream_t stream) {
+  if (a.codes && a.codes_t) quantize_groups_kernel<T, kBlocks, true, true><<<dim3(grid), dim3(256), 0, stream>>>(a);
+  else if (a.codes) quantize_groups_kernel<T, kBlocks, true, false><<<dim3(grid), dim3(256), 0, stream>>>(a);
+  else quantize_groups_kernel<T, kBlocks, false, true><<<dim3(grid), dim3(256), 0, stream>>>(a);
+}
+
+// ---- product ----------------------------------------------------------------------------------------
+
+struct ProductArgs {
+  const uint8_t *a, *b;
+  const float *sa, *sb;
+  __bf16* out;
+  int64_t out_stride;
+  int32_t M, N, groups;
+  int32_t b_blocks;  // 128-row blocks of B
+};
+
+__device__ __forceinline__ i32x8 sixteen_rows(const uint8_t* row) {
+  const u32x4 lo = *(const u32x4*)row, hi = *(const u32x4*)(row + 16);
+  return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+}
+
+// D[16 x 16] = A[16 x 128] B[128 x 16] of E4M3 codes: lane l supplies bytes 32 (l/16) .. + 31 of row l%16 on either side and
+// holds column l%16, rows 4 (l/16) .. + 3.  The pipe adds eight neighbouring products at a time and drops what is below 2^-13 of the largest
+// (a product of 2^-13 arrives beside 1, one of 2^-14 does not; eight places away both do); the bf16 instruction is exact to float32 but takes twice as long.
+__device__ __forceinline__ f32x4 product16(i32x8 a, i32x8 b) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0x7F7F7F7F, 0, 0x7F7F7F7F);
+}
+
+// Few rows: a workgroup of kParts waves takes 16 columns of C and 16 kTiles rows, each wave every kParts-th group, straight from memory (a
+// lane's 32 bytes of a row, four lanes a line).  The parts meet in LDS.
+constexpr int kParts = 8;
+template <bool kBlocks, int kTiles>
+__global__ void __launch_bounds__(64 * kParts) product_rows_kernel(ProductArgs a) {
+  __shared__ f32x4 parts[kParts][kTiles][64];
+  const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int32_t n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * kTiles;
+  const int64_t bytes = (int64_t)a.groups * kGroup;
+  const uint8_t* b_row = a.b + min(n0 + (lane & 15), a.N - 1) * bytes + (lane >> 4) * 32;
+  const uint8_t* a_row[kTiles];
+  int32_t m[kTiles], n[4];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    m[t] = min(m0 + 16 * t + (lane & 15), a.M - 1);
+    a_row[t] = a.a + m[t] * bytes + (lane >> 4) * 32;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) n[e] = min(n0 + 4 * (lane >> 4) + e, a.N - 1);
+  f32x4 sum[kTiles];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int32_t g = wave; g < a.groups; g += kParts) {
+    const i32x8 bf = sixteen_rows(b_row + (int64_t)g * kGroup);
+    float sb[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sb[e] = kBlocks ? a.sb[(int64_t)g * a.b_blocks + n0 / kGroup] : a.sb[(int64_t)g * a.N + n[e]];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      const f32x4 d = product16(bf, sixteen_rows(a_row[t] + (int64_t)g * kGroup));
+      const float sa = a.sa[(int64_t)g * a.M + m[t]];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[t][e] += d[e] * (sa * sb[e]);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) parts[wave][t][lane] = sum[t];
+  __syncthreads();
+  for (int t = wave; t < kTiles; t += kParts) {
+    f32x4 total = parts[0][t][lane];
+#pragma unroll
+    for (int w = 1; w < kParts; ++w) total += parts[w][t][lane];
+    const int32_t row = m0 + 16 * t + (lane & 15);
+    if (row >= a.M) continue;
+    __bf16* out = a.out + row * a.out_stride;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int32_t col = n0 + 4 * (lane >> 4) + e;
+      if (col < a.N) out[col] = (__bf16)total[e];
+    }
+  }
+}
+
+template <bool kBlocks>
+int launch_product(const ProductArgs& a, hipStream_t stream) {
+  const int64_t columns = (a.N + 15) / 16;
+  const int32_t tiles = a.M <= 16 ? 1 : a.M <= 32 ? 2 : 4;
+  const int64_t rows = (a.M + 16 * tiles - 1) / (16 * tiles);
+  if (rows > 65535) return fail(RADIAL_ESHAPE, "M is too large for one launch");
+  const dim3 grid((unsigned)columns, (unsigned)rows), block(64 * kParts);
+  if (tiles == 1) product_rows_kernel<kBlocks, 1><<<grid, block, 0, stream>>>(a);
+  else if (tiles == 2) product_rows_kernel<kBlocks, 2><<<grid, block, 0, stream>>>(a);
+  else product_rows_kernel<kBlocks, 4><<<grid, block, 0, stream>>>(a);
+  RADIAL_HIP_TRY(hipGetLastError());
+  return RADIAL_OK;
+}
+
+}  // namespace
+}  // namespace radial
+
+using namespace radial;
+
+extern "C" int radial_quantize_groups_fp8(int32_t rows, int32_t cols, const void* x, int32_t type, int64_t stride, int32_t grouping, uint8_t* codes,
+                                          float* scales, uint8_t* codes_t, float* scales_t, void* hip_stream) {
+  if (rows < 1 || cols < 1) return fail(RADIAL_EINVAL, "rows and cols must be >= 1");
+  if (!x) return fail(RADIAL_EINVAL, "x is NULL");
+  if (!is_type(type)) return fail(RADIAL_EINVAL, "type must be RADIAL_BF16 or RADIAL_F32 (got %d)", type);
+  if (grouping != RADIAL_GROUPS && grouping != RADIAL_BLOCKS) return fail(RADIAL_EINVAL, "grouping must be RADIAL_GROUPS or RADIAL_BLOCKS (got %d)", grouping);
+  if (!codes != !scales || !codes_t != !scales_t) return fail(RADIAL_EINVAL, "codes and scales go together");
+  if (!codes && !codes_t) return fail(RADIAL_EINVAL, "neither codes nor codes_t is given");
+  if ((uintptr_t)x % size_of(type)) return fail(RADIAL_ESHAPE, "x is not aligned to its elements");
+  if (stride < cols) return fail(RADIAL_ESHAPE, "stride must not be below cols");
+  if (((uintptr_t)codes | (uintptr_t)codes_t) & 15u) return fail(RADIAL_ESHAPE, "codes are not 16-byte aligned");
+  if (((uintptr_t)scales | (uintptr_t)scales_t) & 3u) return fail(RADIAL_ESHAPE, "scales are not aligned to their elements");
+  QuantArgs a = {};
+  a.x = x; a.stride = stride; a.rows = rows; a.cols = cols;
+  a.codes = codes; a.scales = scales; a.codes_t = codes_t; a.scales_t = scales_t;
+  a.row_tiles = (int32_t)(((int64_t)rows + kGroup - 1) / kGroup);
+  a.col_tiles = (int32_t)(((int64_t)cols + kGroup - 1) / kGroup);
+  a.vec = ((uintptr_t)x & 15u) == 0 && stride * size_of(type) % 16 == 0;
+  const int64_t grid = (int64_t)a.row_tiles * a.col_tiles;
+  if (rows > 0x7fffffff - kGroup || cols > 0x7fffffff - kGroup || grid > 0x7fffffffLL) return fail(RADIAL_ESHAPE, "x is too large for one launch");
+  hipStream_t stream = (hipStream_t)hip_stream;
+  if (type == RADIAL_F32) {
+    if (grouping == RADIAL_BLOCKS) launch_quantize<float, true>(a, (unsigned)grid, stream);
+    else launch_quantize<float, false>(a, (unsigned)grid, stream);
+  } else {
+    if (grouping == RADIAL_BLOCKS) launch_quantize<__bf16, true>(a, (unsigned)grid, stream);
+    else launch_quantize<__bf16, false>(a, (unsigned)grid, stream);
+  }
+  RADIAL_HIP_TRY(hipGetLastError());
+  return RADIAL_OK;
+}
+
+extern "C" int radial_product_fp8(int32_t M, int32_t N, int32_t K, const uint8_t* a_codes, const float* a_scales, const uint8_t* b_codes,
+                                  const float* b_scales, int32_t b_grouping, void* out, int64_t out_stride, void* hip_stream) {
+  if (M < 1 || N < 1 || K < 1) return fail(RADIAL_EINVAL, "M, N, K must be >= 1");
+  if (!a_codes || !a_scales || !b_codes || !b_scales || !out) return fail(RADIAL_EINVAL, "codes, scales or out is NULL");
+  if (b_grouping != RADIAL_GROUPS && b_grouping != RADIAL_BLOCKS) return fail(RADIAL_EINVAL, "b_grouping must be RADIAL_GROUPS or RADIAL_BLOCKS (got %d)", b_grouping);
+  if (((uintptr_t)a_codes | (uintptr_t)b_codes) & 15u) return fail(RADIAL_ESHAPE, "codes are not 16-byte aligned");
+  if (((uintptr_t)a_scales | (uintptr_t)b_scales) & 3u) return fail(RADIAL_ESHAPE, "scales are not aligned to their elements");
+  if ((uintptr_t)out & 1u) return fail(RADIAL_ESHAPE, "out is not aligned to its elements");
+  if (out_stride < N) return fail(RADIAL_ESHAPE, "out_stride must not be below N");
+  if (M > 0x7fffffff - 512 || N > 0x7fffffff - 512 || K > 0x7fffffff - 512) return fail(RADIAL_ESHAPE, "M, N, K are too large for one launch");
+  ProductArgs a = {};
+  a.a = a_codes; a.b = b_codes; a.sa = a_scales; a.sb = b_scales;
+  a.out = (__bf16*)out; a.out_stride = out_stride;
+  a.M = M; a.N = N;
+  a.groups = (K + kGroup - 1) / kGroup;
+  a.b_blocks = (N + kGroup - 1) / kGroup;
+  hipStream_t stream = (hipStream_t)hip_stream;
+  const bool blocks = b_grouping == RADIAL_BLOCKS;
+  return blocks ? launch_product<true>(a, stream) : launch_product<false>(a, stream);
+}
