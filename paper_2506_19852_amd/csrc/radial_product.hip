@@ -6,6 +6,8 @@
 // neighbouring columns n, so that sa is one value per lane and with blocks sa sb is one factor for all of a lane's sums.
 #include <math.h>
 
+#include <type_traits>
+
 #include "radial_layer_common.h"
 
 namespace radial {
@@ -170,6 +172,7 @@ struct ProductArgs {
   int64_t out_stride;
   int32_t M, N, groups;
   int32_t b_blocks;  // 128-row blocks of B
+  int32_t vec;       // rows of out start 16-byte aligned
 };
 
 __device__ __forceinline__ i32x8 sixteen_rows(const uint8_t* row) {
@@ -181,7 +184,7 @@ __device__ __forceinline__ i32x8 sixteen_rows(const uint8_t* row) {
 // holds column l%16, rows 4 (l/16) .. + 3.  The pipe adds eight neighbouring products at a time and drops what is below 2^-13 of the largest
 // (a product of 2^-13 arrives beside 1, one of 2^-14 does not; eight places away both do); the bf16 instruction is exact to float32 but takes twice as long.
 __device__ __forceinline__ f32x4 product16(i32x8 a, i32x8 b) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0x7F7F7F7F, 0, 0x7F7F7F7F);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);  // formats 0: E4M3; no block exponents
 }
 
 // Few rows: a workgroup of kParts waves takes 16 columns of C and 16 kTiles rows, each wave every kParts-th group, straight from memory (a
@@ -237,8 +240,218 @@ __global__ void __launch_bounds__(64 * kParts) product_rows_kernel(ProductArgs a
   }
 }
 
+// Many rows: a workgroup takes a tile of 16 kMTiles kWavesM x 64 kWavesN, stage by stage of one group (128 bytes of every row), which copies put into
+// LDS one stage ahead, straight from memory; a wave takes 16 kMTiles rows of 64 columns.  It holds the four fragments of its columns
+// and walks the fragments of its rows: four matrix instructions each, whose sums are scaled and added while the next ones run.
+template <int kWavesM, int kWavesN, int kMTiles>
+struct TileShape {
+  static constexpr int kWaves = kWavesM * kWavesN;
+  static constexpr int kTileM = 16 * kMTiles * kWavesM, kTileN = 64 * kWavesN;
+  static constexpr int kCodes = (kTileM + kTileN) * kGroup;       // bytes of a stage: rows of A, then of B, 128 each
+  static constexpr int kStage = kCodes + (kTileM + kTileN) * 4;   // and their scales
+  static constexpr int kLds = 2 * kStage;
+  static constexpr int kCopies = kCodes / 1024 / kWaves;          // of a wave
+  static_assert(kCodes % (1024 * kWaves) == 0 && (kTileM + kTileN) % 64 == 0 && (kTileM + kTileN) / 64 <= kWaves, "whole copies");
+};
+
+// Where piece p (16 bytes) of row r of an operand lies: two rows to a line of 256 bytes, pieces exchanged within it so that the 16 lanes that read one piece
+// of 16 rows meet 16 different banks of 16 bytes: of A 16 neighbouring rows, of B rows 16 i + 4 t + j, i and j below 4.  The exchange is the
+// same for all fragments of a lane, so that they are at constant distances from one another.
+template <bool kB>
+__device__ __forceinline__ int exchange_of(int line) { return kB ? (line & 1) | (line >> 3 & 3) << 1 : line & 7; }
+template <bool kB>
+__device__ __forceinline__ int code_piece(int r, int p) {
+  const int line = r >> 1, slot = (r & 1) * 8 + p;
+  return (line << 8) + ((slot ^ exchange_of<kB>(line)) << 4);
+}
+
+// Tile of a workgroup.  XCD x of 8 (workgroup id mod 8) gets a run of neighbouring tiles, in bands of 8 rows of tiles, column by column: the 32 that
+// it works on at a time are 8 x 4, whose codes it fetches into its L2 once.
+__device__ __forceinline__ void tile_of(uint32_t id, int32_t tiles_m, int32_t tiles_n, int32_t& m, int32_t& n) {
+  constexpr uint32_t kXcds = 8, kBand = 8;
+  const uint32_t tiles = (uint32_t)tiles_m * tiles_n, each = tiles / kXcds, more = tiles % kXcds;
+  const uint32_t xcd = id % kXcds, at = xcd * each + (xcd < more ? xcd : more) + id / kXcds;
+  const uint32_t band = at / (kBand * tiles_n), in_band = at - band * kBand * tiles_n;
+  const uint32_t rows = min(kBand, (uint32_t)tiles_m - band * kBand);
+  m = band * kBand + in_band % rows;
+  n = in_band / rows;
+}
+
+template <int kWavesM, int kWavesN, int kMTiles, bool kBlocks>
+__global__ void __launch_bounds__(64 * kWavesM * kWavesN) product_tile_kernel(ProductArgs a) {
+  using S = TileShape<kWavesM, kWavesN, kMTiles>;
+  extern __shared__ __align__(1024) char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int32_t m0, n0;
+  {
+    const int32_t tiles_m = (a.M + S::kTileM - 1) / S::kTileM, tiles_n = (a.N + S::kTileN - 1) / S::kTileN;
+    tile_of(blockIdx.x, tiles_m, tiles_n, m0, n0);
+    m0 *= S::kTileM;
+    n0 *= S::kTileN;
+  }
+  const int64_t bytes = (int64_t)a.groups * kGroup;
+  const uint8_t* a_base = a.a + m0 * bytes;
+  const uint8_t* b_base = a.b + n0 * bytes;
+  const uint32_t lds0 = lds_address(lds);
+
+  // This wave's copies: 8 rows of 128 bytes each; a lane's source row and piece are those that belong at its place.  Rows beyond the matrix
+  // repeat its last one.
+  uint32_t from[S::kCopies];
+#pragma unroll
+  for (int i = 0; i < S::kCopies; ++i) {
+    const int copy = wave * S::kCopies + i;
+    const bool of_a = copy * 8 < S::kTileM;
+    const int place = (of_a ? copy : copy - S::kTileM / 8) * 64 + lane, line = place >> 4;
+    const int source = (place & 15) ^ (of_a ? exchange_of<false>(line) : exchange_of<true>(line));
+    const int32_t r = min(line * 2 + (source >> 3), (of_a ? a.M - m0 : a.N - n0) - 1);
+    from[i] = (uint32_t)(r * (int32_t)bytes + (source & 7) * 16);
+  }
+  const int scale_row = wave * 64 + lane;  // of the tile's rows of A, then B: waves 0 .. copy 64 scales each
+  const bool has_scales = wave * 64 < S::kTileM + (kBlocks ? 0 : S::kTileN);
+  uint32_t scale_from = 0;
+  {
+    const bool of_a = scale_row < S::kTileM;
+    scale_from = 4u * (uint32_t)(of_a ? min(m0 + scale_row, a.M - 1) : min(n0 + scale_row - S::kTileM, a.N - 1));
+  }
+  auto copy_stage = [&](int32_t g, int i) __attribute__((always_inline)) {
+    const int copy = wave * S::kCopies + i;
+    const uint8_t* base = (copy * 8 < S::kTileM ? a_base : b_base) + (int64_t)g * kGroup;
+    copy16_to_lds_sv(base, from[i], lds0 + (g & 1) * S::kStage + copy * 1024);
+  };
+  auto copy_scales = [&](int32_t g) __attribute__((always_inline)) {
+    const float* base = wave * 64 < S::kTileM ? a.sa + (int64_t)g * a.M : a.sb + (int64_t)g * a.N;
+    copy4_to_lds_sv_masked(base, scale_from, lds0 + (g & 1) * S::kStage + S::kCodes + wave * 256, has_scales ? ~0ull : 0ull);
+  };
+
+  const int wm = wave / kWavesN, wn = wave % kWavesN;
+  const int l16 = lane & 15, q = lane >> 4;
+  f32x4 sum[kMTiles][4];
+#pragma unroll
+  for (int i = 0; i < kMTiles; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+#pragma unroll
+  for (int i = 0; i < S::kCopies; ++i) copy_stage(0, i);
+  copy_scales(0);
+
+  // A lane's 32 bytes of a row are pieces q and q + 4, the same on both sides (which bytes make up a lane's part does not matter): a read is served 16
+  // lanes at a time, lanes 0 .. 3, 12 .. 15, 20 .. 27 first, and neighbouring pieces of those rows lie in different banks.  With pieces 2 q and 2 q + 1
+  // they met two by two: 0.31 of 1.78 million cycles at 32 760 x 5120 x 5120.
+  uint32_t a_at[2], b_at[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    a_at[h] = lds0 + wm * kMTiles * 16 * kGroup + code_piece<false>(l16, q + 4 * h);
+    b_at[h] = lds0 + (S::kTileM + wn * 64) * kGroup + code_piece<true>((l16 >> 2) * 16 + (l16 & 3), q + 4 * h);
+  }
+  const uint32_t a_scale_at = lds0 + S::kCodes + (wm * kMTiles * 16 + l16) * 4;
+  const uint32_t b_scale_at = lds0 + S::kCodes + (S::kTileM + wn * 64 + q * 16) * 4;
+  using Lds = __attribute__((address_space(3))) const char*;
+  auto fragment = [&](const Lds (&at)[2], int distance) __attribute__((always_inline)) -> i32x8 {
+    using Piece = __attribute__((address_space(3))) const u32x4*;
+    const u32x4 lo = *(Piece)(at[0] + distance), hi = *(Piece)(at[1] + distance);
+    return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  };
+  auto walk = [&](int32_t g, auto more_) __attribute__((always_inline)) {
+    constexpr bool more = decltype(more_)::value;
+    wait_all_copies();
+    __syncthreads();
+    const uint32_t stage = (g & 1) * S::kStage;
+    const Lds at_a[2] = {lds_pointer<const char>(a_at[0] + stage), lds_pointer<const char>(a_at[1] + stage)};
+    const Lds at_b[2] = {lds_pointer<const char>(b_at[0] + stage), lds_pointer<const char>(b_at[1] + stage)};
+    const auto* a_scales = lds_pointer<const float>(a_scale_at + stage);
+    const auto* b_scales = lds_pointer<const f32x4>(b_scale_at + stage);
+    if (more) copy_scales(g + 1);
+    // Row 4 i + j of fragment t is column 16 i + 4 t + j of the wave's 64: a lane's sums of the four are 16 neighbouring columns.
+    i32x8 columns[4];
+    f32x4 sb[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      columns[t] = fragment(at_b, t * 4 * kGroup);
+      if (!kBlocks) sb[t] = b_scales[t];
+    }
+    const float of_block = kBlocks ? a.sb[(int64_t)g * a.b_blocks + min((n0 + wn * 64) / kGroup, a.b_blocks - 1)] : 0.f;
+    // The sums of one row fragment are added between the matrix instructions of the next: each has the time of three to come out of the pipe.
+    i32x8 rows = fragment(at_a, 0);
+    float factor = a_scales[0], before = 0.f;
+    f32x4 d[4];
+#pragma unroll
+    for (int i = 0; i <= kMTiles; ++i) {
+      i32x8 next;
+      float next_factor = 0.f;
+      if (i + 1 < kMTiles) {
+        next = fragment(at_a, (i + 1) * 16 * kGroup);
+        next_factor = a_scales[(i + 1) * 16];
+      }
+      if (more && i < kMTiles) {
+#pragma unroll
+        for (int c = i * S::kCopies / kMTiles; c < (i + 1) * S::kCopies / kMTiles; ++c) copy_stage(g + 1, c);
+      }
+      if (kBlocks) factor *= of_block;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if (i > 0) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[i - 1][t][e] = __builtin_fmaf(d[t][e], kBlocks ? before : before * sb[t][e], sum[i - 1][t][e]);
+        }
+        if (i < kMTiles) d[t] = product16(columns[t], rows);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      before = factor;
+      rows = next;
+      factor = next_factor;
+    }
+  };
+  for (int32_t g = 0; g + 1 < a.groups; ++g) walk(g, std::true_type());
+  walk(a.groups - 1, std::false_type());
+
+#pragma unroll
+  for (int i = 0; i < kMTiles; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(sum[i][j]));  // the last sums are added here, not where they are stored, which would hold both parts of each
+#pragma unroll
+  for (int i = 0; i < kMTiles; ++i) {
+    const int32_t m = m0 + (wm * kMTiles + i) * 16 + l16;
+    if (m >= a.M) continue;
+    const int32_t n = n0 + wn * 64 + q * 16;
+    __bf16* out = a.out + m * a.out_stride + n;
+    uint32_t pair[8];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      pair[2 * t] = pack_bf16(sum[i][t][0], sum[i][t][1]);
+      pair[2 * t + 1] = pack_bf16(sum[i][t][2], sum[i][t][3]);
+    }
+    if (a.vec && n + 16 <= a.N) {
+      *(u32x4*)out = u32x4{pair[0], pair[1], pair[2], pair[3]};
+      *(u32x4*)(out + 8) = u32x4{pair[4], pair[5], pair[6], pair[7]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (n + e < a.N) out[e] = (__bf16)sum[i][e / 4][e % 4];
+    }
+  }
+}
+
+template <int kWavesM, int kWavesN, int kMTiles, bool kBlocks>
+int launch_tiles(const ProductArgs& a, hipStream_t stream) {
+  using S = TileShape<kWavesM, kWavesN, kMTiles>;
+  const int64_t tiles = ((int64_t)a.M + S::kTileM - 1) / S::kTileM * (((int64_t)a.N + S::kTileN - 1) / S::kTileN);
+  if (tiles > 0x7fffffffLL) return fail(RADIAL_ESHAPE, "M*N is too large for one launch");
+  if constexpr (S::kLds > 65536) {
+    static DeviceOnce configured;
+    if (int rc = allow_dynamic_lds(configured, (const void*)product_tile_kernel<kWavesM, kWavesN, kMTiles, kBlocks>, S::kLds)) return rc;
+  }
+  product_tile_kernel<kWavesM, kWavesN, kMTiles, kBlocks><<<dim3((unsigned)tiles), dim3(64 * S::kWaves), S::kLds, stream>>>(a);
+  RADIAL_HIP_TRY(hipGetLastError());
+  return RADIAL_OK;
+}
+
 template <bool kBlocks>
 int launch_product(const ProductArgs& a, hipStream_t stream) {
+  if (a.M > 64) {
+    const int64_t large = (int64_t)((a.M + 255) / 256) * ((a.N + 255) / 256);
+    return large >= 256 ? launch_tiles<2, 4, 8, kBlocks>(a, stream) : launch_tiles<2, 2, 4, kBlocks>(a, stream);
+  }
   const int64_t columns = (a.N + 15) / 16;
   const int32_t tiles = a.M <= 16 ? 1 : a.M <= 32 ? 2 : 4;
   const int64_t rows = (a.M + 16 * tiles - 1) / (16 * tiles);
@@ -304,6 +517,7 @@ extern "C" int radial_product_fp8(int32_t M, int32_t N, int32_t K, const uint8_t
   a.M = M; a.N = N;
   a.groups = (K + kGroup - 1) / kGroup;
   a.b_blocks = (N + kGroup - 1) / kGroup;
+  a.vec = ((uintptr_t)out & 15u) == 0 && out_stride % 8 == 0;
   hipStream_t stream = (hipStream_t)hip_stream;
   const bool blocks = b_grouping == RADIAL_BLOCKS;
   return blocks ? launch_product<true>(a, stream) : launch_product<false>(a, stream);
