@@ -352,6 +352,11 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN) product_tile_kernel(Pr
     const u32x4 lo = *(Piece)(at[0] + distance), hi = *(Piece)(at[1] + distance);
     return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
   };
+  // The wave's columns are of one block; its scale is a scalar, asked for one stage ahead.  (A vector load would wait for the copies, which come before it.)
+  using Scalars = const float __attribute__((address_space(4)))*;
+  const Scalars block_scales = (Scalars)(a.sb + min((n0 + wn * 64) / kGroup, a.b_blocks - 1));
+  auto block_scale = [&](int32_t g) __attribute__((always_inline)) { return block_scales[(int64_t)g * a.b_blocks]; };
+  float next_block = kBlocks ? block_scale(0) : 0.f;
   auto walk = [&](int32_t g, auto more_) __attribute__((always_inline)) {
     constexpr bool more = decltype(more_)::value;
     wait_all_copies();
@@ -370,7 +375,8 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN) product_tile_kernel(Pr
       columns[t] = fragment(at_b, t * 4 * kGroup);
       if (!kBlocks) sb[t] = b_scales[t];
     }
-    const float of_block = kBlocks ? a.sb[(int64_t)g * a.b_blocks + min((n0 + wn * 64) / kGroup, a.b_blocks - 1)] : 0.f;
+    const float of_block = next_block;
+    if (kBlocks && more) next_block = block_scale(g + 1);
     // The sums of one row fragment are added between the matrix instructions of the next: each has the time of three to come out of the pipe.
     i32x8 rows = fragment(at_a, 0);
     float factor = a_scales[0], before = 0.f;
@@ -385,7 +391,7 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN) product_tile_kernel(Pr
       }
       if (more && i < kMTiles) {
 #pragma unroll
-        for (int c = i * S::kCopies / kMTiles; c < (i + 1) * S::kCopies / kMTiles; ++c) copy_stage(g + 1, c);
+        for (int c = 2 * i * S::kCopies / kMTiles; c < 2 * (i + 1) * S::kCopies / kMTiles && c < S::kCopies; ++c) copy_stage(g + 1, c);
       }
       if (kBlocks) factor *= of_block;
 #pragma unroll
