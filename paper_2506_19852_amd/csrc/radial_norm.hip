@@ -52,7 +52,7 @@ template <bool kVec, int V>
 struct Channels {
   int32_t first, width, C;
   __device__ __forceinline__ int32_t at(int v, int e) const { return kVec ? (v * width + first) * 8 + e : (v * 8 + e) * width + first; }
-  __device__ __forceinline__ bool has(int v, int e) const { return at(v, e) < C; }
+  __device__ __forceinline__ bool has(int v, int e) const { return at(v, kVec ? 0 : e) < C; }  // vectors: all eight or none
   __device__ __forceinline__ int32_t count() const {
     int32_t n = 0;
 #pragma unroll
@@ -78,6 +78,15 @@ struct Held {
     } else {
 #pragma unroll
       for (int i = 0; i < 8 * V; ++i) single[i] = ch.has(i / 8, i % 8) ? row[ch.at(i / 8, i % 8)] : (T)0.f;
+    }
+  }
+  __device__ __forceinline__ void clear() {
+    if constexpr (kVec) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) piece[v].clear();
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8 * V; ++i) single[i] = (T)0.f;
     }
   }
   __device__ __forceinline__ void get(float (&out)[8 * V]) const {
@@ -265,14 +274,23 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) norm_fwd_kernel(NormArgs a
     for (int i = 0; i < E; ++i) factor[i] = (1.f + factor[i]) * w[i];
     load_mod<kVec, V>(shift, a.shift ? a.shift + mod : nullptr, 0.f, s.ch);
   }
-  Held<XT, kVec, V> x;
-  Held<YT, kVec, V> y;
-  // Teams of a wave end together: lanes without a row work on the last one and store nothing.
+  // The next row is fetched while one is worked on.
+  Held<XT, kVec, V> x, next_x;
+  Held<YT, kVec, V> y, next_y;
+  auto fetch = [&](int32_t n) __attribute__((always_inline)) {
+    if (n >= s.last) return;
+    next_x.load(row_of<XT>(a.x, s.b, n), s.ch);
+    if (a.y.ptr) next_y.load(row_of<YT>(a.y, s.b, n), s.ch);
+  };
+  next_x.clear();
+  next_y.clear();
+  fetch(s.first);
+  // Teams of a wave end together: a team without a row left works on its last one again and stores nothing.
   for (int32_t n = s.first; kWide ? n < s.last : __any(n < s.last); n += s.teams) {
     const bool live = kWide || n < s.last;
-    const int32_t row = live ? n : s.last - 1;
-    x.load(row_of<XT>(a.x, s.b, row), s.ch);
-    if (a.y.ptr) y.load(row_of<YT>(a.y, s.b, row), s.ch);
+    x = next_x;
+    y = next_y;
+    fetch(n + s.teams);
     float r[E];
     x.get(r);
     if (a.y.ptr) {
@@ -286,14 +304,14 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) norm_fwd_kernel(NormArgs a
       }
 #pragma unroll
       for (int i = 0; i < E; ++i) r[i] = s.ch.has(i / 8, i % 8) ? a.residual_scale * r[i] + gate[i] * u[i] : 0.f;
-      if (live) store_row<XT, kVec, V>(row_of<XT>(a.r, s.b, row), r, s.ch);
+      if (live) store_row<XT, kVec, V>(row_of<XT>(a.r, s.b, n), r, s.ch);
     }
     if (a.pre != RADIAL_NORM_NONE) {
       float mean, inverse;
       statistics<kVec, V>(r, a.pre, a.eps, s.team, s.ch, s.own_count, mean, inverse);
 #pragma unroll
       for (int i = 0; i < E; ++i) r[i] = (r[i] - mean) * inverse * factor[i] + shift[i];
-      if (live) store_row<YT, kVec, V>(row_of<YT>(a.z, s.b, row), r, s.ch);
+      if (live) store_row<YT, kVec, V>(row_of<YT>(a.z, s.b, n), r, s.ch);
     }
   }
 }
@@ -321,17 +339,29 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) norm_bwd_kernel(NormArgs a
   float P[E], T[E], Q[E];
 #pragma unroll
   for (int i = 0; i < E; ++i) P[i] = T[i] = Q[i] = 0.f;
-  Held<XT, kVec, V> r_held, dr_held;
-  Held<YT, kVec, V> y_held, dz_held;
-  for (int32_t row_n = s.first; kWide ? row_n < s.last : __any(row_n < s.last); row_n += s.teams) {
-    const bool live = kWide || row_n < s.last;
-    const int32_t row = live ? row_n : s.last - 1;
+  Held<XT, kVec, V> r_held, dr_held, next_r, next_dr;
+  Held<YT, kVec, V> y_held, dz_held, next_y, next_dz;
+  auto fetch = [&](int32_t n) __attribute__((always_inline)) {
+    if (n >= s.last) return;
     if (has_z) {
-      r_held.load(row_of<XT>(a.r, s.b, row), s.ch);
-      dz_held.load(row_of<YT>(a.z, s.b, row), s.ch);
+      next_r.load(row_of<XT>(a.r, s.b, n), s.ch);
+      next_dz.load(row_of<YT>(a.z, s.b, n), s.ch);
     }
-    if (a.dr.ptr) dr_held.load(row_of<XT>(a.dr, s.b, row), s.ch);
-    if (has_y) y_held.load(row_of<YT>(a.y, s.b, row), s.ch);
+    if (a.dr.ptr) next_dr.load(row_of<XT>(a.dr, s.b, n), s.ch);
+    if (has_y) next_y.load(row_of<YT>(a.y, s.b, n), s.ch);
+  };
+  next_r.clear();
+  next_dr.clear();
+  next_y.clear();
+  next_dz.clear();
+  fetch(s.first);
+  for (int32_t row = s.first; kWide ? row < s.last : __any(row < s.last); row += s.teams) {
+    const bool live = kWide || row < s.last;
+    r_held = next_r;
+    dr_held = next_dr;
+    y_held = next_y;
+    dz_held = next_dz;
+    fetch(row + s.teams);
     float D[E];
     if (a.dr.ptr) {
       dr_held.get(D);

@@ -187,71 +187,59 @@ __device__ __forceinline__ f32x4 product16(i32x8 a, i32x8 b) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);  // formats 0: E4M3; no block exponents
 }
 
-// Few rows: a workgroup of kParts waves takes 16 columns of C and 16 kTiles rows, each wave every kParts-th group, straight from memory (a
-// lane's 32 bytes of a row, four lanes a line).  The parts meet in LDS.
+// Up to 16 rows: bound by reading B.  A workgroup of 8 waves takes 16 columns of C, each wave every 8th group, straight from memory (a lane's 32
+// bytes of a row, four lanes a line); the parts meet in LDS.  5120 x 5120, 2 rows: 8.7 us with the launch (a tile of 64 x 64: 11.4); 40 rows,
+// three blocks of 16: 22.1 (11.5).
 constexpr int kParts = 8;
-template <bool kBlocks, int kTiles>
+template <bool kBlocks>
 __global__ void __launch_bounds__(64 * kParts) product_rows_kernel(ProductArgs a) {
-  __shared__ f32x4 parts[kParts][kTiles][64];
+  __shared__ f32x4 parts[kParts][64];
   const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int32_t n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * kTiles;
+  const int32_t n0 = blockIdx.x * 16, m = lane & 15, row = min(m, a.M - 1);
   const int64_t bytes = (int64_t)a.groups * kGroup;
   const uint8_t* b_row = a.b + min(n0 + (lane & 15), a.N - 1) * bytes + (lane >> 4) * 32;
-  const uint8_t* a_row[kTiles];
-  int32_t m[kTiles], n[4];
+  const uint8_t* a_row = a.a + row * bytes + (lane >> 4) * 32;
+  int32_t n[4];
 #pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
-    m[t] = min(m0 + 16 * t + (lane & 15), a.M - 1);
-    a_row[t] = a.a + m[t] * bytes + (lane >> 4) * 32;
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) n[e] = min(n0 + 4 * (lane >> 4) + e, a.N - 1);
-  f32x4 sum[kTiles];
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int e = 0; e < 4; ++e) n[e] = n0 + 4 * (lane >> 4) + e;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   for (int32_t g = wave; g < a.groups; g += kParts) {
-    const i32x8 bf = sixteen_rows(b_row + (int64_t)g * kGroup);
-    float sb[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sb[e] = kBlocks ? a.sb[(int64_t)g * a.b_blocks + n0 / kGroup] : a.sb[(int64_t)g * a.N + n[e]];
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      const f32x4 d = product16(bf, sixteen_rows(a_row[t] + (int64_t)g * kGroup));
-      const float sa = a.sa[(int64_t)g * a.M + m[t]];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[t][e] += d[e] * (sa * sb[e]);
-    }
-  }
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) parts[wave][t][lane] = sum[t];
-  __syncthreads();
-  for (int t = wave; t < kTiles; t += kParts) {
-    f32x4 total = parts[0][t][lane];
-#pragma unroll
-    for (int w = 1; w < kParts; ++w) total += parts[w][t][lane];
-    const int32_t row = m0 + 16 * t + (lane & 15);
-    if (row >= a.M) continue;
-    __bf16* out = a.out + row * a.out_stride;
+    const f32x4 d = product16(sixteen_rows(b_row + (int64_t)g * kGroup), sixteen_rows(a_row + (int64_t)g * kGroup));
+    const float sa = a.sa[(int64_t)g * a.M + row];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int32_t col = n0 + 4 * (lane >> 4) + e;
-      if (col < a.N) out[col] = (__bf16)total[e];
+      const float sb = kBlocks ? a.sb[(int64_t)g * a.b_blocks + n0 / kGroup] : a.sb[(int64_t)g * a.N + min(n[e], a.N - 1)];
+      sum[e] = __builtin_fmaf(d[e], sa * sb, sum[e]);
     }
   }
+  parts[wave][lane] = sum;
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int w = 1; w < kParts; ++w) sum += parts[w][lane];
+  if (m >= a.M) return;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (n[e] < a.N) a.out[m * a.out_stride + n[e]] = (__bf16)sum[e];
 }
 
 // Many rows: a workgroup takes a tile of 16 kMTiles kWavesM x 64 kWavesN, stage by stage of one group (128 bytes of every row), which copies put into
 // LDS one stage ahead, straight from memory; a wave takes 16 kMTiles rows of 64 columns.  It holds the four fragments of its columns
 // and walks the fragments of its rows: four matrix instructions each, whose sums are scaled and added while the next ones run.
-template <int kWavesM, int kWavesN, int kMTiles>
+template <int kWavesM, int kWavesN, int kMTiles, int kStages, int kSplit>
 struct TileShape {
-  static constexpr int kWaves = kWavesM * kWavesN;
+  static constexpr int kWaves = kWavesM * kWavesN;  // of one part of the groups
   static constexpr int kTileM = 16 * kMTiles * kWavesM, kTileN = 64 * kWavesN;
-  static constexpr int kCodes = (kTileM + kTileN) * kGroup;       // bytes of a stage: rows of A, then of B, 128 each
-  static constexpr int kStage = kCodes + (kTileM + kTileN) * 4;   // and their scales
-  static constexpr int kLds = 2 * kStage;
-  static constexpr int kCopies = kCodes / 1024 / kWaves;          // of a wave
-  static_assert(kCodes % (1024 * kWaves) == 0 && (kTileM + kTileN) % 64 == 0 && (kTileM + kTileN) / 64 <= kWaves, "whole copies");
+  static constexpr int kCodes = (kTileM + kTileN) * kGroup;                              // bytes of a stage: rows of A, then of B, 128 each
+  static constexpr int kCopies = kCodes / 1024 / kWaves;                                 // of a wave
+  static constexpr int kScaleCopies = ((kTileM + kTileN) / 64 + kWaves - 1) / kWaves;    // of a wave, 64 scales each; what is left over copies more
+  static constexpr int kStage = kCodes + kScaleCopies * kWaves * 256;                    // and the rows' scales
+  static constexpr int kRing = kStages * kStage;                                         // of one part
+  static constexpr int kMerge = (kSplit - 1) * kWaves * kMTiles * 4096;                  // sums of the other parts
+  static constexpr int kLds = kSplit * kRing > kMerge ? kSplit * kRing : kMerge;
+  static constexpr int kAhead = kStages - 1;                                             // stages between a copy and its use
+  static constexpr int kInFlight = (kStages - 2) * (kCopies + kScaleCopies);             // copies of a wave that may be under way when a stage begins
+  static_assert(kCodes % (1024 * kWaves) == 0 && kTileM % 64 == 0 && kLds <= 160 * 1024 && kInFlight <= 63, "whole copies, counted");
 };
 
 // Where piece p (16 bytes) of row r of an operand lies: two rows to a line of 256 bytes, pieces exchanged within it so that the 16 lanes that read one piece
@@ -263,6 +251,14 @@ template <bool kB>
 __device__ __forceinline__ int code_piece(int r, int p) {
   const int line = r >> 1, slot = (r & 1) * 8 + p;
   return (line << 8) + ((slot ^ exchange_of<kB>(line)) << 4);
+}
+
+// Until at most kLeft copies of this wave are under way.
+template <int kLeft>
+__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLeft) : "memory"); }
+// 256 bytes from memory to LDS, 4 to a lane; see copy16_to_lds_sv.
+__device__ __forceinline__ void copy4_to_lds_sv(const void* base, uint32_t byte_offset, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_addr), "v"(byte_offset), "s"(base) : "memory", "m0");
 }
 
 // Tile of a workgroup.  XCD x of 8 (workgroup id mod 8) gets a run of neighbouring tiles, in bands of 8 rows of tiles, column by column: the 32 that
@@ -277,11 +273,12 @@ __device__ __forceinline__ void tile_of(uint32_t id, int32_t tiles_m, int32_t ti
   n = in_band / rows;
 }
 
-template <int kWavesM, int kWavesN, int kMTiles, bool kBlocks>
-__global__ void __launch_bounds__(64 * kWavesM * kWavesN) product_tile_kernel(ProductArgs a) {
-  using S = TileShape<kWavesM, kWavesN, kMTiles>;
+template <int kWavesM, int kWavesN, int kMTiles, int kStages, int kSplit, bool kBlocks>
+__global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) product_tile_kernel(ProductArgs a) {
+  using S = TileShape<kWavesM, kWavesN, kMTiles, kStages, kSplit>;
   extern __shared__ __align__(1024) char lds[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave_of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int part = kSplit == 1 ? 0 : wave_of_all / S::kWaves, wave = wave_of_all - part * S::kWaves;
   int32_t m0, n0;
   {
     const int32_t tiles_m = (a.M + S::kTileM - 1) / S::kTileM, tiles_n = (a.N + S::kTileN - 1) / S::kTileN;
@@ -292,11 +289,11 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN) product_tile_kernel(Pr
   const int64_t bytes = (int64_t)a.groups * kGroup;
   const uint8_t* a_base = a.a + m0 * bytes;
   const uint8_t* b_base = a.b + n0 * bytes;
-  const uint32_t lds0 = lds_address(lds);
+  const uint32_t lds0 = lds_address(lds) + part * S::kRing;
 
   // This wave's copies: 8 rows of 128 bytes each; a lane's source row and piece are those that belong at its place.  Rows beyond the matrix
   // repeat its last one.
-  uint32_t from[S::kCopies];
+  uint32_t from[S::kCopies], scale_from[S::kScaleCopies];
 #pragma unroll
   for (int i = 0; i < S::kCopies; ++i) {
     const int copy = wave * S::kCopies + i;
@@ -304,23 +301,30 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN) product_tile_kernel(Pr
     const int place = (of_a ? copy : copy - S::kTileM / 8) * 64 + lane, line = place >> 4;
     const int source = (place & 15) ^ (of_a ? exchange_of<false>(line) : exchange_of<true>(line));
     const int32_t r = min(line * 2 + (source >> 3), (of_a ? a.M - m0 : a.N - n0) - 1);
-    from[i] = (uint32_t)(r * (int32_t)bytes + (source & 7) * 16);
+    from[i] = (uint32_t)r * (uint32_t)bytes + (source & 7) * 16;
   }
-  const int scale_row = wave * 64 + lane;  // of the tile's rows of A, then B: waves 0 .. copy 64 scales each
-  const bool has_scales = wave * 64 < S::kTileM + (kBlocks ? 0 : S::kTileN);
-  uint32_t scale_from = 0;
-  {
-    const bool of_a = scale_row < S::kTileM;
-    scale_from = 4u * (uint32_t)(of_a ? min(m0 + scale_row, a.M - 1) : min(n0 + scale_row - S::kTileM, a.N - 1));
+#pragma unroll
+  for (int i = 0; i < S::kScaleCopies; ++i) {
+    const int first = (wave * S::kScaleCopies + i) * 64;
+    // scales of blocks are no copies: those of A once more
+    scale_from[i] = 4u * (uint32_t)(first < S::kTileM || kBlocks ? min(m0 + first + lane, a.M - 1) : min(n0 + first - S::kTileM + lane, a.N - 1));
   }
-  auto copy_stage = [&](int32_t g, int i) __attribute__((always_inline)) {
+  // Stage j of the part is group j kSplit + part.
+  constexpr uint64_t kAll = ~0ull;
+  auto copy_codes = [&](int32_t j, uint32_t stage, int i, uint64_t lanes, bool all) __attribute__((always_inline)) {
     const int copy = wave * S::kCopies + i;
-    const uint8_t* base = (copy * 8 < S::kTileM ? a_base : b_base) + (int64_t)g * kGroup;
-    copy16_to_lds_sv(base, from[i], lds0 + (g & 1) * S::kStage + copy * 1024);
+    const uint8_t* base = (copy * 8 < S::kTileM ? a_base : b_base) + (int64_t)(j * kSplit + part) * kGroup;
+    if (all) copy16_to_lds_sv(base, from[i], lds0 + stage + copy * 1024);
+    else copy16_to_lds_sv_masked(base, from[i], lds0 + stage + copy * 1024, lanes);
   };
-  auto copy_scales = [&](int32_t g) __attribute__((always_inline)) {
-    const float* base = wave * 64 < S::kTileM ? a.sa + (int64_t)g * a.M : a.sb + (int64_t)g * a.N;
-    copy4_to_lds_sv_masked(base, scale_from, lds0 + (g & 1) * S::kStage + S::kCodes + wave * 256, has_scales ? ~0ull : 0ull);
+  auto copy_scales = [&](int32_t j, uint32_t stage, uint64_t lanes) __attribute__((always_inline)) {
+    const int64_t g = j * kSplit + part;
+#pragma unroll
+    for (int i = 0; i < S::kScaleCopies; ++i) {
+      const int first = (wave * S::kScaleCopies + i) * 64;
+      const float* base = first < S::kTileM || kBlocks ? a.sa + g * a.M : a.sb + g * a.N;
+      copy4_to_lds_sv_masked(base, scale_from[i], lds0 + stage + S::kCodes + first * 4, lanes);
+    }
   };
 
   const int wm = wave / kWavesN, wn = wave % kWavesN;
@@ -331,9 +335,12 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN) product_tile_kernel(Pr
 #pragma unroll
     for (int j = 0; j < 4; ++j) sum[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+  const int32_t mine = (a.groups - part + kSplit - 1) / kSplit;  // stages of this part
+  for (int32_t j = 0; j < S::kAhead && j < mine; ++j) {
+    copy_scales(j, j * S::kStage, kAll);
 #pragma unroll
-  for (int i = 0; i < S::kCopies; ++i) copy_stage(0, i);
-  copy_scales(0);
+    for (int i = 0; i < S::kCopies; ++i) copy_codes(j, j * S::kStage, i, kAll, true);
+  }
 
   // A lane's 32 bytes of a row are pieces q and q + 4, the same on both sides (which bytes make up a lane's part does not matter): a read is served 16
   // lanes at a time, lanes 0 .. 3, 12 .. 15, 20 .. 27 first, and neighbouring pieces of those rows lie in different banks.  With pieces 2 q and 2 q + 1
@@ -356,17 +363,16 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN) product_tile_kernel(Pr
   using Scalars = const float __attribute__((address_space(4)))*;
   const Scalars block_scales = (Scalars)(a.sb + min((n0 + wn * 64) / kGroup, a.b_blocks - 1));
   auto block_scale = [&](int32_t g) __attribute__((always_inline)) { return block_scales[(int64_t)g * a.b_blocks]; };
-  float next_block = kBlocks ? block_scale(0) : 0.f;
-  auto walk = [&](int32_t g, auto more_) __attribute__((always_inline)) {
-    constexpr bool more = decltype(more_)::value;
-    wait_all_copies();
-    __syncthreads();
-    const uint32_t stage = (g & 1) * S::kStage;
+  float next_block = kBlocks ? block_scale(min(part, a.groups - 1)) : 0.f;
+  uint32_t stage = 0, free = S::kAhead * S::kStage;  // where the stage's codes lie, and where those of the stage kAhead later go
+  // `copies`: there is a stage to copy (1), there is none (0), or `lanes` says so, all or none (2).
+  auto walk = [&](int32_t j, auto copies_, uint64_t lanes) __attribute__((always_inline)) {
+    constexpr int copies = decltype(copies_)::value;
     const Lds at_a[2] = {lds_pointer<const char>(a_at[0] + stage), lds_pointer<const char>(a_at[1] + stage)};
     const Lds at_b[2] = {lds_pointer<const char>(b_at[0] + stage), lds_pointer<const char>(b_at[1] + stage)};
     const auto* a_scales = lds_pointer<const float>(a_scale_at + stage);
     const auto* b_scales = lds_pointer<const f32x4>(b_scale_at + stage);
-    if (more) copy_scales(g + 1);
+    if (copies) copy_scales(j + S::kAhead, free, copies == 1 ? kAll : lanes);
     // Row 4 i + j of fragment t is column 16 i + 4 t + j of the wave's 64: a lane's sums of the four are 16 neighbouring columns.
     i32x8 columns[4];
     f32x4 sb[4];
@@ -376,7 +382,7 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN) product_tile_kernel(Pr
       if (!kBlocks) sb[t] = b_scales[t];
     }
     const float of_block = next_block;
-    if (kBlocks && more) next_block = block_scale(g + 1);
+    if (kBlocks) next_block = block_scale(min((j + 1) * kSplit + part, a.groups - 1));
     // The sums of one row fragment are added between the matrix instructions of the next: each has the time of three to come out of the pipe.
     i32x8 rows = fragment(at_a, 0);
     float factor = a_scales[0], before = 0.f;
@@ -389,9 +395,9 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN) product_tile_kernel(Pr
         next = fragment(at_a, (i + 1) * 16 * kGroup);
         next_factor = a_scales[(i + 1) * 16];
       }
-      if (more && i < kMTiles) {
+      if (copies && i < kMTiles) {
 #pragma unroll
-        for (int c = 2 * i * S::kCopies / kMTiles; c < 2 * (i + 1) * S::kCopies / kMTiles && c < S::kCopies; ++c) copy_stage(g + 1, c);
+        for (int c = 2 * i * S::kCopies / kMTiles; c < 2 * (i + 1) * S::kCopies / kMTiles && c < S::kCopies; ++c) copy_codes(j + S::kAhead, free, c, lanes, copies == 1);
       }
       if (kBlocks) factor *= of_block;
 #pragma unroll
@@ -407,67 +413,147 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN) product_tile_kernel(Pr
       rows = next;
       factor = next_factor;
     }
+    stage = stage + S::kStage == S::kRing ? 0 : stage + S::kStage;
+    free = free + S::kStage == S::kRing ? 0 : free + S::kStage;
   };
-  for (int32_t g = 0; g + 1 < a.groups; ++g) walk(g, std::true_type());
-  walk(a.groups - 1, std::false_type());
+  // Copies come in order: once only those of the kAhead - 1 stages behind are under way, this stage's are done.  The last stages, where
+  // some parts have one less, wait for all.
+  int32_t j = 0;
+  for (; (j + S::kAhead) * kSplit + kSplit - 1 < a.groups; ++j) {
+    wait_copies<S::kInFlight>();
+    __syncthreads();
+    walk(j, std::integral_constant<int, 1>(), kAll);
+  }
+  for (; j * kSplit < a.groups; ++j) {
+    wait_copies<0>();
+    __syncthreads();
+    if (kSplit == 1) walk(j, std::integral_constant<int, 0>(), 0ull);
+    else if (j < mine) walk(j, std::integral_constant<int, kSplit == 1 ? 0 : 2>(), j + S::kAhead < mine ? kAll : 0ull);
+  }
 
 #pragma unroll
   for (int i = 0; i < kMTiles; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(sum[i][j]));  // the last sums are added here, not where they are stored, which would hold both parts of each
+  if constexpr (kSplit > 1) {
+    // the other parts' sums, in order
+    __syncthreads();
+    auto place = [&](int of_part, int i, int t) { return lds_cast<f32x4>(lds + (((of_part - 1) * S::kWaves + wave) * kMTiles * 4 + i * 4 + t) * 1024 + lane * 16); };
+    if (part > 0) {
+#pragma unroll
+      for (int i = 0; i < kMTiles; ++i)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) *place(part, i, t) = sum[i][t];
+    }
+    __syncthreads();
+    if (part > 0) return;
+    for (int from_part = 1; from_part < kSplit; ++from_part)
+#pragma unroll
+      for (int i = 0; i < kMTiles; ++i)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sum[i][t] += *place(from_part, i, t);
+  }
+  // Rows that are not 16-byte aligned go through LDS, 16 at a time, to be stored a row of 64 columns at once (straight from the sums a store would
+  // touch 64 places: 1237 x 1961 x 1000 took 18.3 us instead of 13.6).
+  if (!a.vec) __syncthreads();  // everyone is done with the stages, and with the parts' sums
+  constexpr int kPitch = 144;
+  char* turn = lds + wave * 16 * kPitch;
 #pragma unroll
   for (int i = 0; i < kMTiles; ++i) {
-    const int32_t m = m0 + (wm * kMTiles + i) * 16 + l16;
-    if (m >= a.M) continue;
-    const int32_t n = n0 + wn * 64 + q * 16;
-    __bf16* out = a.out + m * a.out_stride + n;
     uint32_t pair[8];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       pair[2 * t] = pack_bf16(sum[i][t][0], sum[i][t][1]);
       pair[2 * t + 1] = pack_bf16(sum[i][t][2], sum[i][t][3]);
     }
-    if (a.vec && n + 16 <= a.N) {
+    const int32_t row0 = m0 + (wm * kMTiles + i) * 16, column0 = n0 + wn * 64;
+    if (!a.vec) {
+      *lds_cast<u32x4>(turn + l16 * kPitch + q * 32) = u32x4{pair[0], pair[1], pair[2], pair[3]};
+      *lds_cast<u32x4>(turn + l16 * kPitch + q * 32 + 16) = u32x4{pair[4], pair[5], pair[6], pair[7]};
+      asm volatile("" ::: "memory");  // one wave's accesses to LDS come in order
+      for (int r = 0; r < 16; ++r) {
+        const uint16_t v = *lds_cast<const uint16_t>(turn + r * kPitch + lane * 2);
+        if (row0 + r < a.M && column0 + lane < a.N) ((uint16_t*)a.out)[(row0 + r) * a.out_stride + column0 + lane] = v;
+      }
+      asm volatile("" ::: "memory");
+      continue;
+    }
+    const int32_t m = row0 + l16, n = column0 + q * 16;
+    if (m >= a.M) continue;
+    __bf16* out = a.out + m * a.out_stride + n;
+    if (n + 16 <= a.N) {
       *(u32x4*)out = u32x4{pair[0], pair[1], pair[2], pair[3]};
       *(u32x4*)(out + 8) = u32x4{pair[4], pair[5], pair[6], pair[7]};
     } else {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        if (n + e < a.N) out[e] = (__bf16)sum[i][e / 4][e % 4];
+        if (n + e < a.N) ((uint16_t*)out)[e] = (uint16_t)(pair[e / 2] >> (e % 2 * 16));
     }
   }
 }
 
-template <int kWavesM, int kWavesN, int kMTiles, bool kBlocks>
+template <int kWavesM, int kWavesN, int kMTiles, int kStages, int kSplit, bool kBlocks>
 int launch_tiles(const ProductArgs& a, hipStream_t stream) {
-  using S = TileShape<kWavesM, kWavesN, kMTiles>;
+  using S = TileShape<kWavesM, kWavesN, kMTiles, kStages, kSplit>;
   const int64_t tiles = ((int64_t)a.M + S::kTileM - 1) / S::kTileM * (((int64_t)a.N + S::kTileN - 1) / S::kTileN);
   if (tiles > 0x7fffffffLL) return fail(RADIAL_ESHAPE, "M*N is too large for one launch");
   if constexpr (S::kLds > 65536) {
     static DeviceOnce configured;
-    if (int rc = allow_dynamic_lds(configured, (const void*)product_tile_kernel<kWavesM, kWavesN, kMTiles, kBlocks>, S::kLds)) return rc;
+    if (int rc = allow_dynamic_lds(configured, (const void*)product_tile_kernel<kWavesM, kWavesN, kMTiles, kStages, kSplit, kBlocks>, S::kLds)) return rc;
   }
-  product_tile_kernel<kWavesM, kWavesN, kMTiles, kBlocks><<<dim3((unsigned)tiles), dim3(64 * S::kWaves), S::kLds, stream>>>(a);
+  product_tile_kernel<kWavesM, kWavesN, kMTiles, kStages, kSplit, kBlocks><<<dim3((unsigned)tiles), dim3(64 * S::kWaves * kSplit), S::kLds, stream>>>(a);
   RADIAL_HIP_TRY(hipGetLastError());
   return RADIAL_OK;
 }
 
+// Tiles of a product.  What a launch takes is put together from the time of a stage (of each part) and of what a tile does besides, in us, as measured
+// with the chip full of that tile, or with one on each compute unit where two fit (5120 x 5120, 100 to 14 040 rows, and others): large tiles move the
+// fewest codes per product, but a launch of a few of them leaves compute units idle, and a workgroup alone on its unit spends more than half of a small
+// tile's stage waiting, which parts of the groups at the same time make up for.
+struct TileForm {
+  int32_t rows, columns, at_once, split;
+  float stage_full, stage_one, besides;
+};
+constexpr TileForm kTileForms[] = {
+    {256, 256, 1, 1, 1.66f, 1.66f, 6.f}, {192, 256, 1, 1, 1.33f, 1.33f, 5.f}, {128, 128, 2, 1, 1.28f, 0.80f, 3.f}, {128, 128, 1, 2, 1.30f, 1.30f, 3.f},
+    {64, 128, 2, 1, 0.74f, 0.55f, 2.5f}, {64, 128, 1, 2, 0.90f, 0.90f, 2.5f}, {64, 64, 2, 2, 0.90f, 0.62f, 2.f},   {64, 64, 1, 4, 1.15f, 1.15f, 2.f},
+};
+inline int choose_tiles(int32_t M, int32_t N, int32_t groups) {
+  constexpr int64_t kUnits = 256;
+  int best = 0;
+  double least = 0;
+  for (int i = 0; i < (int)(sizeof(kTileForms) / sizeof(kTileForms[0])); ++i) {
+    const TileForm& f = kTileForms[i];
+    const int64_t tiles = (((int64_t)M + f.rows - 1) / f.rows) * (((int64_t)N + f.columns - 1) / f.columns);
+    const int64_t round = kUnits * f.at_once, full = tiles / round, rest = tiles % round;
+    const double stages = (groups + f.split - 1) / f.split;
+    const double last = rest == 0 ? 0.0 : rest <= kUnits ? stages * f.stage_one + f.besides : stages * f.stage_full + f.besides;
+    const double time = full * (stages * f.stage_full + f.besides) + last;
+    if (i == 0 || time < least) {
+      best = i;
+      least = time;
+    }
+  }
+  return best;
+}
+
 template <bool kBlocks>
 int launch_product(const ProductArgs& a, hipStream_t stream) {
-  if (a.M > 64) {
-    const int64_t large = (int64_t)((a.M + 255) / 256) * ((a.N + 255) / 256);
-    return large >= 256 ? launch_tiles<2, 4, 8, kBlocks>(a, stream) : launch_tiles<2, 2, 4, kBlocks>(a, stream);
+  if (a.M <= 16) {
+    product_rows_kernel<kBlocks><<<dim3((unsigned)((a.N + 15) / 16)), dim3(64 * kParts), 0, stream>>>(a);
+    RADIAL_HIP_TRY(hipGetLastError());
+    return RADIAL_OK;
   }
-  const int64_t columns = (a.N + 15) / 16;
-  const int32_t tiles = a.M <= 16 ? 1 : a.M <= 32 ? 2 : 4;
-  const int64_t rows = (a.M + 16 * tiles - 1) / (16 * tiles);
-  if (rows > 65535) return fail(RADIAL_ESHAPE, "M is too large for one launch");
-  const dim3 grid((unsigned)columns, (unsigned)rows), block(64 * kParts);
-  if (tiles == 1) product_rows_kernel<kBlocks, 1><<<grid, block, 0, stream>>>(a);
-  else if (tiles == 2) product_rows_kernel<kBlocks, 2><<<grid, block, 0, stream>>>(a);
-  else product_rows_kernel<kBlocks, 4><<<grid, block, 0, stream>>>(a);
-  RADIAL_HIP_TRY(hipGetLastError());
-  return RADIAL_OK;
+  switch (choose_tiles(a.M, a.N, a.groups)) {
+    case 0: return launch_tiles<2, 4, 8, 2, 1, kBlocks>(a, stream);
+    case 1: return launch_tiles<2, 4, 6, 2, 1, kBlocks>(a, stream);
+    case 2: return launch_tiles<2, 2, 4, 2, 1, kBlocks>(a, stream);
+    case 3: return launch_tiles<2, 2, 4, 2, 2, kBlocks>(a, stream);
+    case 4: return launch_tiles<2, 2, 2, 3, 1, kBlocks>(a, stream);
+    case 5: return launch_tiles<2, 2, 2, 3, 2, kBlocks>(a, stream);
+    case 6: return launch_tiles<2, 1, 2, 2, 2, kBlocks>(a, stream);
+    default: return launch_tiles<2, 1, 2, 2, 4, kBlocks>(a, stream);
+  }
 }
 
 }  // namespace
@@ -516,7 +602,7 @@ extern "C" int radial_product_fp8(int32_t M, int32_t N, int32_t K, const uint8_t
   if (((uintptr_t)a_scales | (uintptr_t)b_scales) & 3u) return fail(RADIAL_ESHAPE, "scales are not aligned to their elements");
   if ((uintptr_t)out & 1u) return fail(RADIAL_ESHAPE, "out is not aligned to its elements");
   if (out_stride < N) return fail(RADIAL_ESHAPE, "out_stride must not be below N");
-  if (M > 0x7fffffff - 512 || N > 0x7fffffff - 512 || K > 0x7fffffff - 512) return fail(RADIAL_ESHAPE, "M, N, K are too large for one launch");
+  if (M > 1 << 29 || N > 1 << 29 || K > 1 << 23) return fail(RADIAL_ESHAPE, "M and N must be at most 2^29 and K 2^23: larger ones are too large for one launch");
   ProductArgs a = {};
   a.a = a_codes; a.b = b_codes; a.sa = a_scales; a.sb = b_scales;
   a.out = (__bf16*)out; a.out_stride = out_stride;
