@@ -39,11 +39,12 @@ struct NormArgs {
   int32_t wants;             // backward: bits of the sums that are wanted: 1 P, 2 T, 4 Q
 };
 
-// Sum over a team that is the whole workgroup: each wave's sum through LDS.  kCount sums at once; `turn` alternates between two places, so
-// that one barrier does for each call (who writes a place again has passed the barrier of the call between, behind all reads of it).
-constexpr int kMaxWaves = 16;
+// Where the waves of a team that is the whole workgroup meet: up to four values of each, zero where there is no wave.  `turn` alternates between two
+// places, so that one barrier does for each meeting (who writes a place again has passed the barrier of the meeting between, behind all
+// reads of it).
+constexpr int kMaxWaves = 8;
 struct Meeting {
-  float place[2][kMaxWaves][4];
+  f32x4 place[2][kMaxWaves];
 };
 
 // The channels of a thread: 8 V of them.  Vectors: eight in a row, V times, a workgroup's width apart; single elements: each a
@@ -135,96 +136,122 @@ __device__ __forceinline__ void load_mod(float (&out)[8 * V], const float* row, 
   }
 }
 
-// Rows of a team and its sums.  kWide: the team is the workgroup; otherwise L lanes.
-template <bool kWide, int L>
+// Rows of a team and its sums.  kWide: the team is the workgroup; otherwise L lanes.  kFast: fewer instructions and waits for more registers (what the
+// waves left is read at once, channels are masked an eight at a time): the gradients at 5120 channels, where only eight waves fit a compute unit
+// anyway, take 443 us instead of 482; the forward, which loses a wave of four by it, 276 instead of 256, the gradients at 1536 channels 175 instead of 154.
+template <bool kWide, int L, bool kFast>
 struct Team {
+  static constexpr bool kExchanges = kWide, kEights = kFast;
   Meeting* meet;
   int32_t turn, wave, waves;
   float C;
   float own;       // channels of this wave (wide) or of the row
   __device__ __forceinline__ float lanes(float x) const { return lane_sum<kWide ? 64 : L>(x); }
-  // Every wave's `k` values to every wave.
-  template <int kCount>
-  __device__ __forceinline__ void exchange(const float (&mine)[kCount]) {
-    turn ^= 1;
-    if ((threadIdx.x & 63) == 0) {
+  // Every wave's values to every wave: add(values) for one after the other.
+  template <class Add>
+  __device__ __forceinline__ void each(Add&& add) const {
+    if constexpr (kFast) {
+      f32x4 all[kMaxWaves];
 #pragma unroll
-      for (int i = 0; i < kCount; ++i) meet->place[turn][wave][i] = mine[i];
+      for (int w = 0; w < kMaxWaves; ++w) all[w] = meet->place[turn][w];
+#pragma unroll
+      for (int w = 0; w < kMaxWaves; ++w) add(all[w]);
+    } else {
+#pragma unroll 1
+      for (int w = 0; w < waves; ++w) add(meet->place[turn][w]);
     }
+  }
+  __device__ __forceinline__ void exchange(f32x4 mine) {
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) meet->place[turn][wave] = mine;
     __syncthreads();
   }
-  __device__ __forceinline__ float theirs(int w, int i) const { return meet->place[turn][w][i]; }
 };
 
 // Mean and 1/size of the row, from `val` (zero beyond the channels).  A layer norm's variance is taken about the mean of the wave's own channels and then
 // moved to the row's (sum (v - m)^2 = sum (v - m_w)^2 + n_w (m_w - m)^2 per wave): no cancellation where the mean is large, and one exchange instead of two.
-template <bool kVec, int V>
-__device__ __forceinline__ float sum_of(const float (&val)[8 * V]) {
+template <int E>
+__device__ __forceinline__ float sum_of(const float (&val)[E]) {
   float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8 * V; ++i) s += val[i];
+  for (int i = 0; i < E; ++i) s += val[i];
   return s;
 }
-template <bool kVec, int V>
+// Masked one by one, or (kEights: vectors) an eight at a time.
+template <bool kVec, int V, bool kEights>
 __device__ __forceinline__ float squares_about(const float (&val)[8 * V], float mean, const Channels<kVec, V>& ch) {
   float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8 * V; ++i) {
-    const float d = ch.has(i / 8, i % 8) ? val[i] - mean : 0.f;
-    s += d * d;
+  for (int v = 0; v < V; ++v) {
+    float of_eight = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float d = kEights || ch.has(v, e) ? val[8 * v + e] - mean : 0.f;
+      if (kEights) of_eight = __builtin_fmaf(d, d, of_eight);
+      else s = __builtin_fmaf(d, d, s);
+    }
+    if (kEights) s += ch.has(v, 0) ? of_eight : 0.f;
   }
   return s;
 }
 
-template <bool kVec, int V, bool kWide, int L>
-__device__ __forceinline__ void statistics(const float (&val)[8 * V], int32_t kind, float eps, Team<kWide, L>& team, const Channels<kVec, V>& ch, float own_count,
+template <bool kVec, int V, class T>
+__device__ __forceinline__ void statistics(const float (&val)[8 * V], int32_t kind, float eps, T& team, const Channels<kVec, V>& ch, float own_count,
                                            float& mean, float& inverse) {
   mean = 0.f;
   float about = 0.f;
-  if (kind == RADIAL_NORM_LAYER) about = team.lanes(sum_of<kVec, V>(val)) / fmaxf(own_count, 1.f);
-  float squares = team.lanes(squares_about<kVec, V>(val, about, ch));
-  if constexpr (kWide) {
-    const float mine[3] = {about, squares, own_count};
-    team.exchange(mine);
+  if (kind == RADIAL_NORM_LAYER) about = team.lanes(sum_of(val)) / fmaxf(own_count, 1.f);
+  float squares = team.lanes(squares_about<kVec, V, T::kEights>(val, about, ch));
+  if constexpr (T::kExchanges) {
+    team.exchange(f32x4{about * own_count, squares, own_count, about});
     squares = 0.f;
-    if (kind == RADIAL_NORM_LAYER) {
-      float total = 0.f;
-      for (int w = 0; w < team.waves; ++w) total += team.theirs(w, 0) * team.theirs(w, 2);
-      mean = total / team.C;
-      for (int w = 0; w < team.waves; ++w) {
-        const float d = team.theirs(w, 0) - mean;
-        squares += team.theirs(w, 1) + team.theirs(w, 2) * d * d;
-      }
-    } else {
-      for (int w = 0; w < team.waves; ++w) squares += team.theirs(w, 1);
-    }
+    team.each([&](f32x4 theirs) {
+      mean += theirs[0];
+      squares += theirs[1];
+    });
+    mean /= team.C;
+    if (kind == RADIAL_NORM_LAYER)
+      team.each([&](f32x4 theirs) {
+        const float d = theirs[3] - mean;
+        squares = __builtin_fmaf(theirs[2] * d, d, squares);
+      });
   } else {
     mean = about;
   }
   inverse = 1.f / sqrtf(squares / team.C + eps);
 }
 
+// v <- (v - mean) inverse, zero where there is no channel.
+template <bool kVec, int V, bool kEights>
+__device__ __forceinline__ void normalise(float (&val)[8 * V], float mean, float inverse, const Channels<kVec, V>& ch) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const float factor = !kEights || ch.has(v, 0) ? inverse : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) val[8 * v + e] = kEights || ch.has(v, e) ? (val[8 * v + e] - mean) * factor : 0.f;
+  }
+}
+
 // Two sums over the row at once.
-template <bool kWide, int L>
-__device__ __forceinline__ void two_sums(float& a, float& b, Team<kWide, L>& team) {
+template <class T>
+__device__ __forceinline__ void two_sums(float& a, float& b, T& team) {
   a = team.lanes(a);
   b = team.lanes(b);
-  if constexpr (kWide) {
-    const float mine[2] = {a, b};
-    team.exchange(mine);
+  if constexpr (T::kExchanges) {
+    team.exchange(f32x4{a, b, 0.f, 0.f});
     a = b = 0.f;
-    for (int w = 0; w < team.waves; ++w) {
-      a += team.theirs(w, 0);
-      b += team.theirs(w, 1);
-    }
+    team.each([&](f32x4 theirs) {
+      a += theirs[0];
+      b += theirs[1];
+    });
   }
 }
 
 // What a workgroup works on.
-template <bool kVec, int V, bool kWide, int L>
+template <bool kVec, int V, bool kWide, int L, bool kFast>
 struct Share {
   Channels<kVec, V> ch;
-  Team<kWide, L> team;
+  Team<kWide, L, kFast> team;
   int32_t teams, first, last;  // rows first, first + teams, ... below last, of batch b
   int32_t b, group;            // group: b * groups_of_batch + g
   float own_count;
@@ -242,6 +269,10 @@ struct Share {
     ch.width = kWide ? blockDim.x : L;
     ch.C = a.C;
     team.meet = meet;
+    if (kWide) {
+      if (threadIdx.x < 2 * kMaxWaves) meet->place[threadIdx.x / kMaxWaves][threadIdx.x % kMaxWaves] = f32x4{0.f, 0.f, 0.f, 0.f};
+      __syncthreads();
+    }
     team.turn = 0;
     team.wave = threadIdx.x >> 6;
     team.waves = (blockDim.x + 63) >> 6;
@@ -256,9 +287,9 @@ __device__ __forceinline__ T* row_of(const RowsArg& t, int32_t b, int32_t n) {
 }
 
 template <class XT, class YT, bool kVec, int V, bool kWide, int L>
-__global__ void __launch_bounds__(kWide ? 1024 : 256) norm_fwd_kernel(NormArgs a) {
+__global__ void __launch_bounds__(kWide ? 512 : 256) norm_fwd_kernel(NormArgs a) {
   __shared__ Meeting meet;
-  Share<kVec, V, kWide, L> s(a, &meet);
+  Share<kVec, V, kWide, L, false> s(a, &meet);
   constexpr int E = 8 * V;
   const int64_t mod = (int64_t)s.group * a.mod_stride;
   float gate[E], factor[E], shift[E];
@@ -317,10 +348,11 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) norm_fwd_kernel(NormArgs a
 }
 
 template <class XT, class YT, bool kVec, int V, bool kWide, int L>
-__global__ void __launch_bounds__(kWide ? 1024 : 256) norm_bwd_kernel(NormArgs a) {
+__global__ void __launch_bounds__(kWide ? 512 : 256) norm_bwd_kernel(NormArgs a) {
   __shared__ Meeting meet;
   __shared__ float merged[kWide ? 1 : 3][kWide ? 1 : 256 * 8];
-  Share<kVec, V, kWide, L> s(a, &meet);
+  constexpr bool kFast = kVec && kWide && V == 2;
+  Share<kVec, V, kWide, L, kFast> s(a, &meet);
   constexpr int E = 8 * V;
   const int64_t mod = (int64_t)s.group * a.mod_stride;
   const bool has_y = a.y.ptr != nullptr, has_z = a.z.ptr != nullptr;
@@ -330,7 +362,7 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) norm_bwd_kernel(NormArgs a
     load_mod<kVec, V>(gate, a.gate ? a.gate + mod : nullptr, 1.f, s.ch);
     load_mod<kVec, V>(w, a.post_weight, 1.f, s.ch);
 #pragma unroll
-    for (int i = 0; i < E; ++i) gate[i] *= w[i];
+    for (int i = 0; i < E; ++i) gate[i] = s.ch.has(i / 8, i % 8) ? gate[i] * w[i] : 0.f;
     load_mod<kVec, V>(factor, a.scale ? a.scale + mod : nullptr, 0.f, s.ch);
     load_mod<kVec, V>(w, a.weight, 1.f, s.ch);
 #pragma unroll
@@ -339,46 +371,52 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) norm_bwd_kernel(NormArgs a
   float P[E], T[E], Q[E];
 #pragma unroll
   for (int i = 0; i < E; ++i) P[i] = T[i] = Q[i] = 0.f;
-  Held<XT, kVec, V> r_held, dr_held, next_r, next_dr;
-  Held<YT, kVec, V> y_held, dz_held, next_y, next_dz;
-  auto fetch = [&](int32_t n) __attribute__((always_inline)) {
+  // The next row is fetched while one is worked on, where registers allow it.
+  constexpr int kAhead = V < 4 ? 1 : 0;
+  struct Row {
+    Held<XT, kVec, V> r, dr;
+    Held<YT, kVec, V> y, dz;
+  } held[kAhead + 1];
+  auto fetch = [&](int32_t n, Row& to) __attribute__((always_inline)) {
     if (n >= s.last) return;
     if (has_z) {
-      next_r.load(row_of<XT>(a.r, s.b, n), s.ch);
-      next_dz.load(row_of<YT>(a.z, s.b, n), s.ch);
+      to.r.load(row_of<XT>(a.r, s.b, n), s.ch);
+      to.dz.load(row_of<YT>(a.z, s.b, n), s.ch);
     }
-    if (a.dr.ptr) next_dr.load(row_of<XT>(a.dr, s.b, n), s.ch);
-    if (has_y) next_y.load(row_of<YT>(a.y, s.b, n), s.ch);
+    if (a.dr.ptr) to.dr.load(row_of<XT>(a.dr, s.b, n), s.ch);
+    if (has_y) to.y.load(row_of<YT>(a.y, s.b, n), s.ch);
   };
-  next_r.clear();
-  next_dr.clear();
-  next_y.clear();
-  next_dz.clear();
-  fetch(s.first);
+#pragma unroll
+  for (int i = 0; i <= kAhead; ++i) {
+    held[i].r.clear();
+    held[i].dr.clear();
+    held[i].y.clear();
+    held[i].dz.clear();
+    if (i > 0) fetch(s.first + (i - 1) * s.teams, held[i]);
+  }
   for (int32_t row = s.first; kWide ? row < s.last : __any(row < s.last); row += s.teams) {
     const bool live = kWide || row < s.last;
-    r_held = next_r;
-    dr_held = next_dr;
-    y_held = next_y;
-    dz_held = next_dz;
-    fetch(row + s.teams);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) held[i] = held[i + 1];
+    fetch(row + kAhead * s.teams, held[kAhead]);
+    const Row& now = held[0];
     float D[E];
     if (a.dr.ptr) {
-      dr_held.get(D);
+      now.dr.get(D);
     } else {
 #pragma unroll
       for (int i = 0; i < E; ++i) D[i] = 0.f;
     }
     if (has_z) {
       float n[E], d[E];
-      r_held.get(n);
-      dz_held.get(d);
+      now.r.get(n);
+      now.dz.get(d);
       float mean, inverse;
       statistics<kVec, V>(n, a.pre, a.eps, s.team, s.ch, s.own_count, mean, inverse);
       float along = 0.f, flat = 0.f;
+      normalise<kVec, V, kFast>(n, mean, inverse, s.ch);
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        n[i] = s.ch.has(i / 8, i % 8) ? (n[i] - mean) * inverse : 0.f;
         if (live) {
           P[i] += d[i] * n[i];
           T[i] += d[i];
@@ -401,24 +439,26 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) norm_bwd_kernel(NormArgs a
     }
     if (has_y) {
       float m[E];
-      y_held.get(m);
+      now.y.get(m);
       float inverse = 1.f;
       if (a.post != RADIAL_NORM_NONE) {
         float mean;
         statistics<kVec, V>(m, a.post, a.eps, s.team, s.ch, s.own_count, mean, inverse);
-#pragma unroll
-        for (int i = 0; i < E; ++i) m[i] = s.ch.has(i / 8, i % 8) ? (m[i] - mean) * inverse : 0.f;
+        normalise<kVec, V, kFast>(m, mean, inverse, s.ch);
       }
-      float along = 0.f, flat = 0.f;
+      // where there is no channel m is 0, and so is gate
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        D[i] = s.ch.has(i / 8, i % 8) ? D[i] : 0.f;
         if (live) Q[i] += D[i] * m[i];
         D[i] *= gate[i];
-        flat += D[i];
-        along += D[i] * m[i];
       }
       if (a.post != RADIAL_NORM_NONE) {
+        float along = 0.f, flat = 0.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          flat += D[i];
+          along += D[i] * m[i];
+        }
         two_sums(flat, along, s.team);
         flat = a.post == RADIAL_NORM_LAYER ? flat / s.team.C : 0.f;
         along /= s.team.C;
@@ -465,17 +505,26 @@ struct GradArgs {
   int64_t mod_stride, dmod_stride;
 };
 
-constexpr int kGradSlices = 16;
+constexpr int kGradColumns = 16, kGradSlices = 64;
 
-// 64 channels of a group: 16 slices of its workgroups' sums each, then the slices' sums.
-__global__ void __launch_bounds__(64 * kGradSlices) norm_grad_kernel(GradArgs a) {
-  __shared__ float sums[kGradSlices][3][64];
+// The slices' sums of a column, in order.
+__device__ __forceinline__ float over_slices(const float (&sums)[kGradSlices][kGradColumns + 1], int column) {
+  float s = 0.f;
+#pragma unroll 16
+  for (int i = 0; i < kGradSlices; ++i) s += sums[i][column];
+  return s;
+}
+
+// 16 channels of a group: 64 slices of its workgroups' sums each, then the slices' sums.  (64 channels and 16 slices: 30 us of a small call.)
+__global__ void __launch_bounds__(kGradColumns * kGradSlices) norm_grad_kernel(GradArgs a) {
+  __shared__ float sums[3][kGradSlices][kGradColumns + 1];
   const int32_t lane = threadIdx.x, slice = threadIdx.y;
-  const int32_t c = blockIdx.x * 64 + lane;
+  const int32_t c = blockIdx.x * kGradColumns + lane;
   const int64_t group = blockIdx.y + (int64_t)blockIdx.z * 32768;
   if (group >= a.groups) return;
   float sum[3] = {0.f, 0.f, 0.f};
   if (c < a.C) {
+#pragma unroll 4
     for (int32_t i = slice; i < a.chunks; i += kGradSlices) {
       const float* p = a.partial + (group * a.chunks + i) * 3 * a.C + c;
 #pragma unroll
@@ -484,29 +533,22 @@ __global__ void __launch_bounds__(64 * kGradSlices) norm_grad_kernel(GradArgs a)
     }
   }
 #pragma unroll
-  for (int k = 0; k < 3; ++k) sums[slice][k][lane] = sum[k];
+  for (int k = 0; k < 3; ++k) sums[k][slice][lane] = sum[k];
   __syncthreads();
-  if (slice != 0 || c >= a.C) return;
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    sum[k] = 0.f;
-    for (int i = 0; i < kGradSlices; ++i) sum[k] += sums[i][k][lane];
-  }
+  if (slice >= 3 || c >= a.C || !(a.wants >> slice & 1)) return;
+  const float total = over_slices(sums[slice], lane);  // of P, T or Q
   const int64_t mod = group * a.dmod_stride + c;
-  if (a.dscale) a.dscale[mod] = a.weight ? sum[0] * a.weight[c] : sum[0];
-  if (a.dshift) a.dshift[mod] = sum[1];
-  if (a.dgate) a.dgate[mod] = a.post_weight ? sum[2] * a.post_weight[c] : sum[2];
-  if (a.of_group) {
-    a.of_group[(group * 2) * a.C + c] = sum[0];
-    a.of_group[(group * 2 + 1) * a.C + c] = sum[2];
-  }
+  if (slice == 0 && a.dscale) a.dscale[mod] = a.weight ? total * a.weight[c] : total;
+  if (slice == 1) a.dshift[mod] = total;
+  if (slice == 2 && a.dgate) a.dgate[mod] = a.post_weight ? total * a.post_weight[c] : total;
+  if (a.of_group && slice != 1) a.of_group[(group * 2 + (slice == 2)) * a.C + c] = total;
 }
 
 // dw and dw_post: sums over the groups, each times its conditioning.
-__global__ void __launch_bounds__(64 * kGradSlices) norm_weight_grad_kernel(GradArgs a) {
-  __shared__ float sums[kGradSlices][2][64];
+__global__ void __launch_bounds__(kGradColumns * kGradSlices) norm_weight_grad_kernel(GradArgs a) {
+  __shared__ float sums[2][kGradSlices][kGradColumns + 1];
   const int32_t lane = threadIdx.x, slice = threadIdx.y;
-  const int32_t c = blockIdx.x * 64 + lane;
+  const int32_t c = blockIdx.x * kGradColumns + lane;
   float dw = 0.f, dw_post = 0.f;
   if (c < a.C) {
     for (int64_t g = slice; g < a.groups; g += kGradSlices) {
@@ -514,17 +556,12 @@ __global__ void __launch_bounds__(64 * kGradSlices) norm_weight_grad_kernel(Grad
       if (a.dpost_weight) dw_post += a.of_group[(g * 2 + 1) * a.C + c] * (a.gate ? a.gate[g * a.mod_stride + c] : 1.f);
     }
   }
-  sums[slice][0][lane] = dw;
-  sums[slice][1][lane] = dw_post;
+  sums[0][slice][lane] = dw;
+  sums[1][slice][lane] = dw_post;
   __syncthreads();
-  if (slice != 0 || c >= a.C) return;
-  dw = dw_post = 0.f;
-  for (int i = 0; i < kGradSlices; ++i) {
-    dw += sums[i][0][lane];
-    dw_post += sums[i][1][lane];
-  }
-  if (a.dweight) a.dweight[c] = dw;
-  if (a.dpost_weight) a.dpost_weight[c] = dw_post;
+  if (c >= a.C) return;
+  if (slice == 0 && a.dweight) a.dweight[c] = over_slices(sums[0], lane);
+  if (slice == 1 && a.dpost_weight) a.dpost_weight[c] = over_slices(sums[1], lane);
 }
 
 // ---- launches -----------------------------------------------------------------------------------
@@ -536,13 +573,24 @@ struct Layout {
   int32_t chunks, rows;
 };
 
-Layout make_layout(const radial_norm_params& p, int64_t workgroups, int32_t least_rows) {
+constexpr int32_t kNarrow = 512;  // channels up to which a row is a wave's or less
+
+// Channels of a thread of a wide team, in eights.
+int eights_of(int32_t C) { return C <= 4096 ? 1 : C <= 8192 ? 2 : 4; }
+
+// `rounds` times the workgroups that run at a time, by the waves that fit a compute unit, shared out over the groups; a workgroup has at least
+// `least` rows for each of its teams, since each loads the conditioning and, backward, writes its sums.
+Layout make_layout(const radial_norm_params& p, int32_t waves_of_unit, int32_t rounds, int32_t least) {
   Layout l;
   l.groups_of_batch = (int32_t)(((int64_t)p.N + p.group - 1) / p.group);
   l.groups = (int64_t)p.B * l.groups_of_batch;
   const int32_t of_group = p.group < p.N ? p.group : p.N;
-  int64_t chunks = (workgroups + l.groups - 1) / l.groups;
-  const int64_t most = ((int64_t)of_group + least_rows - 1) / least_rows;
+  const int32_t V = eights_of(p.C);
+  const int32_t waves = p.C <= kNarrow ? 4 : (p.C + 512 * V - 1) / (512 * V);
+  const int32_t teams = p.C <= 128 ? 16 : p.C <= 256 ? 8 : p.C <= kNarrow ? 4 : 1;
+  const int64_t workgroups = (int64_t)256 * rounds * (waves_of_unit > waves ? waves_of_unit / waves : 1);
+  int64_t chunks = workgroups / l.groups;
+  const int64_t most = ((int64_t)of_group + least * teams - 1) / (least * teams);
   if (chunks > most) chunks = most;
   if (chunks < 1) chunks = 1;
   l.rows = (int32_t)((of_group + chunks - 1) / chunks);
@@ -550,10 +598,8 @@ Layout make_layout(const radial_norm_params& p, int64_t workgroups, int32_t leas
   return l;
 }
 
-constexpr int32_t kNarrow = 512;  // channels up to which a row is a wave's or less
-
-Layout fwd_layout(const radial_norm_params& p) { return make_layout(p, 4096, p.C <= kNarrow ? 16 : 1); }
-Layout bwd_layout(const radial_norm_params& p) { return make_layout(p, 1024, p.C <= kNarrow ? 16 : 1); }
+Layout fwd_layout(const radial_norm_params& p) { return make_layout(p, 16, 8, 1); }
+Layout bwd_layout(const radial_norm_params& p) { return make_layout(p, p.C <= 4096 ? 16 : 8, 1, 4); }
 
 bool aligned(const void* ptr, int64_t sb, int64_t sn, int size) {
   return ((uintptr_t)ptr & 15u) == 0 && sb * size % 16 == 0 && sn * size % 16 == 0;
@@ -563,20 +609,29 @@ template <class XT, class YT, bool kVec, int V, bool kWide, int L>
 int launch_one(const NormArgs& a, bool backward, int64_t grid, hipStream_t stream) {
   int threads = 256;
   if (kWide) threads = ((a.C + 8 * V - 1) / (8 * V) + 63) / 64 * 64;
-  if (backward) norm_bwd_kernel<XT, YT, kVec, V, kWide, L><<<dim3((unsigned)grid), dim3(threads), 0, stream>>>(a);
-  else norm_fwd_kernel<XT, YT, kVec, V, kWide, L><<<dim3((unsigned)grid), dim3(threads), 0, stream>>>(a);
+  if (backward) {
+    norm_bwd_kernel<XT, YT, kVec, V, kWide, L><<<dim3((unsigned)grid), dim3(threads), 0, stream>>>(a);
+  } else {
+    norm_fwd_kernel<XT, YT, kVec, V, kWide, L><<<dim3((unsigned)grid), dim3(threads), 0, stream>>>(a);
+  }
   RADIAL_HIP_TRY(hipGetLastError());
   return RADIAL_OK;
 }
 
 template <class XT, class YT>
 int launch_types(const NormArgs& a, bool vec, bool backward, int64_t grid, hipStream_t stream) {
-  if (!vec) return a.C <= 8192 ? launch_one<XT, YT, false, 1, true, 64>(a, backward, grid, stream) : launch_one<XT, YT, false, 2, true, 64>(a, backward, grid, stream);
+  const int eights = eights_of(a.C);
+  if (!vec) {
+    if (eights == 1) return launch_one<XT, YT, false, 1, true, 64>(a, backward, grid, stream);
+    if (eights == 2) return launch_one<XT, YT, false, 2, true, 64>(a, backward, grid, stream);
+    return launch_one<XT, YT, false, 4, true, 64>(a, backward, grid, stream);
+  }
   if (a.C <= 128) return launch_one<XT, YT, true, 1, false, 16>(a, backward, grid, stream);
   if (a.C <= 256) return launch_one<XT, YT, true, 1, false, 32>(a, backward, grid, stream);
   if (a.C <= kNarrow) return launch_one<XT, YT, true, 1, false, 64>(a, backward, grid, stream);
-  if (a.C <= 8192) return launch_one<XT, YT, true, 1, true, 64>(a, backward, grid, stream);
-  return launch_one<XT, YT, true, 2, true, 64>(a, backward, grid, stream);
+  if (eights == 1) return launch_one<XT, YT, true, 1, true, 64>(a, backward, grid, stream);
+  if (eights == 2) return launch_one<XT, YT, true, 2, true, 64>(a, backward, grid, stream);
+  return launch_one<XT, YT, true, 4, true, 64>(a, backward, grid, stream);
 }
 
 int launch(const NormArgs& a, int32_t x_type, int32_t y_type, bool vec, bool backward, int64_t grid, hipStream_t stream) {
@@ -755,8 +810,8 @@ extern "C" int radial_norm_bwd(const radial_norm_params* params, radial_rows r, 
   g.dgate = dgate; g.dscale = dscale; g.dshift = dshift; g.dpost_weight = dpost_weight; g.dweight = dweight;
   g.C = p.C; g.chunks = l.chunks; g.groups = (int32_t)l.groups; g.wants = a.wants;
   g.mod_stride = p.mod_stride; g.dmod_stride = p.dmod_stride;
-  const unsigned columns = (unsigned)((p.C + 63) / 64);
-  const dim3 block(64, kGradSlices);
+  const unsigned columns = (unsigned)((p.C + kGradColumns - 1) / kGradColumns);
+  const dim3 block(kGradColumns, kGradSlices);
   const unsigned in_y = l.groups < 32768 ? (unsigned)l.groups : 32768u, in_z = (unsigned)((l.groups + 32767) / 32768);
   norm_grad_kernel<<<dim3(columns, in_y, in_z), block, 0, (hipStream_t)hip_stream>>>(g);
   RADIAL_HIP_TRY(hipGetLastError());
