@@ -119,9 +119,9 @@ typedef struct {
  * magnitude * cos and magnitude * sin. */
 RADIAL_API size_t radial_rope_table_bytes(const radial_rope_params* params);
 
-/* Fills the table (device, 16-byte aligned) for the calls below, which only read it.  Angles are computed in 64 bits and reduced before
+/* Fills the table (device, 16-byte aligned, table_bytes of at least radial_rope_table_bytes) for the calls below, which only read it.  Angles are computed in 64 bits and reduced before
  * they are rounded, so that far positions are as exact as near ones. */
-RADIAL_API int radial_rope_table(const radial_rope_params* params, float* table, void* hip_stream);
+RADIAL_API int radial_rope_table(const radial_rope_params* params, float* table, size_t table_bytes, void* hip_stream);
 
 /* q_out, k_out <- q, k turned to their positions; both in one launch.
  *   q, q_out : [B, q_heads, N, D] with strides as in radial.h; D a multiple of 8, up to 1024, R <= D;
@@ -132,13 +132,13 @@ RADIAL_API int radial_rope_table(const radial_rope_params* params, float* table,
  *   first    : index of token 0 without positions (a shard's, or a single new token's); >= 0, ignored with positions.
  * Outputs may be their input's memory with the same strides, and otherwise share no elements with an input.
  * Errors: EINVAL, EUNSUPPORTED (D), ESHAPE, EHIP. */
-RADIAL_API int radial_rope_fwd(const radial_rope_params* params, const float* table, int32_t B, int32_t N, int32_t D, int32_t q_heads,
-                               radial_tensor q, radial_tensor q_out, int32_t k_heads, radial_tensor k, radial_tensor k_out, int32_t type,
+RADIAL_API int radial_rope_fwd(const radial_rope_params* params, const float* table, size_t table_bytes, int32_t B, int32_t N, int32_t D,
+                               int32_t q_heads, radial_tensor q, radial_tensor q_out, int32_t k_heads, radial_tensor k, radial_tensor k_out, int32_t type,
                                const int32_t* positions, int32_t first, void* hip_stream);
 
 /* The gradient: dq, dk <- gradients of radial_rope_fwd's inputs from those of its outputs (the turn's transpose).  Arguments as there. */
-RADIAL_API int radial_rope_bwd(const radial_rope_params* params, const float* table, int32_t B, int32_t N, int32_t D, int32_t q_heads,
-                               radial_tensor dq_out, radial_tensor dq, int32_t k_heads, radial_tensor dk_out, radial_tensor dk, int32_t type,
+RADIAL_API int radial_rope_bwd(const radial_rope_params* params, const float* table, size_t table_bytes, int32_t B, int32_t N, int32_t D,
+                               int32_t q_heads, radial_tensor dq_out, radial_tensor dq, int32_t k_heads, radial_tensor dk_out, radial_tensor dk, int32_t type,
                                const int32_t* positions, int32_t first, void* hip_stream);
 
 /* ---- products in 8-bit floating point ----------------------------------------------------------

@@ -252,13 +252,19 @@ void launch(const RopeArgs& a, Pieces pieces, bool interleaved, dim3 grid, hipSt
   else rope_kernel<T, Pieces::kSingles><<<grid, dim3(256), 0, stream>>>(a, interleaved);
 }
 
-int turn(const radial_rope_params* params, const float* table, int32_t B, int32_t N, int32_t D, int32_t q_heads, radial_tensor q,
+int check_table(const radial_rope_params& p, const float* table, size_t bytes) {
+  if (!table) return fail(RADIAL_EINVAL, "table is NULL");
+  if ((uintptr_t)table & 15u) return fail(RADIAL_ESHAPE, "table is not 16-byte aligned");
+  const size_t need = (size_t)turns_of(p) * 2 * sizeof(float);
+  return bytes >= need ? RADIAL_OK : fail(RADIAL_ESHAPE, "table holds %zu bytes, %zu needed", bytes, need);
+}
+
+int turn(const radial_rope_params* params, const float* table, size_t table_bytes, int32_t B, int32_t N, int32_t D, int32_t q_heads, radial_tensor q,
          radial_tensor q_out, int32_t k_heads, radial_tensor k, radial_tensor k_out, int32_t type, const int32_t* positions, int32_t first,
          bool gradient, void* hip_stream) {
   if (int rc = check_params(params)) return rc;
   const radial_rope_params& p = *params;
-  if (!table) return fail(RADIAL_EINVAL, "table is NULL");
-  if ((uintptr_t)table & 15u) return fail(RADIAL_ESHAPE, "table is not 16-byte aligned");
+  if (int rc = check_table(p, table, table_bytes)) return rc;
   if (B < 1 || N < 1 || q_heads < 1) return fail(RADIAL_EINVAL, "B, N, q_heads must be >= 1");
   if (D < 8 || D % 8 || D > kMaxHeadDim) return fail(RADIAL_EUNSUPPORTED, "head dimension must be a multiple of 8 up to %d (got %d)", kMaxHeadDim, D);
   if (!is_type(type)) return fail(RADIAL_EINVAL, "type must be RADIAL_BF16 or RADIAL_F32 (got %d)", type);
@@ -319,11 +325,10 @@ extern "C" size_t radial_rope_table_bytes(const radial_rope_params* params) {
   return check_params(params) == RADIAL_OK ? (size_t)turns_of(*params) * 2 * sizeof(float) : 0;
 }
 
-extern "C" int radial_rope_table(const radial_rope_params* params, float* table, void* hip_stream) {
+extern "C" int radial_rope_table(const radial_rope_params* params, float* table, size_t table_bytes, void* hip_stream) {
   if (int rc = check_params(params)) return rc;
-  if (!table) return fail(RADIAL_EINVAL, "table is NULL");
-  if ((uintptr_t)table & 15u) return fail(RADIAL_ESHAPE, "table is not 16-byte aligned");
   const radial_rope_params& p = *params;
+  if (int rc = check_table(p, table, table_bytes)) return rc;
   TableArgs a = {};
   a.table = table;
   a.axes = p.axes;
@@ -338,14 +343,14 @@ extern "C" int radial_rope_table(const radial_rope_params* params, float* table,
   return RADIAL_OK;
 }
 
-extern "C" int radial_rope_fwd(const radial_rope_params* params, const float* table, int32_t B, int32_t N, int32_t D, int32_t q_heads, radial_tensor q,
+extern "C" int radial_rope_fwd(const radial_rope_params* params, const float* table, size_t table_bytes, int32_t B, int32_t N, int32_t D, int32_t q_heads, radial_tensor q,
                                radial_tensor q_out, int32_t k_heads, radial_tensor k, radial_tensor k_out, int32_t type, const int32_t* positions,
                                int32_t first, void* hip_stream) {
-  return turn(params, table, B, N, D, q_heads, q, q_out, k_heads, k, k_out, type, positions, first, false, hip_stream);
+  return turn(params, table, table_bytes, B, N, D, q_heads, q, q_out, k_heads, k, k_out, type, positions, first, false, hip_stream);
 }
 
-extern "C" int radial_rope_bwd(const radial_rope_params* params, const float* table, int32_t B, int32_t N, int32_t D, int32_t q_heads, radial_tensor dq_out,
+extern "C" int radial_rope_bwd(const radial_rope_params* params, const float* table, size_t table_bytes, int32_t B, int32_t N, int32_t D, int32_t q_heads, radial_tensor dq_out,
                                radial_tensor dq, int32_t k_heads, radial_tensor dk_out, radial_tensor dk, int32_t type, const int32_t* positions,
                                int32_t first, void* hip_stream) {
-  return turn(params, table, B, N, D, q_heads, dq_out, dq, k_heads, dk_out, dk, type, positions, first, true, hip_stream);
+  return turn(params, table, table_bytes, B, N, D, q_heads, dq_out, dq, k_heads, dk_out, dk, type, positions, first, true, hip_stream);
 }

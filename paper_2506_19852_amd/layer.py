@@ -38,11 +38,12 @@ class radial_rope_params(ctypes.Structure):
 
 _lib = None
 _types = None  # torch dtype -> RADIAL_ type
+_f32 = _bf16 = _u8 = _i32 = None  # torch dtypes, set by load()
 
 
 def load():
     """Loads libradial.so and declares the prototypes of radial_layer.h."""
-    global _lib, _types
+    global _lib, _types, _f32, _bf16, _u8, _i32
     if _lib is not None:
         return _lib
     lib = binding.load()
@@ -53,9 +54,9 @@ def load():
     lib.radial_norm_bwd.argtypes = [POINTER(radial_norm_params)] + [rows] * 4 + [floats] * 4 + [rows] * 2 + [floats] * 5 + [c_void_p, c_size_t, c_void_p]
     lib.radial_rope_table_bytes.argtypes = [POINTER(radial_rope_params)]
     lib.radial_rope_table_bytes.restype = c_size_t
-    lib.radial_rope_table.argtypes = [POINTER(radial_rope_params), c_void_p, c_void_p]
+    lib.radial_rope_table.argtypes = [POINTER(radial_rope_params), c_void_p, c_size_t, c_void_p]
     for fn in (lib.radial_rope_fwd, lib.radial_rope_bwd):
-        fn.argtypes = [POINTER(radial_rope_params), c_void_p, c_int32, c_int32, c_int32, c_int32, heads, heads, c_int32, heads, heads, c_int32,
+        fn.argtypes = [POINTER(radial_rope_params), c_void_p, c_size_t, c_int32, c_int32, c_int32, c_int32, heads, heads, c_int32, heads, heads, c_int32,
                        c_void_p, c_int32, c_void_p]
     lib.radial_quantize_groups_fp8.argtypes = [c_int32, c_int32, c_void_p, c_int32, c_int64, c_int32] + [c_void_p] * 5
     lib.radial_product_fp8.argtypes = [c_int32, c_int32, c_int32] + [c_void_p] * 4 + [c_int32, c_void_p, c_int64, c_void_p]
@@ -65,6 +66,7 @@ def load():
             fn.restype = ctypes.c_int
     torch = _load_torch()
     _types = {torch.bfloat16: RADIAL_BF16, torch.float32: RADIAL_F32}
+    _f32, _bf16, _u8, _i32 = torch.float32, torch.bfloat16, torch.uint8, torch.int32
     _lib = lib
     return lib
 
@@ -77,28 +79,33 @@ _NO_ROWS = radial_rows(None, 0, 0, RADIAL_BF16)
 def _rows(t, name, shape) -> radial_rows:
     if t is None:
         return _NO_ROWS
-    kind = _types.get(t.dtype)
     stride = t.stride()
+    kind = _types.get(t.dtype)
     if kind is None or not t.is_cuda or t.shape != shape or (stride[2] != 1 and shape[2] > 1):
         raise ValueError(f"{name} must be a CUDA bf16 or float32 tensor {list(shape)} with unit stride in C")
     return radial_rows(t.data_ptr(), stride[0], stride[1], kind)
 
 
-def _mod_stride(named, B, G, C) -> int:
-    """Elements between rows of the conditioning tensors [B, G, C] given: one stride for all of them, across batch entries too."""
-    found = None
-    for name, t in named:
+def _mods(B, G, C, **named):
+    """Addresses of the conditioning tensors [B, G, C] that are given, and the elements between their rows: one stride for all of them, across
+    batch entries too."""
+    shape, found, out = (B, G, C), None, []
+    for name, t in named.items():
         if t is None:
+            out.append(None)
             continue
-        if t.dtype is not _load_torch().float32 or not t.is_cuda or t.shape != (B, G, C) or (C > 1 and t.stride(2) != 1):
+        stride = t.stride()
+        if t.dtype is not _f32 or not t.is_cuda or t.shape != shape or (stride[2] != 1 and C > 1):
             raise ValueError(f"{name} must be a CUDA float32 tensor {[B, G, C]} with unit stride in C")
-        step = t.stride(1) if G > 1 else t.stride(0) if B > 1 else max(C, t.stride(1))
-        if G > 1 and B > 1 and t.stride(0) != G * step:
+        step = stride[1] if G > 1 else stride[0] if B > 1 else C
+        if G > 1 and B > 1 and stride[0] != G * step:
             raise ValueError(f"the rows of {name} must be evenly spaced over batch entries and groups")
-        if found is not None and step != found and B * G > 1:
-            raise ValueError(f"{', '.join(n for n, x in named if x is not None)} must have the same strides")
-        found = step if found is None else found
-    return C if found is None else found
+        if found is not None and step != found:
+            raise ValueError(f"{', '.join(n for n, x in named.items() if x is not None)} must have the same strides")
+        found = step
+        out.append(t.data_ptr())
+    out.append(C if found is None else found)
+    return out
 
 
 def _group(group, N) -> int:
@@ -109,13 +116,9 @@ def _group(group, N) -> int:
 def _channels(t, name, C):
     if t is None:
         return None
-    if t.dtype is not _load_torch().float32 or not t.is_cuda or t.shape != (C,) or (C > 1 and t.stride(0) != 1):
+    if t.dtype is not _f32 or not t.is_cuda or t.shape != (C,) or (C > 1 and t.stride()[0] != 1):
         raise ValueError(f"{name} must be a contiguous CUDA float32 tensor [C]")
     return t.data_ptr()
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
 
 
 def radial_norm_fwd(x, r, z, *, y=None, gate=None, post_weight=None, weight=None, scale=None, shift=None, group=None, post=RADIAL_NORM_NONE,
@@ -128,12 +131,10 @@ def radial_norm_fwd(x, r, z, *, y=None, gate=None, post_weight=None, weight=None
     shape = x.shape
     B, N, C = shape
     group = _group(group, N)
-    mods = (("gate", gate), ("scale", scale), ("shift", shift))
-    mod_stride = _mod_stride(mods, B, -(-N // max(group, 1)), C)
-    p = radial_norm_params(B, N, C, group, post, pre, eps, residual_scale, mod_stride, mod_stride)
-    _check(lib.radial_norm_fwd(byref(p), _rows(x, "x", shape), _rows(y, "y", shape), _ptr(gate), _channels(post_weight, "post_weight", C),
-                               _channels(weight, "weight", C), _ptr(scale), _ptr(shift), _rows(r, "r", shape), _rows(z, "z", shape),
-                               _stream_ptr(stream)))
+    gate, scale, shift, step = _mods(B, -(-N // max(group, 1)), C, gate=gate, scale=scale, shift=shift)
+    p = radial_norm_params(B, N, C, group, post, pre, eps, residual_scale, step, step)
+    _check(lib.radial_norm_fwd(byref(p), _rows(x, "x", shape), _rows(y, "y", shape), gate, _channels(post_weight, "post_weight", C),
+                               _channels(weight, "weight", C), scale, shift, _rows(r, "r", shape), _rows(z, "z", shape), _stream_ptr(stream)))
 
 
 def radial_norm_bwd_workspace(B: int, N: int, C: int, *, group=None, post=RADIAL_NORM_NONE, pre=RADIAL_NORM_LAYER) -> int:
@@ -152,12 +153,12 @@ def radial_norm_bwd(r, dz, dx, workspace, *, dr=None, y=None, dy=None, gate=None
     B, N, C = shape
     group = _group(group, N)
     G = -(-N // max(group, 1))
-    mod_stride = _mod_stride((("gate", gate), ("scale", scale)), B, G, C)
-    dmod_stride = _mod_stride((("dgate", dgate), ("dscale", dscale), ("dshift", dshift)), B, G, C)
-    p = radial_norm_params(B, N, C, group, post, pre, eps, residual_scale, mod_stride, dmod_stride)
-    _check(lib.radial_norm_bwd(byref(p), _rows(r, "r", shape), _rows(y, "y", shape), _rows(dz, "dz", shape), _rows(dr, "dr", shape), _ptr(gate),
-                               _channels(post_weight, "post_weight", C), _channels(weight, "weight", C), _ptr(scale), _rows(dx, "dx", shape),
-                               _rows(dy, "dy", shape), _ptr(dgate), _ptr(dscale), _ptr(dshift), _channels(dpost_weight, "dpost_weight", C),
+    gate, scale, step = _mods(B, G, C, gate=gate, scale=scale)
+    dgate, dscale, dshift, dstep = _mods(B, G, C, dgate=dgate, dscale=dscale, dshift=dshift)
+    p = radial_norm_params(B, N, C, group, post, pre, eps, residual_scale, step, dstep)
+    _check(lib.radial_norm_bwd(byref(p), _rows(r, "r", shape), _rows(y, "y", shape), _rows(dz, "dz", shape), _rows(dr, "dr", shape), gate,
+                               _channels(post_weight, "post_weight", C), _channels(weight, "weight", C), scale, _rows(dx, "dx", shape),
+                               _rows(dy, "dy", shape), dgate, dscale, dshift, _channels(dpost_weight, "dpost_weight", C),
                                _channels(dweight, "dweight", C), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                _stream_ptr(stream)))
 
@@ -200,53 +201,54 @@ def radial_rope_table_bytes(params: radial_rope_params) -> int:
     return int((_lib or load()).radial_rope_table_bytes(byref(params)))
 
 
-def _table(params, table):
-    if table.dtype is not _load_torch().float32 or not table.is_cuda or not table.is_contiguous():
-        raise ValueError("table must be a contiguous CUDA float32 tensor")
-    if table.numel() * 4 < radial_rope_table_bytes(params):
-        raise ValueError(f"table holds {table.numel() * 4} bytes, {radial_rope_table_bytes(params)} needed")
-    return table.data_ptr()
-
-
 def radial_rope_table(params: radial_rope_params, table, stream=None):
     """table (float32, radial_rope_table_bytes(params) bytes) <- the turns of every position."""
     lib = _lib or load()
-    _check(lib.radial_rope_table(byref(params), _table(params, table), _stream_ptr(stream)))
+    _check_table(table)
+    _check(lib.radial_rope_table(byref(params), table.data_ptr(), table.numel() * 4, _stream_ptr(stream)))
+
+
+def _check_table(table):
+    if table.dtype is not _f32 or not table.is_cuda or not table.is_contiguous():
+        raise ValueError("table must be a contiguous CUDA float32 tensor")
 
 
 _NO_HEADS = radial_tensor(None, 0, 0, 0)
 
 
-def _heads(t, name, B, N, D, dtype) -> radial_tensor:
+def _heads(t, name, shape, dtype) -> radial_tensor:
     stride = t.stride()
-    shape = t.shape
-    if t.dtype is not dtype or not t.is_cuda or len(stride) != 4 or stride[3] != 1 or shape[0] != B or shape[2] != N or shape[3] != D:
-        raise ValueError(f"{name} must be a CUDA tensor [{B}, heads, {N}, {D}] of q's type with unit stride in D")
+    if t.dtype is not dtype or not t.is_cuda or t.shape != shape or stride[3] != 1:
+        raise ValueError(f"{name} must be a CUDA tensor {list(shape)} of q's type with unit stride in D")
     return radial_tensor(t.data_ptr(), stride[0], stride[1], stride[2])
 
 
 def _rope(call, names, params, table, q, q_out, k, k_out, positions, first, stream):
-    B, q_heads, N, D = q.shape
+    shape = q.shape
+    B, q_heads, N, D = shape
     dtype = q.dtype
-    if dtype not in _types:
+    kind = _types.get(dtype)
+    if kind is None:
         raise ValueError(f"{names[0]} must be bf16 or float32")
-    if q_out.shape != q.shape:
-        raise ValueError(f"{names[1]} has shape {tuple(q_out.shape)}, expected {tuple(q.shape)}")
-    if first >= 1 << 31:
-        raise ValueError("first must be below 2^31")
     k_heads, k_in, k_to = 0, _NO_HEADS, _NO_HEADS
     if k is not None or k_out is not None:
-        if k is None or k_out is None or k.shape != k_out.shape:
-            raise ValueError(f"{names[2]} and {names[3]} go together and have one shape")
-        k_heads = k.shape[1]
-        k_in, k_to = _heads(k, names[2], B, N, D, dtype), _heads(k_out, names[3], B, N, D, dtype)
+        if k is None or k_out is None:
+            raise ValueError(f"{names[2]} and {names[3]} go together")
+        k_shape = k.shape
+        k_heads = k_shape[1]
+        if k_shape != shape and k_shape != (B, k_heads, N, D):
+            raise ValueError(f"{names[2]} must have {names[0]}'s shape but for the heads")
+        k_in, k_to = _heads(k, names[2], k_shape, dtype), _heads(k_out, names[3], k_shape, dtype)
     at = None
     if positions is not None:
-        if positions.dtype is not _load_torch().int32 or not positions.is_cuda or not positions.is_contiguous() or positions.shape != (B, N):
+        if positions.dtype is not _i32 or not positions.is_cuda or not positions.is_contiguous() or positions.shape != (B, N):
             raise ValueError("positions must be a contiguous CUDA int32 tensor [B, N]")
         at = positions.data_ptr()
-    _check(call(byref(params), _table(params, table), B, N, D, q_heads, _heads(q, names[0], B, N, D, dtype), _heads(q_out, names[1], B, N, D, dtype),
-                k_heads, k_in, k_to, _types[dtype], at, first, _stream_ptr(stream)))
+    elif first >= 1 << 31:
+        raise ValueError("first must be below 2^31")
+    _check_table(table)
+    _check(call(byref(params), table.data_ptr(), table.numel() * 4, B, N, D, q_heads, _heads(q, names[0], shape, dtype),
+                _heads(q_out, names[1], shape, dtype), k_heads, k_in, k_to, kind, at, first, _stream_ptr(stream)))
 
 
 def radial_rope_fwd(params: radial_rope_params, table, q, q_out, k=None, k_out=None, positions=None, first: int = 0, stream=None):
@@ -264,13 +266,12 @@ def radial_rope_bwd(params: radial_rope_params, table, dq_out, dq, dk_out=None, 
 # ---- products in 8-bit floating point -----------------------------------------------------------
 
 def _codes(codes, scales, name, rows, cols, scale_rows):
-    torch = _load_torch()
     if codes is None and scales is None:
         return None, None
     groups = -(-cols // 128)
-    if codes is None or codes.dtype is not torch.uint8 or not codes.is_cuda or not codes.is_contiguous() or codes.shape != (rows, groups * 128):
+    if codes is None or codes.dtype is not _u8 or not codes.is_cuda or not codes.is_contiguous() or codes.shape != (rows, groups * 128):
         raise ValueError(f"{name}codes must be a contiguous CUDA uint8 tensor {[rows, groups * 128]}")
-    if scales is None or scales.dtype is not torch.float32 or not scales.is_cuda or not scales.is_contiguous() or scales.shape != (groups, scale_rows):
+    if scales is None or scales.dtype is not _f32 or not scales.is_cuda or not scales.is_contiguous() or scales.shape != (groups, scale_rows):
         raise ValueError(f"{name}scales must be a contiguous CUDA float32 tensor {[groups, scale_rows]}")
     return codes.data_ptr(), scales.data_ptr()
 
@@ -281,27 +282,27 @@ def radial_quantize_groups_fp8(x, codes=None, scales=None, codes_t=None, scales_
     codes [rows, P], scales [P/128, rows] with P = cols rounded up to 128; codes_t [cols, Pt], scales_t [Pt/128, cols] likewise with rows.
     grouping = RADIAL_BLOCKS: one scale for 128 x 128, scales [P/128, ceil(rows/128)] and scales_t [Pt/128, ceil(cols/128)]."""
     lib = _lib or load()
-    kind = _types.get(x.dtype)
-    if kind is None or not x.is_cuda or x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
+    kind, shape, stride = _types.get(x.dtype), x.shape, x.stride()
+    if kind is None or not x.is_cuda or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError("x must be a CUDA bf16 or float32 tensor [rows, cols] with unit stride in cols")
-    rows, cols = x.shape
+    rows, cols = shape
     blocks = grouping == RADIAL_BLOCKS
     c, s = _codes(codes, scales, "", rows, cols, -(-rows // 128) if blocks else rows)
     ct, st = _codes(codes_t, scales_t, "transposed ", cols, rows, -(-cols // 128) if blocks else cols)
-    stride = x.stride(0) if rows > 1 else max(cols, x.stride(0))
-    _check(lib.radial_quantize_groups_fp8(rows, cols, x.data_ptr(), kind, stride, grouping, c, s, ct, st, _stream_ptr(stream)))
+    step = stride[0] if rows > 1 else max(cols, stride[0])
+    _check(lib.radial_quantize_groups_fp8(rows, cols, x.data_ptr(), kind, step, grouping, c, s, ct, st, _stream_ptr(stream)))
 
 
 def radial_product_fp8(a_codes, a_scales, b_codes, b_scales, out, stream=None):
     """out [M, N] (bf16) <- A B^T from the codes and scales of A [M, K] (groups) and B [N, K] (groups or blocks, by b_scales' shape)."""
     lib = _lib or load()
-    if out.dtype is not _load_torch().bfloat16 or not out.is_cuda or out.dim() != 2 or (out.stride(1) != 1 and out.shape[1] > 1):
+    shape, stride = out.shape, out.stride()
+    if out.dtype is not _bf16 or not out.is_cuda or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError("out must be a CUDA bf16 tensor [M, N] with unit stride in N")
-    M, N = out.shape
+    M, N = shape
     K = a_codes.shape[-1]
     a, sa = _codes(a_codes, a_scales, "a_", M, K, M)
     blocks = b_scales.shape[-1] != N
     b, sb = _codes(b_codes, b_scales, "b_", N, K, -(-N // 128) if blocks else N)
-    stride = out.stride(0) if M > 1 else max(N, out.stride(0))
-    _check(lib.radial_product_fp8(M, N, K, a, sa, b, sb, RADIAL_BLOCKS if blocks else RADIAL_GROUPS, out.data_ptr(), stride,
-                                  _stream_ptr(stream)))
+    step = stride[0] if M > 1 else max(N, stride[0])
+    _check(lib.radial_product_fp8(M, N, K, a, sa, b, sb, RADIAL_BLOCKS if blocks else RADIAL_GROUPS, out.data_ptr(), step, _stream_ptr(stream)))

@@ -147,14 +147,14 @@ BAD_PARAMS = [
 def test_rope_parameters(change, text):
     p = _params(**change)
     assert rl.radial_rope_table_bytes(p) == 0
-    _refused(rl.load().radial_rope_table(ctypes.byref(p), AT, None), EINVAL, text)
+    _refused(rl.load().radial_rope_table(ctypes.byref(p), AT, 1 << 30, None), EINVAL, text)
     for direction in ("fwd", "bwd"):
         _refused(_rope(direction, p), EINVAL, text)
 
 
 def _rope(direction="fwd", p=None, **change):
     t = rb.radial_tensor(AT, 4096, 128, 512)
-    a = dict(table=AT, B=1, N=10, D=64, q_heads=4, q=t, q_out=t, k_heads=2, k=t, k_out=t, type=BF16, positions=None, first=0)
+    a = dict(table=AT, bytes=1 << 30, B=1, N=10, D=64, q_heads=4, q=t, q_out=t, k_heads=2, k=t, k_out=t, type=BF16, positions=None, first=0)
     a.update(change)
     fn = getattr(rl.load(), "radial_rope_" + direction)
     return fn(ctypes.byref(p or _params()), *a.values(), None)
@@ -165,7 +165,7 @@ def _heads(ptr=AT, sb=4096, sh=128, sn=512):
 
 
 @pytest.mark.parametrize("change, code, text", [
-    (dict(table=None), EINVAL, "table"), (dict(table=AT + 4), ESHAPE, "table"), (dict(B=0), EINVAL, ">= 1"), (dict(N=-1), EINVAL, ">= 1"), (dict(q_heads=0), EINVAL, ">= 1"),
+    (dict(table=None), EINVAL, "table"), (dict(table=AT + 4), ESHAPE, "table"), (dict(bytes=(4 * 8 + 5 * 12 + 6 * 12) * 8 - 1), ESHAPE, "needed"), (dict(B=0), EINVAL, ">= 1"), (dict(N=-1), EINVAL, ">= 1"), (dict(q_heads=0), EINVAL, ">= 1"),
     (dict(D=4), EUNSUPPORTED, "head dimension"), (dict(D=68), EUNSUPPORTED, "head dimension"), (dict(D=1032), EUNSUPPORTED, "head dimension"), (dict(type=2), EINVAL, "type"),
     (dict(D=56), ESHAPE, "turn 64"), (dict(q=_heads(None)), EINVAL, "ptr is NULL"), (dict(q_out=_heads(AT + 8)), ESHAPE, "16-byte"), (dict(q=_heads(sn=56)), ESHAPE, "strides"),
     (dict(q=_heads(sn=516)), ESHAPE, "strides"), (dict(k=_heads(sh=-8)), ESHAPE, "strides"), (dict(k=_heads(None)), EINVAL, "ptr is NULL"),
@@ -179,9 +179,10 @@ def test_rope_arguments(change, code, text):
 
 def test_rope_table_arguments():
     lib, p = rl.load(), _params()
-    _refused(lib.radial_rope_table(None, AT, None), EINVAL, "params")
-    _refused(lib.radial_rope_table(ctypes.byref(p), None, None), EINVAL, "table")
-    _refused(lib.radial_rope_table(ctypes.byref(p), AT + 8, None), ESHAPE, "table")
+    _refused(lib.radial_rope_table(None, AT, 1 << 30, None), EINVAL, "params")
+    _refused(lib.radial_rope_table(ctypes.byref(p), None, 1 << 30, None), EINVAL, "table")
+    _refused(lib.radial_rope_table(ctypes.byref(p), AT, 8, None), ESHAPE, "needed")
+    _refused(lib.radial_rope_table(ctypes.byref(p), AT + 8, 1 << 30, None), ESHAPE, "table")
     assert rl.radial_rope_table_bytes(p) == (4 * 8 + 5 * 12 + 6 * 12) * 8
     assert lib.radial_rope_table_bytes(None) == 0
     for bad in (dict(sizes=[], dims=[]), dict(sizes=[1, 2], dims=[4]), dict(sizes=[1], dims=[4], layout="other"), dict(sizes=[1], dims=[4], scaling="other"),
@@ -243,7 +244,7 @@ def test_shapes_and_types_are_checked_before_the_library_is_entered():
                 dict(q=q, q_out=q, positions=_fake(torch.int64, 1, 8)), dict(q=q, q_out=q, positions=_fake(i32, 8)), dict(q=q, q_out=q, first=1 << 31)):
         with pytest.raises(ValueError):
             rl.radial_rope_fwd(p, table, **bad, stream=1)
-    with pytest.raises(ValueError, match="needed"):
+    with pytest.raises(rb.RadialError, match="needed"):
         rl.radial_rope_fwd(p, _fake(f32, 8 * 64 - 1), q, q, stream=1)
     m = _fake(bf16, 100, 200)
     codes, scales = _fake(u8, 100, 256), _fake(f32, 2, 100)

@@ -1,0 +1,60 @@
+"""The rules of the 8-bit product on the host: every form of tiles is reached, and by a size that the GPU tests run; every tile is taken once; the
+pieces of a stage fill their place in LDS without overlap and are read without bank conflicts."""
+import os
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+
+from paper_2506_19852_amd import build as hip_build
+from test_gpu_product import SIZES
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def rule(tmp_path_factory):
+    if not os.path.exists(hip_build.HIPCC) and shutil.which(hip_build.HIPCC) is None:
+        pytest.skip("hipcc not available")
+    exe = tmp_path_factory.mktemp("host") / "product_rule"
+    r = subprocess.run([hip_build.HIPCC, *hip_build.FLAGS, "--cuda-host-only", os.path.join(ROOT, "tests", "host", "product_rule.hip"), "-o", str(exe)],
+                       stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert r.returncode == 0, r.stdout[-3000:]
+
+    def run(lines):
+        r = subprocess.run([str(exe)], input="\n".join(lines), stdout=subprocess.PIPE, text=True, timeout=120)
+        assert r.returncode == 0
+        return [[int(v) for v in line.split()] for line in r.stdout.strip().split("\n")]
+    return run
+
+
+def test_every_form_is_reached_by_a_tested_size(rule):
+    tested = [s for s in SIZES if s[0] > 16]
+    forms = {f[0] for f in rule([f"form {m} {n} {-(-k // 128)}" for m, n, k in tested])}
+    assert forms == set(range(8)), forms
+
+
+def test_large_products_take_large_tiles_and_few_tiles_split_the_groups(rule):
+    large, few, one = rule(["form 32760 5120 40", "form 64 512 64", "form 17 1 1"])
+    assert large[1:] == [256, 256, 1] and few[3] > 1 and one[1:3] == [64, 64] or one[1] <= 128
+
+
+@pytest.mark.parametrize("shape", [(1, 1), (1, 20), (20, 1), (7, 3), (8, 8), (9, 5), (128, 20), (17, 33)], ids=str)
+def test_every_tile_is_taken_once(rule, shape):
+    (flat,) = rule([f"tiles {shape[0]} {shape[1]}"])
+    got = {(flat[i], flat[i + 1]) for i in range(0, len(flat), 2)}
+    assert len(flat) == 2 * shape[0] * shape[1] and got == {(m, n) for m in range(shape[0]) for n in range(shape[1])}
+
+
+@pytest.mark.parametrize("operand", [0, 1])
+def test_pieces(rule, operand):
+    at, conflicts = rule([f"pieces {operand}"])
+    at = np.array(at).reshape(256, 8)
+    assert np.array_equal(np.sort(at.ravel()), np.arange(256 * 8) * 16) and (at // 256 == np.arange(256)[:, None] // 2).all()
+    # fragments of a lane lie at constant distances: rows 16 apart of A, 4 apart (within 16) of B
+    step = 4 if operand else 16
+    rows = [r for r in range(64) if r % 16 < 4] if operand else range(240)
+    for r in rows:
+        assert (at[r + step] - at[r] == step * 128).all()
+    assert conflicts == [0]
