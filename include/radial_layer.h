@@ -44,7 +44,7 @@ typedef struct {
   int32_t group;        /* tokens that share a row of conditioning: token n of batch b has row b*G + n/group,  */
                         /*   G = ceil(N/group): N for one row per batch, tokens per frame for one per frame    */
   int32_t post, pre;    /* RADIAL_NORM_*: of the branch y; of the new residual r (NONE: no z)                  */
-  float eps;            /* > 0                                                                                 */
+  float eps;            /* > 0, a normal number                                                                */
   float residual_scale; /* finite                                                                              */
   int64_t mod_stride;   /* elements from one row of gate, scale, shift to the next, >= C (6*C for chunks of    */
                         /*   [B, G, 6, C])                                                                     */

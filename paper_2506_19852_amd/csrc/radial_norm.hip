@@ -12,6 +12,7 @@
 // has the same channels in all rows of its workgroup, so that it loads the conditioning row once and keeps the sums over tokens in registers; a
 // workgroup's rows are of one group.  The backward writes a workgroup's sums to the workspace, where a second kernel adds them up
 // in a fixed order (no atomics).
+#include <float.h>
 #include <math.h>
 
 #include "radial_layer_common.h"
@@ -144,8 +145,7 @@ struct Team {
   static constexpr bool kExchanges = kWide, kEights = kFast;
   Meeting* meet;
   int32_t turn, wave, waves;
-  float C;
-  float own;       // channels of this wave (wide) or of the row
+  float of_C;  // 1 / channels of a row
   __device__ __forceinline__ float lanes(float x) const { return lane_sum<kWide ? 64 : L>(x); }
   // Every wave's values to every wave: add(values) for one after the other.
   template <class Add>
@@ -197,10 +197,10 @@ __device__ __forceinline__ float squares_about(const float (&val)[8 * V], float 
 
 template <bool kVec, int V, class T>
 __device__ __forceinline__ void statistics(const float (&val)[8 * V], int32_t kind, float eps, T& team, const Channels<kVec, V>& ch, float own_count,
-                                           float& mean, float& inverse) {
+                                           float of_own, float& mean, float& inverse) {
   mean = 0.f;
   float about = 0.f;
-  if (kind == RADIAL_NORM_LAYER) about = team.lanes(sum_of(val)) / fmaxf(own_count, 1.f);
+  if (kind == RADIAL_NORM_LAYER) about = team.lanes(sum_of(val)) * of_own;
   float squares = team.lanes(squares_about<kVec, V, T::kEights>(val, about, ch));
   if constexpr (T::kExchanges) {
     team.exchange(f32x4{about * own_count, squares, own_count, about});
@@ -209,7 +209,7 @@ __device__ __forceinline__ void statistics(const float (&val)[8 * V], int32_t ki
       mean += theirs[0];
       squares += theirs[1];
     });
-    mean /= team.C;
+    mean *= team.of_C;
     if (kind == RADIAL_NORM_LAYER)
       team.each([&](f32x4 theirs) {
         const float d = theirs[3] - mean;
@@ -218,7 +218,7 @@ __device__ __forceinline__ void statistics(const float (&val)[8 * V], int32_t ki
   } else {
     mean = about;
   }
-  inverse = 1.f / sqrtf(squares / team.C + eps);
+  inverse = __builtin_amdgcn_rsqf(squares * team.of_C + eps);  // to one unit; eps is a normal number
 }
 
 // v <- (v - mean) inverse, zero where there is no channel.
@@ -254,7 +254,7 @@ struct Share {
   Team<kWide, L, kFast> team;
   int32_t teams, first, last;  // rows first, first + teams, ... below last, of batch b
   int32_t b, group;            // group: b * groups_of_batch + g
-  float own_count;
+  float own_count, of_own;     // channels of this wave (wide) or of the row, and 1 / them
   __device__ __forceinline__ Share(const NormArgs& a, Meeting* meet) {
     group = blockIdx.x / a.chunks;
     const int32_t chunk = blockIdx.x % a.chunks;
@@ -276,8 +276,9 @@ struct Share {
     team.turn = 0;
     team.wave = threadIdx.x >> 6;
     team.waves = (blockDim.x + 63) >> 6;
-    team.C = (float)a.C;
+    team.of_C = 1.f / (float)a.C;
     own_count = team.lanes((float)ch.count());
+    of_own = 1.f / fmaxf(own_count, 1.f);
   }
 };
 
@@ -329,7 +330,7 @@ __global__ void __launch_bounds__(kWide ? 512 : 256) norm_fwd_kernel(NormArgs a)
       y.get(u);
       if (a.post != RADIAL_NORM_NONE) {
         float mean, inverse;
-        statistics<kVec, V>(u, a.post, a.eps, s.team, s.ch, s.own_count, mean, inverse);
+        statistics<kVec, V>(u, a.post, a.eps, s.team, s.ch, s.own_count, s.of_own, mean, inverse);
 #pragma unroll
         for (int i = 0; i < E; ++i) u[i] = (u[i] - mean) * inverse;
       }
@@ -339,7 +340,7 @@ __global__ void __launch_bounds__(kWide ? 512 : 256) norm_fwd_kernel(NormArgs a)
     }
     if (a.pre != RADIAL_NORM_NONE) {
       float mean, inverse;
-      statistics<kVec, V>(r, a.pre, a.eps, s.team, s.ch, s.own_count, mean, inverse);
+      statistics<kVec, V>(r, a.pre, a.eps, s.team, s.ch, s.own_count, s.of_own, mean, inverse);
 #pragma unroll
       for (int i = 0; i < E; ++i) r[i] = (r[i] - mean) * inverse * factor[i] + shift[i];
       if (live) store_row<YT, kVec, V>(row_of<YT>(a.z, s.b, n), r, s.ch);
@@ -412,7 +413,7 @@ __global__ void __launch_bounds__(kWide ? 512 : 256) norm_bwd_kernel(NormArgs a)
       now.r.get(n);
       now.dz.get(d);
       float mean, inverse;
-      statistics<kVec, V>(n, a.pre, a.eps, s.team, s.ch, s.own_count, mean, inverse);
+      statistics<kVec, V>(n, a.pre, a.eps, s.team, s.ch, s.own_count, s.of_own, mean, inverse);
       float along = 0.f, flat = 0.f;
       normalise<kVec, V, kFast>(n, mean, inverse, s.ch);
 #pragma unroll
@@ -426,8 +427,8 @@ __global__ void __launch_bounds__(kWide ? 512 : 256) norm_bwd_kernel(NormArgs a)
         along += d[i] * n[i];
       }
       two_sums(flat, along, s.team);
-      flat = a.pre == RADIAL_NORM_LAYER ? flat / s.team.C : 0.f;
-      along /= s.team.C;
+      flat = a.pre == RADIAL_NORM_LAYER ? flat * s.team.of_C : 0.f;
+      along *= s.team.of_C;
 #pragma unroll
       for (int i = 0; i < E; ++i) D[i] += inverse * (d[i] - flat - n[i] * along);
     }
@@ -443,7 +444,7 @@ __global__ void __launch_bounds__(kWide ? 512 : 256) norm_bwd_kernel(NormArgs a)
       float inverse = 1.f;
       if (a.post != RADIAL_NORM_NONE) {
         float mean;
-        statistics<kVec, V>(m, a.post, a.eps, s.team, s.ch, s.own_count, mean, inverse);
+        statistics<kVec, V>(m, a.post, a.eps, s.team, s.ch, s.own_count, s.of_own, mean, inverse);
         normalise<kVec, V, kFast>(m, mean, inverse, s.ch);
       }
       // where there is no channel m is 0, and so is gate
@@ -460,8 +461,8 @@ __global__ void __launch_bounds__(kWide ? 512 : 256) norm_bwd_kernel(NormArgs a)
           along += D[i] * m[i];
         }
         two_sums(flat, along, s.team);
-        flat = a.post == RADIAL_NORM_LAYER ? flat / s.team.C : 0.f;
-        along /= s.team.C;
+        flat = a.post == RADIAL_NORM_LAYER ? flat * s.team.of_C : 0.f;
+        along *= s.team.of_C;
 #pragma unroll
         for (int i = 0; i < E; ++i) D[i] = inverse * (D[i] - flat - m[i] * along);
       }
@@ -498,7 +499,7 @@ __global__ void __launch_bounds__(kWide ? 512 : 256) norm_bwd_kernel(NormArgs a)
 
 struct GradArgs {
   const float* partial;  // [groups][chunks][3][C]
-  float* of_group;       // [groups][2][C]: P and Q of each group, or null
+  float* of_group;       // [groups][2][C]: P and Q of each group, where another kernel adds them up, or null
   const float *gate, *post_weight, *weight, *scale;
   float *dgate, *dscale, *dshift, *dpost_weight, *dweight;
   int32_t C, chunks, groups, wants;
@@ -506,6 +507,7 @@ struct GradArgs {
 };
 
 constexpr int kGradColumns = 16, kGradSlices = 64;
+constexpr int64_t kMostInY = 65535;
 
 // The slices' sums of a column, in order.
 __device__ __forceinline__ float over_slices(const float (&sums)[kGradSlices][kGradColumns + 1], int column) {
@@ -516,12 +518,9 @@ __device__ __forceinline__ float over_slices(const float (&sums)[kGradSlices][kG
 }
 
 // 16 channels of a group: 64 slices of its workgroups' sums each, then the slices' sums.  (64 channels and 16 slices: 30 us of a small call.)
-__global__ void __launch_bounds__(kGradColumns * kGradSlices) norm_grad_kernel(GradArgs a) {
-  __shared__ float sums[3][kGradSlices][kGradColumns + 1];
+// total: P, T, Q of the channel in slices 0, 1, 2, where they are wanted (true).
+__device__ __forceinline__ bool sums_of_group(const GradArgs& a, int64_t group, float (&sums)[3][kGradSlices][kGradColumns + 1], int32_t c, float& total) {
   const int32_t lane = threadIdx.x, slice = threadIdx.y;
-  const int32_t c = blockIdx.x * kGradColumns + lane;
-  const int64_t group = blockIdx.y + (int64_t)blockIdx.z * 32768;
-  if (group >= a.groups) return;
   float sum[3] = {0.f, 0.f, 0.f};
   if (c < a.C) {
 #pragma unroll 4
@@ -535,13 +534,39 @@ __global__ void __launch_bounds__(kGradColumns * kGradSlices) norm_grad_kernel(G
 #pragma unroll
   for (int k = 0; k < 3; ++k) sums[k][slice][lane] = sum[k];
   __syncthreads();
-  if (slice >= 3 || c >= a.C || !(a.wants >> slice & 1)) return;
-  const float total = over_slices(sums[slice], lane);  // of P, T or Q
+  if (slice >= 3 || c >= a.C || !(a.wants >> slice & 1)) return false;
+  total = over_slices(sums[slice], lane);
   const int64_t mod = group * a.dmod_stride + c;
   if (slice == 0 && a.dscale) a.dscale[mod] = a.weight ? total * a.weight[c] : total;
   if (slice == 1) a.dshift[mod] = total;
   if (slice == 2 && a.dgate) a.dgate[mod] = a.post_weight ? total * a.post_weight[c] : total;
-  if (a.of_group && slice != 1) a.of_group[(group * 2 + (slice == 2)) * a.C + c] = total;
+  return true;
+}
+
+__global__ void __launch_bounds__(kGradColumns * kGradSlices) norm_grad_kernel(GradArgs a) {
+  __shared__ float sums[3][kGradSlices][kGradColumns + 1];
+  const int32_t c = blockIdx.x * kGradColumns + threadIdx.x;
+  const int64_t group = blockIdx.y + (int64_t)blockIdx.z * kMostInY;
+  if (group >= a.groups) return;
+  float total;
+  if (sums_of_group(a, group, sums, c, total) && a.of_group && threadIdx.y != 1) a.of_group[(group * 2 + (threadIdx.y == 2)) * a.C + c] = total;
+}
+
+// The same, and the gradients of the weights, where there are few groups: a workgroup takes all of them.
+__global__ void __launch_bounds__(kGradColumns * kGradSlices) norm_few_groups_kernel(GradArgs a) {
+  __shared__ float sums[3][kGradSlices][kGradColumns + 1];
+  const int32_t c = blockIdx.x * kGradColumns + threadIdx.x, slice = threadIdx.y;
+  float of_weight = 0.f;  // slice 0: dw, slice 2: dw_post
+  for (int64_t group = 0; group < a.groups; ++group) {
+    if (group) __syncthreads();
+    float total;
+    if (!sums_of_group(a, group, sums, c, total)) continue;
+    if (slice == 0) of_weight += a.scale ? total * (1.f + a.scale[group * a.mod_stride + c]) : total;
+    if (slice == 2) of_weight += a.gate ? total * a.gate[group * a.mod_stride + c] : total;
+  }
+  if (c >= a.C) return;
+  if (slice == 0 && a.dweight) a.dweight[c] = of_weight;
+  if (slice == 2 && a.dpost_weight) a.dpost_weight[c] = of_weight;
 }
 
 // dw and dw_post: sums over the groups, each times its conditioning.
@@ -651,7 +676,7 @@ int check_params(const radial_norm_params* p) {
   if (p->C > kMaxChannels) return fail(RADIAL_EUNSUPPORTED, "C must be at most %d (got %d)", kMaxChannels, p->C);
   if (p->post != RADIAL_NORM_NONE && !is_norm(p->post)) return fail(RADIAL_EINVAL, "post must be a RADIAL_NORM_ value (got %d)", p->post);
   if (p->pre != RADIAL_NORM_NONE && !is_norm(p->pre)) return fail(RADIAL_EINVAL, "pre must be a RADIAL_NORM_ value (got %d)", p->pre);
-  if (!(p->eps > 0.f) || !isfinite(p->eps)) return fail(RADIAL_EINVAL, "eps must be positive and finite");
+  if (!(p->eps >= FLT_MIN) || !isfinite(p->eps)) return fail(RADIAL_EINVAL, "eps must be positive, normal and finite");
   if (!isfinite(p->residual_scale)) return fail(RADIAL_EINVAL, "residual_scale must be finite");
   return RADIAL_OK;
 }
@@ -805,15 +830,18 @@ extern "C" int radial_norm_bwd(const radial_norm_params* params, radial_rows r, 
 
   GradArgs g = {};
   g.partial = a.partial;
-  g.of_group = dweight || dpost_weight ? a.partial + (size_t)l.groups * l.chunks * 3 * p.C : nullptr;
+  constexpr int64_t kFewGroups = 4;
+  const bool weights = dweight || dpost_weight, few = weights && l.groups <= kFewGroups;
+  g.of_group = weights && !few ? a.partial + (size_t)l.groups * l.chunks * 3 * p.C : nullptr;
   g.gate = gate; g.post_weight = post_weight; g.weight = weight; g.scale = scale;
   g.dgate = dgate; g.dscale = dscale; g.dshift = dshift; g.dpost_weight = dpost_weight; g.dweight = dweight;
   g.C = p.C; g.chunks = l.chunks; g.groups = (int32_t)l.groups; g.wants = a.wants;
   g.mod_stride = p.mod_stride; g.dmod_stride = p.dmod_stride;
   const unsigned columns = (unsigned)((p.C + kGradColumns - 1) / kGradColumns);
   const dim3 block(kGradColumns, kGradSlices);
-  const unsigned in_y = l.groups < 32768 ? (unsigned)l.groups : 32768u, in_z = (unsigned)((l.groups + 32767) / 32768);
-  norm_grad_kernel<<<dim3(columns, in_y, in_z), block, 0, (hipStream_t)hip_stream>>>(g);
+  const unsigned in_y = (unsigned)(l.groups < kMostInY ? l.groups : kMostInY), in_z = (unsigned)((l.groups + kMostInY - 1) / kMostInY);
+  if (few) norm_few_groups_kernel<<<dim3(columns), block, 0, (hipStream_t)hip_stream>>>(g);
+  else norm_grad_kernel<<<dim3(columns, in_y, in_z), block, 0, (hipStream_t)hip_stream>>>(g);
   RADIAL_HIP_TRY(hipGetLastError());
   if (g.of_group) {
     norm_weight_grad_kernel<<<dim3(columns), block, 0, (hipStream_t)hip_stream>>>(g);

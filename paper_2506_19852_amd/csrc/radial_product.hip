@@ -172,6 +172,7 @@ struct ProductArgs {
   __bf16* out;
   int64_t out_stride;
   int32_t M, N, groups;
+  int64_t sa_stride;  // scales of A from one group to the next
   int32_t b_blocks;  // 128-row blocks of B
   int32_t vec;       // rows of out start 16-byte aligned
 };
@@ -188,9 +189,9 @@ __device__ __forceinline__ f32x4 product16(i32x8 a, i32x8 b) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);  // formats 0: E4M3; no block exponents
 }
 
-// Up to 16 rows: bound by reading B.  A workgroup of 8 waves takes 16 columns of C, each wave every 8th group, straight from memory (a lane's 32
-// bytes of a row, four lanes a line); the parts meet in LDS.  5120 x 5120, 2 rows: 8.7 us with the launch (a tile of 64 x 64: 11.4); 40 rows,
-// three blocks of 16: 22.1 (11.5).
+// Up to 16 rows: bound by reading B (2 x 30 720 x 5120: 27.7 us, 5.7 TB/s; 2 x 5120 x 5120: 8.8 us, of which the launch is half).  A workgroup of
+// 8 waves takes 16 columns of C, each wave every 8th group, straight from memory (a lane's 32 bytes of a row, four lanes a line); the parts meet in
+// LDS.  Four groups of a wave at a time, or 16 waves, were slower by 0.7 us and more.
 constexpr int kParts = 8;
 template <bool kBlocks>
 __global__ void __launch_bounds__(64 * kParts) product_rows_kernel(ProductArgs a) {
@@ -206,7 +207,7 @@ __global__ void __launch_bounds__(64 * kParts) product_rows_kernel(ProductArgs a
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   for (int32_t g = wave; g < a.groups; g += kParts) {
     const f32x4 d = product16(sixteen_rows(b_row + (int64_t)g * kGroup), sixteen_rows(a_row + (int64_t)g * kGroup));
-    const float sa = a.sa[(int64_t)g * a.M + row];
+    const float sa = a.sa[(int64_t)g * a.sa_stride + row];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float sb = kBlocks ? a.sb[(int64_t)g * a.b_blocks + n0 / kGroup] : a.sb[(int64_t)g * a.N + min(n[e], a.N - 1)];
@@ -300,7 +301,7 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) product_tile_
 #pragma unroll
     for (int i = 0; i < S::kScaleCopies; ++i) {
       const int first = (wave * S::kScaleCopies + i) * 64;
-      const float* base = first < S::kTileM || kBlocks ? a.sa + g * a.M : a.sb + g * a.N;
+      const float* base = first < S::kTileM || kBlocks ? a.sa + g * a.sa_stride : a.sb + g * a.N;
       copy4_to_lds_sv_masked(base, scale_from[i], lds0 + stage + S::kCodes + first * 4, lanes);
     }
   };
@@ -485,13 +486,8 @@ int launch_tiles(const ProductArgs& a, hipStream_t stream) {
 }
 
 template <bool kBlocks>
-int launch_product(const ProductArgs& a, hipStream_t stream) {
-  if (a.M <= 16) {
-    product_rows_kernel<kBlocks><<<dim3((unsigned)((a.N + 15) / 16)), dim3(64 * kParts), 0, stream>>>(a);
-    RADIAL_HIP_TRY(hipGetLastError());
-    return RADIAL_OK;
-  }
-  switch (choose_tiles(a.M, a.N, a.groups)) {
+int launch_form(int form, const ProductArgs& a, hipStream_t stream) {
+  switch (form) {
     case 0: return launch_tiles<2, 4, 8, 2, 1, kBlocks>(a, stream);
     case 1: return launch_tiles<2, 4, 6, 2, 1, kBlocks>(a, stream);
     case 2: return launch_tiles<2, 2, 4, 2, 1, kBlocks>(a, stream);
@@ -501,6 +497,25 @@ int launch_product(const ProductArgs& a, hipStream_t stream) {
     case 6: return launch_tiles<2, 1, 2, 2, 2, kBlocks>(a, stream);
     default: return launch_tiles<2, 1, 2, 2, 4, kBlocks>(a, stream);
   }
+}
+
+template <bool kBlocks>
+int launch_product(const ProductArgs& a, hipStream_t stream) {
+  if (a.M <= 16) {
+    product_rows_kernel<kBlocks><<<dim3((unsigned)((a.N + 15) / 16)), dim3(64 * kParts), 0, stream>>>(a);
+    RADIAL_HIP_TRY(hipGetLastError());
+    return RADIAL_OK;
+  }
+  const ProductPlan plan = plan_product(a.M, a.N, a.groups);
+  ProductArgs part = a;
+  part.M = plan.rows;
+  if (int rc = launch_form<kBlocks>(plan.form, part, stream)) return rc;
+  if (plan.rows == a.M) return RADIAL_OK;
+  part.M = a.M - plan.rows;
+  part.a += (int64_t)plan.rows * a.groups * kGroup;
+  part.sa += plan.rows;
+  part.out += plan.rows * a.out_stride;
+  return launch_form<kBlocks>(plan.rest, part, stream);
 }
 
 }  // namespace
@@ -553,7 +568,7 @@ extern "C" int radial_product_fp8(int32_t M, int32_t N, int32_t K, const uint8_t
   ProductArgs a = {};
   a.a = a_codes; a.b = b_codes; a.sa = a_scales; a.sb = b_scales;
   a.out = (__bf16*)out; a.out_stride = out_stride;
-  a.M = M; a.N = N;
+  a.M = M; a.N = N; a.sa_stride = M;
   a.groups = (K + kGroup - 1) / kGroup;
   a.b_blocks = (N + kGroup - 1) / kGroup;
   a.vec = ((uintptr_t)out & 15u) == 0 && out_stride % 8 == 0;

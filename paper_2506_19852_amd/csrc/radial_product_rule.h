@@ -18,23 +18,54 @@ constexpr TileForm kTileForms[] = {
     {256, 256, 1, 1, 1.66f, 1.66f, 6.f}, {192, 256, 1, 1, 1.33f, 1.33f, 5.f}, {128, 128, 2, 1, 1.28f, 0.80f, 3.f}, {128, 128, 1, 2, 1.25f, 1.25f, 3.f},
     {64, 128, 2, 1, 0.74f, 0.55f, 2.5f}, {64, 128, 1, 2, 0.80f, 0.80f, 2.5f}, {64, 64, 2, 2, 0.90f, 0.62f, 2.f},   {64, 64, 1, 4, 1.10f, 1.10f, 2.f},
 };
-inline int choose_tiles(int32_t M, int32_t N, int32_t groups) {
-  constexpr int64_t kUnits = 256;
+constexpr int kTileFormCount = sizeof(kTileForms) / sizeof(kTileForms[0]);
+constexpr int64_t kComputeUnits = 256;
+
+inline double tile_time(const TileForm& f, int32_t M, int32_t N, int32_t groups) {
+  const int64_t tiles = (((int64_t)M + f.rows - 1) / f.rows) * (((int64_t)N + f.columns - 1) / f.columns);
+  const int64_t round = kComputeUnits * f.at_once, full = tiles / round, rest = tiles % round;
+  const double stages = (groups + f.split - 1) / f.split;
+  const double last = rest == 0 ? 0.0 : rest <= kComputeUnits ? stages * f.stage_one + f.besides : stages * f.stage_full + f.besides;
+  return full * (stages * f.stage_full + f.besides) + last;
+}
+
+inline int choose_tiles(int32_t M, int32_t N, int32_t groups, double* time) {
   int best = 0;
-  double least = 0;
-  for (int i = 0; i < (int)(sizeof(kTileForms) / sizeof(kTileForms[0])); ++i) {
-    const TileForm& f = kTileForms[i];
-    const int64_t tiles = (((int64_t)M + f.rows - 1) / f.rows) * (((int64_t)N + f.columns - 1) / f.columns);
-    const int64_t round = kUnits * f.at_once, full = tiles / round, rest = tiles % round;
-    const double stages = (groups + f.split - 1) / f.split;
-    const double last = rest == 0 ? 0.0 : rest <= kUnits ? stages * f.stage_one + f.besides : stages * f.stage_full + f.besides;
-    const double time = full * (stages * f.stage_full + f.besides) + last;
-    if (i == 0 || time < least) {
+  for (int i = 0; i < kTileFormCount; ++i) {
+    const double t = tile_time(kTileForms[i], M, N, groups);
+    if (i == 0 || t < *time) {
       best = i;
-      least = time;
+      *time = t;
     }
   }
   return best;
+}
+
+// The forms of a product: one for all rows, or where whole rounds of large tiles leave a small part of a round over, one for the rows of the whole rounds and
+// another, in a launch of its own, for the rest.  (5120 x 5120 x 14 040: 400 tiles of 256 x 256 are two rounds; 240 of them, and 220 of 192 x 256,
+// one round each.)
+struct ProductPlan {
+  int32_t rows, form, rest;  // rows in `form`, those behind them in `rest`
+};
+inline ProductPlan plan_product(int32_t M, int32_t N, int32_t groups) {
+  constexpr double kLaunch = 8.0, kWorth = 0.95;  // us of another launch and its start; what the estimate has to promise
+  double least = 0;
+  ProductPlan plan = {M, choose_tiles(M, N, groups, &least), 0};
+  least *= kWorth;
+  for (int form = 0; form < 2; ++form) {
+    const TileForm& f = kTileForms[form];
+    const int64_t of_row = ((int64_t)N + f.columns - 1) / f.columns, tiles = ((int64_t)M + f.rows - 1) / f.rows * of_row;
+    const int64_t rows = tiles / kComputeUnits * kComputeUnits / of_row * f.rows;
+    if (rows < f.rows || rows >= M) continue;
+    double rest_time = 0;
+    const int rest = choose_tiles((int32_t)(M - rows), N, groups, &rest_time);
+    const double time = tile_time(f, (int32_t)rows, N, groups) + rest_time + kLaunch;
+    if (time < least) {
+      least = time;
+      plan = {(int32_t)rows, form, rest};
+    }
+  }
+  return plan;
 }
 
 // Tile of a workgroup.  XCD x of 8 (workgroup id mod 8) gets a run of neighbouring tiles, in bands of 8 rows of tiles, column by column: the 32 that

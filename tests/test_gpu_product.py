@@ -79,7 +79,8 @@ def test_what_is_not_finite_stays_in_its_group():
 # M, N, K
 SIZES = [(1, 1, 1), (1, 5120, 5120), (2, 300, 1000), (16, 128, 128), (17, 129, 256), (33, 64, 384), (64, 512, 1536), (65, 96, 128), (100, 1961, 1000),
          (128, 128, 128), (256, 256, 512), (257, 255, 130), (700, 900, 640), (1024, 1024, 1024), (1237, 520, 2048), (2048, 1792, 384),
-         (517, 3604, 740), (517, 3608, 600), (385, 2519, 1400), (3601, 1032, 600), (2050, 3999, 640), (3604, 3601, 600), (3604, 3608, 384)]
+         (517, 3604, 740), (517, 3608, 600), (385, 2519, 1400), (3601, 1032, 600), (2050, 3999, 640), (3604, 3601, 600), (3604, 3608, 384),
+         (4109, 3999, 1560)]
 
 
 @pytest.mark.parametrize("blocks", [False, True], ids=["groups", "blocks"])

@@ -37,7 +37,17 @@ def test_every_form_is_reached_by_a_tested_size(rule):
 
 def test_large_products_take_large_tiles_and_few_tiles_split_the_groups(rule):
     large, few, one = rule(["form 32760 5120 40", "form 64 512 64", "form 17 1 1"])
-    assert large[1:] == [256, 256, 1] and few[3] > 1 and one[1:3] == [64, 64] or one[1] <= 128
+    assert large[1:4] == [256, 256, 1] and few[3] > 1 and max(one[1:3]) <= 128
+
+
+def test_rows_left_over_take_a_form_of_their_own(rule):
+    shapes = [(m, n, g) for m in (300, 2000, 5120, 5121, 9999, 14040, 32760) for n in (1500, 5120, 8192) for g in (3, 40, 110)]
+    got = rule([f"form {m} {n} {g}" for m, n, g in shapes])
+    for (m, n, g), (form, rows, columns, _, of_form, rest) in zip(shapes, got):
+        assert of_form == m or (0 < of_form < m and of_form % rows == 0 and form < 2), (m, n, g)
+    assert any(r[4] != m for (m, _, _), r in zip(shapes, got)) and any(r[4] == m for (m, _, _), r in zip(shapes, got))
+    tested = [s for s in SIZES if s[0] > 16]
+    assert any(r[4] != s[0] for s, r in zip(tested, rule([f"form {m} {n} {-(-k // 128)}" for m, n, k in tested])))
 
 
 @pytest.mark.parametrize("shape", [(1, 1), (1, 20), (20, 1), (7, 3), (8, 8), (9, 5), (128, 20), (17, 33)], ids=str)
