@@ -303,6 +303,67 @@ def complexity_curve(frames_list, heads, args):
     print(json.dumps(summary))
 
 
+def layer_times(w, args):
+    """Prints one JSON line: the attention half of a layer at workload w's sizes, hidden size H*D, with random weights: norm, projection of q, k, v,
+    rotary positions, block-sparse attention, output projection, gated residual and norm; the projections in E4M3 with a scale for each 128 values."""
+    import torch
+    from paper_2506_19852_amd import binding as rb
+    from paper_2506_19852_amd import layer as rl
+
+    dev, N, H, D = "cuda:0", w.N, w.H, w.D
+    C = H * D
+    g = torch.Generator(device=dev).manual_seed(w.seed & 0x7fffffff)
+
+    def rand(*shape, size=1.0, dtype=torch.bfloat16):
+        return torch.empty(shape, dtype=dtype, device=dev).normal_(0.0, size, generator=g)
+
+    def codes(rows, cols, blocks=False):
+        groups = -(-cols // 128)
+        return torch.empty((rows, groups * 128), dtype=torch.uint8, device=dev), torch.empty((groups, -(-rows // 128) if blocks else rows), device=dev)
+
+    x, mod = rand(w.B, N, C), rand(w.B, 1, 6, C, size=0.3, dtype=torch.float32)
+    weights = {}
+    for name, rows in (("qkv", 3 * C), ("out", C)):
+        weights[name] = codes(rows, C, True)
+        rl.radial_quantize_groups_fp8(rand(rows, C, size=C ** -0.5), *weights[name], grouping=rl.RADIAL_BLOCKS)
+    params = rl.rope_params([w.frames, w.grid_h, w.grid_w], [16, D // 2 - 8, D // 2 - 8])
+    table = torch.empty(rl.radial_rope_table_bytes(params) // 4, device=dev)
+    rl.radial_rope_table(params, table)
+    mask = rb.radial_mask_build(w.frames, w.tokens_per_frame, w.block, 1)
+    h, o, z, r, attn = (torch.empty_like(x) for _ in range(5))
+    qkv = torch.empty((w.B, N, 3, H, D), dtype=torch.bfloat16, device=dev)
+    q, k = (torch.empty((w.B, H, N, D), dtype=torch.bfloat16, device=dev) for _ in range(2))
+    act = codes(w.B * N, C)
+    heads = [qkv[:, :, i].transpose(1, 2) for i in range(3)]
+    parts = [
+        ("norm", lambda: rl.radial_norm_fwd(x, None, h, scale=mod[:, :, 0], shift=mod[:, :, 1])),
+        ("quantise", lambda: rl.radial_quantize_groups_fp8(h.view(-1, C), *act)),
+        ("project_qkv", lambda: rl.radial_product_fp8(*act, *weights["qkv"], qkv.view(-1, 3 * C))),
+        ("rotary", lambda: rl.radial_rope_fwd(params, table, heads[0], q, heads[1], k)),
+        ("attention", lambda: rb.radial_attn_fwd(q, k, heads[2], attn.view(w.B, N, H, D).transpose(1, 2), None, mask, w.scale)),
+        ("quantise_out", lambda: rl.radial_quantize_groups_fp8(attn.view(-1, C), *act)),
+        ("project_out", lambda: rl.radial_product_fp8(*act, *weights["out"], o.view(-1, C))),
+        ("residual_norm", lambda: rl.radial_norm_fwd(x, r, z, y=o, gate=mod[:, :, 2], scale=mod[:, :, 3], shift=mod[:, :, 4])),
+    ]
+    total = {name: 0.0 for name, _ in parts}
+    for step in range(args.warmup + args.steps):
+        marks = [torch.cuda.Event(enable_timing=True) for _ in range(len(parts) + 1)]
+        marks[0].record()
+        for (_, call), mark in zip(parts, marks[1:]):
+            call()
+            mark.record()
+        torch.cuda.synchronize()
+        if step >= args.warmup:
+            for i, (name, _) in enumerate(parts):
+                total[name] += marks[i].elapsed_time(marks[i + 1]) / args.steps
+    mask.free()
+    ms = sum(total.values())
+    print(json.dumps({"metric": "attention half of a layer, forward", "value": round(ms, 3), "unit": "ms", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
+                      "higher_is_better": False, "dtype": "bf16, projections E4M3 with a scale for each 128 values", "data": "synthetic",
+                      "config": {"model": w.name, "global_batch": w.B, "seq_len": N, "hidden": C}, "ms": {n: round(t, 4) for n, t in total.items()},
+                      "attention_share": round(total["attention"] / ms, 4)}))
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -326,6 +387,8 @@ def main():
     ap.add_argument("--curve-frames", default=None, metavar="F1,F2,...",
                     help="instead of the benchmark line: forward time vs video length at the 720p geometry (s = 3600)")
     ap.add_argument("--curve-heads", type=int, default=2)
+    ap.add_argument("--layer", action="store_true",
+                    help="instead of the benchmark line: the attention half of a layer at the workload's sizes, part by part")
     ap.add_argument("--secondary", default="cfg2_wan480p,cfg4_hunyuan720p_4x,cfg5_wan480p_4x_bwd", metavar="W1,W2,...",
                     help="other workloads reported in the line's `secondary` array (kernel times only; 'none' to skip)")
     ap.add_argument("--secondary-launches", type=int, default=2)
@@ -350,6 +413,9 @@ def main():
     from paper_2506_19852_amd import workloads as wl
 
     w = wl.WORKLOADS[args.workload]
+    if args.layer:
+        layer_times(w, args)
+        return
     width_num, width_den = (int(t) for t in args.width_scale.split("/"))
     dev = "cuda:0"
     torch.cuda.set_device(0)

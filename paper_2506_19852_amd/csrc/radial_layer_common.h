@@ -11,6 +11,8 @@
 namespace radial {
 
 inline bool is_type(int32_t t) { return t == RADIAL_BF16 || t == RADIAL_F32; }
+// Threads that a launch may have in its first dimension.
+constexpr int64_t kMostThreads = (1LL << 32) - 1024;
 inline int size_of(int32_t type) { return type == RADIAL_F32 ? 4 : 2; }
 
 // ---- elements ---------------------------------------------------------------------------------

@@ -714,7 +714,7 @@ NormArgs common_args(const radial_norm_params& p, const Layout& l) {
 }
 
 int check_grid(const Layout& l) {
-  return l.groups * l.chunks <= 0x7fffffffLL ? RADIAL_OK : fail(RADIAL_ESHAPE, "too many groups for one launch");
+  return l.groups * l.chunks <= kMostThreads / 512 ? RADIAL_OK : fail(RADIAL_ESHAPE, "too many groups for one launch");
 }
 
 }  // namespace

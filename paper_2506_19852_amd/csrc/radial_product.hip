@@ -157,11 +157,51 @@ __global__ void __launch_bounds__(256) quantize_groups_kernel(QuantArgs a) {
   }
 }
 
-template <class T, bool kBlocks>
-void launch_quantize(const QuantArgs& a, unsigned grid, hipStream_t stream) {
-  if (a.codes && a.codes_t) quantize_groups_kernel<T, kBlocks, true, true><<<dim3(grid), dim3(256), 0, stream>>>(a);
-  else if (a.codes) quantize_groups_kernel<T, kBlocks, true, false><<<dim3(grid), dim3(256), 0, stream>>>(a);
-  else quantize_groups_kernel<T, kBlocks, false, true><<<dim3(grid), dim3(256), 0, stream>>>(a);
+// Groups along the rows alone need no tile: a thread holds one row's eight columns.  Against eight rows a thread, as above, 2 x 5120 took 2.4 us instead
+// of 4.9, 1237 x 1000 2.6 (6.3), 32 760 x 5120 93 (100): 5.4 TB/s.
+template <class T>
+__global__ void __launch_bounds__(256) quantize_rows_kernel(QuantArgs a) {
+  const int32_t tc = threadIdx.x & 15, col_tile = blockIdx.x % a.col_tiles;
+  const int32_t row = blockIdx.x / a.col_tiles * 16 + (threadIdx.x >> 4), c0 = col_tile * kGroup + tc * 8;
+  const bool live = row < a.rows;
+  const T* p = (const T*)a.x + (int64_t)(live ? row : 0) * a.stride + c0;
+  float v[8];
+  if (a.vec && c0 + 8 <= a.cols) {
+    Eight<T> raw;
+    raw.load(p);
+    raw.get(v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c0 + j < a.cols ? (float)p[j] : 0.f;
+  }
+  float amax = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(v[j]));
+  amax = max_dpp<kSwapOnes>(amax);
+  amax = max_dpp<kSwapTwos>(amax);
+  amax = max_dpp<kHalfRowMirror>(amax);
+  amax = max_dpp<kRowMirror>(amax);
+  const Quotient q(amax);
+  if (!live) return;
+  *(u32x2*)(a.codes + ((int64_t)row * a.col_tiles + col_tile) * kGroup + tc * 8) =
+      u32x2{four_codes(q(v[0]), q(v[1]), q(v[2]), q(v[3])), four_codes(q(v[4]), q(v[5]), q(v[6]), q(v[7]))};
+  if (tc == 0) a.scales[(int64_t)col_tile * a.rows + row] = q.scale;
+}
+
+template <class T>
+int launch_quantize(const QuantArgs& a, bool blocks, hipStream_t stream) {
+  const bool rows_alone = a.codes && !a.codes_t && !blocks;
+  const int64_t grid = rows_alone ? ((int64_t)a.rows + 15) / 16 * a.col_tiles : (int64_t)a.row_tiles * a.col_tiles;
+  if (grid > kMostThreads / 256) return fail(RADIAL_ESHAPE, "x is too large for one launch");
+  const dim3 blocks_of_grid((unsigned)grid), threads(256);
+  if (rows_alone) quantize_rows_kernel<T><<<blocks_of_grid, threads, 0, stream>>>(a);
+  else if (blocks && a.codes && a.codes_t) quantize_groups_kernel<T, true, true, true><<<blocks_of_grid, threads, 0, stream>>>(a);
+  else if (blocks && a.codes) quantize_groups_kernel<T, true, true, false><<<blocks_of_grid, threads, 0, stream>>>(a);
+  else if (blocks) quantize_groups_kernel<T, true, false, true><<<blocks_of_grid, threads, 0, stream>>>(a);
+  else if (a.codes) quantize_groups_kernel<T, false, true, true><<<blocks_of_grid, threads, 0, stream>>>(a);
+  else quantize_groups_kernel<T, false, false, true><<<blocks_of_grid, threads, 0, stream>>>(a);
+  RADIAL_HIP_TRY(hipGetLastError());
+  return RADIAL_OK;
 }
 
 // ---- product ----------------------------------------------------------------------------------------
@@ -475,7 +515,7 @@ template <int kWavesM, int kWavesN, int kMTiles, int kStages, int kSplit, bool k
 int launch_tiles(const ProductArgs& a, hipStream_t stream) {
   using S = TileShape<kWavesM, kWavesN, kMTiles, kStages, kSplit>;
   const int64_t tiles = ((int64_t)a.M + S::kTileM - 1) / S::kTileM * (((int64_t)a.N + S::kTileN - 1) / S::kTileN);
-  if (tiles > 0x7fffffffLL) return fail(RADIAL_ESHAPE, "M*N is too large for one launch");
+  if (tiles > kMostThreads / (64 * S::kWaves * kSplit)) return fail(RADIAL_ESHAPE, "M*N is too large for one launch");
   if constexpr (S::kLds > 65536) {
     static DeviceOnce configured;
     if (int rc = allow_dynamic_lds(configured, (const void*)product_tile_kernel<kWavesM, kWavesN, kMTiles, kStages, kSplit, kBlocks>, S::kLds)) return rc;
@@ -535,24 +575,15 @@ extern "C" int radial_quantize_groups_fp8(int32_t rows, int32_t cols, const void
   if (stride < cols) return fail(RADIAL_ESHAPE, "stride must not be below cols");
   if (((uintptr_t)codes | (uintptr_t)codes_t) & 15u) return fail(RADIAL_ESHAPE, "codes are not 16-byte aligned");
   if (((uintptr_t)scales | (uintptr_t)scales_t) & 3u) return fail(RADIAL_ESHAPE, "scales are not aligned to their elements");
+  if (rows > 0x7fffffff - kGroup || cols > 0x7fffffff - kGroup) return fail(RADIAL_ESHAPE, "x is too large for one launch");
   QuantArgs a = {};
   a.x = x; a.stride = stride; a.rows = rows; a.cols = cols;
   a.codes = codes; a.scales = scales; a.codes_t = codes_t; a.scales_t = scales_t;
   a.row_tiles = (int32_t)(((int64_t)rows + kGroup - 1) / kGroup);
   a.col_tiles = (int32_t)(((int64_t)cols + kGroup - 1) / kGroup);
   a.vec = ((uintptr_t)x & 15u) == 0 && stride * size_of(type) % 16 == 0;
-  const int64_t grid = (int64_t)a.row_tiles * a.col_tiles;
-  if (rows > 0x7fffffff - kGroup || cols > 0x7fffffff - kGroup || grid > 0x7fffffffLL) return fail(RADIAL_ESHAPE, "x is too large for one launch");
-  hipStream_t stream = (hipStream_t)hip_stream;
-  if (type == RADIAL_F32) {
-    if (grouping == RADIAL_BLOCKS) launch_quantize<float, true>(a, (unsigned)grid, stream);
-    else launch_quantize<float, false>(a, (unsigned)grid, stream);
-  } else {
-    if (grouping == RADIAL_BLOCKS) launch_quantize<__bf16, true>(a, (unsigned)grid, stream);
-    else launch_quantize<__bf16, false>(a, (unsigned)grid, stream);
-  }
-  RADIAL_HIP_TRY(hipGetLastError());
-  return RADIAL_OK;
+  const bool blocks = grouping == RADIAL_BLOCKS;
+  return type == RADIAL_F32 ? launch_quantize<float>(a, blocks, (hipStream_t)hip_stream) : launch_quantize<__bf16>(a, blocks, (hipStream_t)hip_stream);
 }
 
 extern "C" int radial_product_fp8(int32_t M, int32_t N, int32_t K, const uint8_t* a_codes, const float* a_scales, const uint8_t* b_codes,

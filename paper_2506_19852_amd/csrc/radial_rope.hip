@@ -301,10 +301,10 @@ int turn(const radial_rope_params* params, const float* table, size_t table_byte
   const Pieces pieces = interleaved ? Pieces::kInterleaved : a.pairs % 8 == 0 ? Pieces::kHalf : Pieces::kSingles;
   a.units = pieces == Pieces::kInterleaved ? D / 8 : pieces == Pieces::kHalf ? a.pairs / 8 + (D - 2 * a.pairs) / 8 : a.pairs + D - 2 * a.pairs;
   const int32_t heads = q_heads + k_heads;
+  if ((int64_t)B * N > kMostThreads / a.units) return fail(RADIAL_ESHAPE, "B*N*D is too large for one launch");
   const int64_t lanes = (int64_t)B * N * a.units;
   a.heads_each = 8;
   const int64_t groups = (lanes + 255) / 256;
-  if (groups > 0x7fffffffLL) return fail(RADIAL_ESHAPE, "B*N*D is too large for one launch");
   // few tokens: heads over more lanes, until there are some for every compute unit
   while (a.heads_each > 1 && groups * ((heads + a.heads_each - 1) / a.heads_each) < 1024) a.heads_each /= 2;
   const int32_t parts = (heads + a.heads_each - 1) / a.heads_each;

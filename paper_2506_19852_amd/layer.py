@@ -1,5 +1,5 @@
 """ctypes binding of the operators around the attention (include/radial_layer.h): same names as the C ABI, argument marshalling only.
-Tensors are torch CUDA tensors of the current device (device memory + strides); every step of the computation runs in the library's HIP kernels.
+Tensors are torch CUDA tensors on the current device (others are refused); every step of the computation runs in the library's HIP kernels.
 There is no fallback: a missing library or a failing call raises."""
 from __future__ import annotations
 
@@ -39,11 +39,12 @@ class radial_rope_params(ctypes.Structure):
 _lib = None
 _types = None  # torch dtype -> RADIAL_ type
 _f32 = _bf16 = _u8 = _i32 = None  # torch dtypes, set by load()
+_device = None  # torch.cuda.current_device, set by load()
 
 
 def load():
     """Loads libradial.so and declares the prototypes of radial_layer.h."""
-    global _lib, _types, _f32, _bf16, _u8, _i32
+    global _lib, _types, _f32, _bf16, _u8, _i32, _device
     if _lib is not None:
         return _lib
     lib = binding.load()
@@ -67,6 +68,7 @@ def load():
     torch = _load_torch()
     _types = {torch.bfloat16: RADIAL_BF16, torch.float32: RADIAL_F32}
     _f32, _bf16, _u8, _i32 = torch.float32, torch.bfloat16, torch.uint8, torch.int32
+    _device = torch.cuda.current_device
     _lib = lib
     return lib
 
@@ -76,17 +78,17 @@ def load():
 _NO_ROWS = radial_rows(None, 0, 0, RADIAL_BF16)
 
 
-def _rows(t, name, shape) -> radial_rows:
+def _rows(t, name, shape, device) -> radial_rows:
     if t is None:
         return _NO_ROWS
     stride = t.stride()
     kind = _types.get(t.dtype)
-    if kind is None or not t.is_cuda or t.shape != shape or (stride[2] != 1 and shape[2] > 1):
+    if kind is None or t.get_device() != device or t.shape != shape or (stride[2] != 1 and shape[2] > 1):
         raise ValueError(f"{name} must be a CUDA bf16 or float32 tensor {list(shape)} with unit stride in C")
     return radial_rows(t.data_ptr(), stride[0], stride[1], kind)
 
 
-def _mods(B, G, C, **named):
+def _mods(B, G, C, device, **named):
     """Addresses of the conditioning tensors [B, G, C] that are given, and the elements between their rows: one stride for all of them, across
     batch entries too."""
     shape, found, out = (B, G, C), None, []
@@ -95,7 +97,7 @@ def _mods(B, G, C, **named):
             out.append(None)
             continue
         stride = t.stride()
-        if t.dtype is not _f32 or not t.is_cuda or t.shape != shape or (stride[2] != 1 and C > 1):
+        if t.dtype is not _f32 or t.get_device() != device or t.shape != shape or (stride[2] != 1 and C > 1):
             raise ValueError(f"{name} must be a CUDA float32 tensor {[B, G, C]} with unit stride in C")
         step = stride[1] if G > 1 else stride[0] if B > 1 else C
         if G > 1 and B > 1 and stride[0] != G * step:
@@ -108,15 +110,21 @@ def _mods(B, G, C, **named):
     return out
 
 
+def _bytes(t, name, device):
+    if t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor on the current CUDA device")
+    return t.data_ptr()
+
+
 def _group(group, N) -> int:
     """Tokens that share a row of conditioning: all without `group`, and where it is larger."""
     return N if group is None or group > N else group
 
 
-def _channels(t, name, C):
+def _channels(t, name, C, device):
     if t is None:
         return None
-    if t.dtype is not _f32 or not t.is_cuda or t.shape != (C,) or (C > 1 and t.stride()[0] != 1):
+    if t.dtype is not _f32 or t.get_device() != device or t.shape != (C,) or (C > 1 and t.stride()[0] != 1):
         raise ValueError(f"{name} must be a contiguous CUDA float32 tensor [C]")
     return t.data_ptr()
 
@@ -128,13 +136,13 @@ def radial_norm_fwd(x, r, z, *, y=None, gate=None, post_weight=None, weight=None
     x, r: residual stream [B, N, C]; y, z: branch in and out (bf16 or float32); r None without y, z None with pre = RADIAL_NORM_NONE.
     gate, scale, shift: float32 [B, ceil(N/group), C], a row for every `group` tokens (default: one for all); post_weight, weight: float32 [C]."""
     lib = _lib or load()
-    shape = x.shape
+    shape, device = x.shape, _device()
     B, N, C = shape
     group = _group(group, N)
-    gate, scale, shift, step = _mods(B, -(-N // max(group, 1)), C, gate=gate, scale=scale, shift=shift)
+    gate, scale, shift, step = _mods(B, -(-N // max(group, 1)), C, device, gate=gate, scale=scale, shift=shift)
     p = radial_norm_params(B, N, C, group, post, pre, eps, residual_scale, step, step)
-    _check(lib.radial_norm_fwd(byref(p), _rows(x, "x", shape), _rows(y, "y", shape), gate, _channels(post_weight, "post_weight", C),
-                               _channels(weight, "weight", C), scale, shift, _rows(r, "r", shape), _rows(z, "z", shape), _stream_ptr(stream)))
+    _check(lib.radial_norm_fwd(byref(p), _rows(x, "x", shape, device), _rows(y, "y", shape, device), gate, _channels(post_weight, "post_weight", C, device),
+                               _channels(weight, "weight", C, device), scale, shift, _rows(r, "r", shape, device), _rows(z, "z", shape, device), _stream_ptr(stream)))
 
 
 def radial_norm_bwd_workspace(B: int, N: int, C: int, *, group=None, post=RADIAL_NORM_NONE, pre=RADIAL_NORM_LAYER) -> int:
@@ -149,17 +157,18 @@ def radial_norm_bwd(r, dz, dx, workspace, *, dr=None, y=None, dy=None, gate=None
 
     r: the forward's r (its x without y), not read with pre = RADIAL_NORM_NONE; workspace: CUDA uint8 tensor of radial_norm_bwd_workspace bytes."""
     lib = _lib or load()
-    shape = dx.shape
+    shape, device = dx.shape, _device()
     B, N, C = shape
     group = _group(group, N)
     G = -(-N // max(group, 1))
-    gate, scale, step = _mods(B, G, C, gate=gate, scale=scale)
-    dgate, dscale, dshift, dstep = _mods(B, G, C, dgate=dgate, dscale=dscale, dshift=dshift)
+    gate, scale, step = _mods(B, G, C, device, gate=gate, scale=scale)
+    dgate, dscale, dshift, dstep = _mods(B, G, C, device, dgate=dgate, dscale=dscale, dshift=dshift)
     p = radial_norm_params(B, N, C, group, post, pre, eps, residual_scale, step, dstep)
-    _check(lib.radial_norm_bwd(byref(p), _rows(r, "r", shape), _rows(y, "y", shape), _rows(dz, "dz", shape), _rows(dr, "dr", shape), gate,
-                               _channels(post_weight, "post_weight", C), _channels(weight, "weight", C), scale, _rows(dx, "dx", shape),
-                               _rows(dy, "dy", shape), dgate, dscale, dshift, _channels(dpost_weight, "dpost_weight", C),
-                               _channels(dweight, "dweight", C), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+    _check(lib.radial_norm_bwd(byref(p), _rows(r, "r", shape, device), _rows(y, "y", shape, device), _rows(dz, "dz", shape, device), _rows(dr, "dr", shape, device), gate,
+                               _channels(post_weight, "post_weight", C, device), _channels(weight, "weight", C, device), scale, _rows(dx, "dx", shape, device),
+                               _rows(dy, "dy", shape, device), dgate, dscale, dshift, _channels(dpost_weight, "dpost_weight", C, device),
+                               _channels(dweight, "dweight", C, device), _bytes(workspace, "workspace", device),
+                               workspace.numel() * workspace.element_size(),
                                _stream_ptr(stream)))
 
 
@@ -204,27 +213,27 @@ def radial_rope_table_bytes(params: radial_rope_params) -> int:
 def radial_rope_table(params: radial_rope_params, table, stream=None):
     """table (float32, radial_rope_table_bytes(params) bytes) <- the turns of every position."""
     lib = _lib or load()
-    _check_table(table)
+    _check_table(table, _device())
     _check(lib.radial_rope_table(byref(params), table.data_ptr(), table.numel() * 4, _stream_ptr(stream)))
 
 
-def _check_table(table):
-    if table.dtype is not _f32 or not table.is_cuda or not table.is_contiguous():
+def _check_table(table, device):
+    if table.dtype is not _f32 or table.get_device() != device or not table.is_contiguous():
         raise ValueError("table must be a contiguous CUDA float32 tensor")
 
 
 _NO_HEADS = radial_tensor(None, 0, 0, 0)
 
 
-def _heads(t, name, shape, dtype) -> radial_tensor:
+def _heads(t, name, shape, dtype, device) -> radial_tensor:
     stride = t.stride()
-    if t.dtype is not dtype or not t.is_cuda or t.shape != shape or stride[3] != 1:
+    if t.dtype is not dtype or t.get_device() != device or t.shape != shape or stride[3] != 1:
         raise ValueError(f"{name} must be a CUDA tensor {list(shape)} of q's type with unit stride in D")
     return radial_tensor(t.data_ptr(), stride[0], stride[1], stride[2])
 
 
 def _rope(call, names, params, table, q, q_out, k, k_out, positions, first, stream):
-    shape = q.shape
+    shape, device = q.shape, _device()
     B, q_heads, N, D = shape
     dtype = q.dtype
     kind = _types.get(dtype)
@@ -238,17 +247,17 @@ def _rope(call, names, params, table, q, q_out, k, k_out, positions, first, stre
         k_heads = k_shape[1]
         if k_shape != shape and k_shape != (B, k_heads, N, D):
             raise ValueError(f"{names[2]} must have {names[0]}'s shape but for the heads")
-        k_in, k_to = _heads(k, names[2], k_shape, dtype), _heads(k_out, names[3], k_shape, dtype)
+        k_in, k_to = _heads(k, names[2], k_shape, dtype, device), _heads(k_out, names[3], k_shape, dtype, device)
     at = None
     if positions is not None:
-        if positions.dtype is not _i32 or not positions.is_cuda or not positions.is_contiguous() or positions.shape != (B, N):
+        if positions.dtype is not _i32 or positions.get_device() != device or not positions.is_contiguous() or positions.shape != (B, N):
             raise ValueError("positions must be a contiguous CUDA int32 tensor [B, N]")
         at = positions.data_ptr()
     elif first >= 1 << 31:
         raise ValueError("first must be below 2^31")
-    _check_table(table)
-    _check(call(byref(params), table.data_ptr(), table.numel() * 4, B, N, D, q_heads, _heads(q, names[0], shape, dtype),
-                _heads(q_out, names[1], shape, dtype), k_heads, k_in, k_to, kind, at, first, _stream_ptr(stream)))
+    _check_table(table, device)
+    _check(call(byref(params), table.data_ptr(), table.numel() * 4, B, N, D, q_heads, _heads(q, names[0], shape, dtype, device),
+                _heads(q_out, names[1], shape, dtype, device), k_heads, k_in, k_to, kind, at, first, _stream_ptr(stream)))
 
 
 def radial_rope_fwd(params: radial_rope_params, table, q, q_out, k=None, k_out=None, positions=None, first: int = 0, stream=None):
@@ -265,13 +274,13 @@ def radial_rope_bwd(params: radial_rope_params, table, dq_out, dq, dk_out=None, 
 
 # ---- products in 8-bit floating point -----------------------------------------------------------
 
-def _codes(codes, scales, name, rows, cols, scale_rows):
+def _codes(codes, scales, name, rows, cols, scale_rows, device):
     if codes is None and scales is None:
         return None, None
     groups = -(-cols // 128)
-    if codes is None or codes.dtype is not _u8 or not codes.is_cuda or not codes.is_contiguous() or codes.shape != (rows, groups * 128):
+    if codes is None or codes.dtype is not _u8 or codes.get_device() != device or not codes.is_contiguous() or codes.shape != (rows, groups * 128):
         raise ValueError(f"{name}codes must be a contiguous CUDA uint8 tensor {[rows, groups * 128]}")
-    if scales is None or scales.dtype is not _f32 or not scales.is_cuda or not scales.is_contiguous() or scales.shape != (groups, scale_rows):
+    if scales is None or scales.dtype is not _f32 or scales.get_device() != device or not scales.is_contiguous() or scales.shape != (groups, scale_rows):
         raise ValueError(f"{name}scales must be a contiguous CUDA float32 tensor {[groups, scale_rows]}")
     return codes.data_ptr(), scales.data_ptr()
 
@@ -282,13 +291,13 @@ def radial_quantize_groups_fp8(x, codes=None, scales=None, codes_t=None, scales_
     codes [rows, P], scales [P/128, rows] with P = cols rounded up to 128; codes_t [cols, Pt], scales_t [Pt/128, cols] likewise with rows.
     grouping = RADIAL_BLOCKS: one scale for 128 x 128, scales [P/128, ceil(rows/128)] and scales_t [Pt/128, ceil(cols/128)]."""
     lib = _lib or load()
-    kind, shape, stride = _types.get(x.dtype), x.shape, x.stride()
-    if kind is None or not x.is_cuda or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+    kind, shape, stride, device = _types.get(x.dtype), x.shape, x.stride(), _device()
+    if kind is None or x.get_device() != device or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError("x must be a CUDA bf16 or float32 tensor [rows, cols] with unit stride in cols")
     rows, cols = shape
     blocks = grouping == RADIAL_BLOCKS
-    c, s = _codes(codes, scales, "", rows, cols, -(-rows // 128) if blocks else rows)
-    ct, st = _codes(codes_t, scales_t, "transposed ", cols, rows, -(-cols // 128) if blocks else cols)
+    c, s = _codes(codes, scales, "", rows, cols, -(-rows // 128) if blocks else rows, device)
+    ct, st = _codes(codes_t, scales_t, "transposed ", cols, rows, -(-cols // 128) if blocks else cols, device)
     step = stride[0] if rows > 1 else max(cols, stride[0])
     _check(lib.radial_quantize_groups_fp8(rows, cols, x.data_ptr(), kind, step, grouping, c, s, ct, st, _stream_ptr(stream)))
 
@@ -296,13 +305,13 @@ def radial_quantize_groups_fp8(x, codes=None, scales=None, codes_t=None, scales_
 def radial_product_fp8(a_codes, a_scales, b_codes, b_scales, out, stream=None):
     """out [M, N] (bf16) <- A B^T from the codes and scales of A [M, K] (groups) and B [N, K] (groups or blocks, by b_scales' shape)."""
     lib = _lib or load()
-    shape, stride = out.shape, out.stride()
-    if out.dtype is not _bf16 or not out.is_cuda or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+    shape, stride, device = out.shape, out.stride(), _device()
+    if out.dtype is not _bf16 or out.get_device() != device or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError("out must be a CUDA bf16 tensor [M, N] with unit stride in N")
     M, N = shape
     K = a_codes.shape[-1]
-    a, sa = _codes(a_codes, a_scales, "a_", M, K, M)
+    a, sa = _codes(a_codes, a_scales, "a_", M, K, M, device)
     blocks = b_scales.shape[-1] != N
-    b, sb = _codes(b_codes, b_scales, "b_", N, K, -(-N // 128) if blocks else N)
+    b, sb = _codes(b_codes, b_scales, "b_", N, K, -(-N // 128) if blocks else N, device)
     step = stride[0] if M > 1 else max(N, stride[0])
     _check(lib.radial_product_fp8(M, N, K, a, sa, b, sb, RADIAL_BLOCKS if blocks else RADIAL_GROUPS, out.data_ptr(), step, _stream_ptr(stream)))

@@ -184,3 +184,17 @@ def test_captured_and_replayed():
             graph.replay()
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(L.results(), want)), turn
+
+
+def test_the_benchmark_times_a_layer(capsys):
+    import json
+    import os
+    import sys
+    import types
+    sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    import bench
+    from paper_2506_19852_amd import workloads as wl
+    bench.layer_times(wl.WORKLOADS["cfg1_tiny"], types.SimpleNamespace(warmup=1, steps=2))
+    line = json.loads(capsys.readouterr().out.strip().split("\n")[-1])
+    assert line["unit"] == "ms" and line["steps"] == 2 and len(line["ms"]) == 8 and all(t > 0 for t in line["ms"].values())
+    assert line["value"] == pytest.approx(sum(line["ms"].values()), rel=1e-2)

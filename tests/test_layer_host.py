@@ -119,6 +119,10 @@ def test_norm_parts_that_do_not_go_together():
     _refused(_norm("bwd", workspace=AT + 64), ESHAPE, "256-byte")
     need = rl.radial_norm_bwd_workspace(2, 8, 64, group=4, post=2, pre=1)
     _refused(_norm("bwd", bytes=need - 1), ESHAPE, "needed")
+    many = dict(B=1 << 10, N=1 << 20, C=4096, group=1, mod_stride=4096, dmod_stride=4096)   # a workgroup of 512 threads for each token: beyond a launch
+    wide = {k: rl.radial_rows(AT, 4096 << 20, 4096, BF16) for k in ("x", "y", "r", "z", "dz", "dr", "dx", "dy")}
+    _refused(_norm("fwd", many, **wide), ESHAPE, "too many groups")
+    _refused(_norm("bwd", many, **wide), ESHAPE, "too many groups")
     assert rl.radial_norm_bwd_workspace(2, 8, 64, group=1 << 31) == rl.radial_norm_bwd_workspace(2, 8, 64)
 
 
@@ -170,7 +174,7 @@ def _heads(ptr=AT, sb=4096, sh=128, sn=512):
     (dict(D=56), ESHAPE, "turn 64"), (dict(q=_heads(None)), EINVAL, "ptr is NULL"), (dict(q_out=_heads(AT + 8)), ESHAPE, "16-byte"), (dict(q=_heads(sn=56)), ESHAPE, "strides"),
     (dict(q=_heads(sn=516)), ESHAPE, "strides"), (dict(k=_heads(sh=-8)), ESHAPE, "strides"), (dict(k=_heads(None)), EINVAL, "ptr is NULL"),
     (dict(k_out=_heads(None)), EINVAL, "ptr is NULL"), (dict(k_heads=0), EINVAL, "k_heads"), (dict(k_heads=-1), EINVAL, "k_heads"), (dict(first=-1), EINVAL, "first"),
-    (dict(positions=AT + 2), ESHAPE, "positions"),
+    (dict(positions=AT + 2), ESHAPE, "positions"), (dict(B=1 << 20, N=1 << 20), ESHAPE, "too large"),
 ], ids=lambda v: str(list(v.items())[0][0]) if isinstance(v, dict) else str(v))
 def test_rope_arguments(change, code, text):
     for direction in ("fwd", "bwd"):
@@ -209,7 +213,7 @@ def test_quantise_arguments(change, code, text):
     (dict(M=0), EINVAL, ">= 1"), (dict(N=0), EINVAL, ">= 1"), (dict(K=-5), EINVAL, ">= 1"), (dict(a=None), EINVAL, "NULL"), (dict(sa=None), EINVAL, "NULL"),
     (dict(b=None), EINVAL, "NULL"), (dict(sb=None), EINVAL, "NULL"), (dict(out=None), EINVAL, "NULL"), (dict(grouping=3), EINVAL, "b_grouping"), (dict(a=AT + 8), ESHAPE, "codes"),
     (dict(b=AT + 4), ESHAPE, "codes"), (dict(sb=AT + 2), ESHAPE, "scales"), (dict(out=AT + 1), ESHAPE, "out"), (dict(stride=9), ESHAPE, "out_stride"),
-    (dict(K=0x7fffffff), ESHAPE, "too large"),
+    (dict(K=0x7fffffff), ESHAPE, "too large"), (dict(M=(1 << 29) + 1), ESHAPE, "too large"), (dict(M=1 << 29, N=1 << 29, stride=1 << 29), ESHAPE, "too large"),
 ], ids=str)
 def test_product_arguments(change, code, text):
     a = dict(M=10, N=10, K=100, a=AT, sa=AT, b=AT, sb=AT, grouping=0, out=AT, stride=10)
@@ -219,14 +223,21 @@ def test_product_arguments(change, code, text):
 
 # ---- marshalling --------------------------------------------------------------------------------
 
-def _fake(dtype, *shape):
+@pytest.fixture
+def one_device(monkeypatch):
+    rl.load()
+    monkeypatch.setattr(rl, "_device", lambda: 0)
+
+
+def _fake(dtype, *shape, device=0):
     t = FakeTensor(dtype, *shape)
+    t.get_device = lambda: device
     full = t.stride()
     t.stride = lambda i=None: full if i is None else full[i]
     return t
 
 
-def test_shapes_and_types_are_checked_before_the_library_is_entered():
+def test_shapes_and_types_are_checked_before_the_library_is_entered(one_device):
     bf16, f32, u8, i32 = torch.bfloat16, torch.float32, torch.uint8, torch.int32
     x = _fake(bf16, 2, 8, 64)
     for bad in (dict(x=_fake(torch.float16, 2, 8, 64), r=None, z=x), dict(x=x, r=None, z=_fake(bf16, 2, 8, 32)), dict(x=x, r=None, z=x, weight=_fake(bf16, 64)),
@@ -257,6 +268,35 @@ def test_shapes_and_types_are_checked_before_the_library_is_entered():
     for bad in ((codes, scales, b, sb, _fake(f32, 100, 300)), (codes, scales, b, sb, _fake(bf16, 99, 300)), (codes, scales, _fake(u8, 300, 128), sb, out), (codes, scales, b, _fake(f32, 2, 4), out)):
         with pytest.raises(ValueError):
             rl.radial_product_fp8(*bad, stream=1)
+
+
+def test_tensors_of_another_device_or_of_none_are_refused(one_device):
+    bf16, f32, u8, i32 = torch.bfloat16, torch.float32, torch.uint8, torch.int32
+    for other in (1, -1):
+        x, there = _fake(bf16, 2, 8, 64), _fake(bf16, 2, 8, 64, device=other)
+        mod = _fake(f32, 2, 1, 64, device=other)
+        for bad in (dict(x=there, r=None, z=x), dict(x=x, r=None, z=there), dict(x=x, r=None, z=x, scale=mod), dict(x=x, r=None, z=x, weight=_fake(f32, 64, device=other)),
+                    dict(x=x, r=there, z=x, y=x)):
+            with pytest.raises(ValueError):
+                rl.radial_norm_fwd(**bad, stream=1)
+        for bad in (dict(dz=there), dict(dx=there), dict(workspace=_fake(u8, 1 << 20, device=other)), dict(dscale=mod)):
+            with pytest.raises(ValueError):
+                rl.radial_norm_bwd(**{**dict(r=x, dz=x, dx=x, workspace=_fake(u8, 1 << 20)), **bad}, stream=1)
+        p, q, table = rl.rope_params([8], [64]), _fake(bf16, 1, 2, 8, 64), _fake(f32, 512)
+        q_there = _fake(bf16, 1, 2, 8, 64, device=other)
+        for bad in (dict(q=q_there), dict(q_out=q_there), dict(k=q, k_out=q_there), dict(table=_fake(f32, 512, device=other)), dict(positions=_fake(i32, 1, 8, device=other))):
+            with pytest.raises(ValueError):
+                rl.radial_rope_bwd(p, **{"dq_out" if k == "q" else "dq" if k == "q_out" else "dk_out" if k == "k" else "dk" if k == "k_out" else k: v
+                                         for k, v in {**dict(q=q, q_out=q, table=table), **bad}.items()}, stream=1)
+        m, codes, scales = _fake(bf16, 100, 200), _fake(u8, 100, 256), _fake(f32, 2, 100)
+        for bad in ((_fake(bf16, 100, 200, device=other), codes, scales), (m, _fake(u8, 100, 256, device=other), scales), (m, codes, _fake(f32, 2, 100, device=other))):
+            with pytest.raises(ValueError):
+                rl.radial_quantize_groups_fp8(*bad, stream=1)
+        for i in range(5):
+            args = [codes, scales, _fake(u8, 300, 256), _fake(f32, 2, 300), _fake(bf16, 100, 300)]
+            args[i] = _fake(args[i].dtype, *args[i].shape, device=other)
+            with pytest.raises(ValueError):
+                rl.radial_product_fp8(*args, stream=1)
 
 
 def test_numpy_numbers_and_defaults():
