@@ -506,72 +506,73 @@ struct GradArgs {
   int64_t mod_stride, dmod_stride;
 };
 
-constexpr int kGradColumns = 16, kGradSlices = 64;
+constexpr int kGradColumns = 16, kGradSlices = 64;  // a wave: 16 channels, four slices
+constexpr int kFewGroups = 4;
 constexpr int64_t kMostInY = 65535;
 
-// The slices' sums of a column, in order.
-__device__ __forceinline__ float over_slices(const float (&sums)[kGradSlices][kGradColumns + 1], int column) {
-  float s = 0.f;
-#pragma unroll 16
-  for (int i = 0; i < kGradSlices; ++i) s += sums[i][column];
-  return s;
+// The sum over a wave's four slices, in all of them.
+__device__ __forceinline__ float over_four(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
 }
 
-// 16 channels of a group: 64 slices of its workgroups' sums each, then the slices' sums.  (64 channels and 16 slices: 30 us of a small call.)
-// total: P, T, Q of the channel in slices 0, 1, 2, where they are wanted (true).
-__device__ __forceinline__ bool sums_of_group(const GradArgs& a, int64_t group, float (&sums)[3][kGradSlices][kGradColumns + 1], int32_t c, float& total) {
+// 16 channels of a group (kFew: of up to four groups, each with its share of the slices): 64 slices of its workgroups' sums each, then the slices' sums.
+// (64 channels and 16 slices: 30 us of a small call.)  With few groups the gradients of the weights come along, instead of from another launch.
+template <bool kFew>
+__global__ void __launch_bounds__(kGradColumns * kGradSlices) norm_grad_kernel(GradArgs a) {
+  __shared__ float sums[3][kGradSlices / 4][kGradColumns], of_groups[3][kFewGroups][kGradColumns];
   const int32_t lane = threadIdx.x, slice = threadIdx.y;
+  const int32_t c = blockIdx.x * kGradColumns + lane;
+  const int32_t slices = !kFew || a.groups == 1 ? kGradSlices : a.groups == 2 ? kGradSlices / 2 : kGradSlices / 4;  // of a group
+  const int64_t group = kFew ? slice / slices : blockIdx.y + (int64_t)blockIdx.z * kMostInY;
+  if (!kFew && group >= a.groups) return;
   float sum[3] = {0.f, 0.f, 0.f};
-  if (c < a.C) {
-#pragma unroll 4
-    for (int32_t i = slice; i < a.chunks; i += kGradSlices) {
-      const float* p = a.partial + (group * a.chunks + i) * 3 * a.C + c;
+  if (c < a.C && group < a.groups) {
+    const float* p = a.partial + group * a.chunks * 3 * a.C + c;
+    const int64_t step = 3 * (int64_t)a.C;
 #pragma unroll
-      for (int k = 0; k < 3; ++k)
-        if (a.wants >> k & 1) sum[k] += p[(int64_t)k * a.C];
+    for (int k = 0; k < 3; ++k, p += a.C) {
+      if (!(a.wants >> k & 1)) continue;
+#pragma unroll 8
+      for (int32_t i = slice % slices; i < a.chunks; i += slices) sum[k] += p[i * step];
     }
   }
 #pragma unroll
-  for (int k = 0; k < 3; ++k) sums[k][slice][lane] = sum[k];
-  __syncthreads();
-  if (slice >= 3 || c >= a.C || !(a.wants >> slice & 1)) return false;
-  total = over_slices(sums[slice], lane);
-  const int64_t mod = group * a.dmod_stride + c;
-  if (slice == 0 && a.dscale) a.dscale[mod] = a.weight ? total * a.weight[c] : total;
-  if (slice == 1) a.dshift[mod] = total;
-  if (slice == 2 && a.dgate) a.dgate[mod] = a.post_weight ? total * a.post_weight[c] : total;
-  return true;
-}
-
-__global__ void __launch_bounds__(kGradColumns * kGradSlices) norm_grad_kernel(GradArgs a) {
-  __shared__ float sums[3][kGradSlices][kGradColumns + 1];
-  const int32_t c = blockIdx.x * kGradColumns + threadIdx.x;
-  const int64_t group = blockIdx.y + (int64_t)blockIdx.z * kMostInY;
-  if (group >= a.groups) return;
-  float total;
-  if (sums_of_group(a, group, sums, c, total) && a.of_group && threadIdx.y != 1) a.of_group[(group * 2 + (threadIdx.y == 2)) * a.C + c] = total;
-}
-
-// The same, and the gradients of the weights, where there are few groups: a workgroup takes all of them.
-__global__ void __launch_bounds__(kGradColumns * kGradSlices) norm_few_groups_kernel(GradArgs a) {
-  __shared__ float sums[3][kGradSlices][kGradColumns + 1];
-  const int32_t c = blockIdx.x * kGradColumns + threadIdx.x, slice = threadIdx.y;
-  float of_weight = 0.f;  // slice 0: dw, slice 2: dw_post
-  for (int64_t group = 0; group < a.groups; ++group) {
-    if (group) __syncthreads();
-    float total;
-    if (!sums_of_group(a, group, sums, c, total)) continue;
-    if (slice == 0) of_weight += a.scale ? total * (1.f + a.scale[group * a.mod_stride + c]) : total;
-    if (slice == 2) of_weight += a.gate ? total * a.gate[group * a.mod_stride + c] : total;
+  for (int k = 0; k < 3; ++k) {
+    sum[k] = over_four(sum[k]);
+    if (slice % 4 == k) sums[k][slice / 4][lane] = sum[k];
   }
-  if (c >= a.C) return;
-  if (slice == 0 && a.dweight) a.dweight[c] = of_weight;
-  if (slice == 2 && a.dpost_weight) a.dpost_weight[c] = of_weight;
+  __syncthreads();
+  // slice k (few groups: k of each group's slices) adds up P, T or Q
+  const int32_t k = slice % slices;
+  const bool adds = k < 3 && c < a.C && group < a.groups && (a.wants >> k & 1);
+  if (adds) {
+    float total = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < slices / 4; ++i) total += sums[k][slice / slices * (slices / 4) + i][lane];
+    const int64_t mod = group * a.dmod_stride + c;
+    if (k == 0 && a.dscale) a.dscale[mod] = a.weight ? total * a.weight[c] : total;
+    if (k == 1) a.dshift[mod] = total;
+    if (k == 2 && a.dgate) a.dgate[mod] = a.post_weight ? total * a.post_weight[c] : total;
+    if (!kFew && a.of_group && k != 1) a.of_group[(group * 2 + (k == 2)) * a.C + c] = total;
+    if (kFew) {
+      if (k == 0 && a.scale) total *= 1.f + a.scale[group * a.mod_stride + c];
+      if (k == 2 && a.gate) total *= a.gate[group * a.mod_stride + c];
+      of_groups[k][group][lane] = total;
+    }
+  }
+  if (!kFew) return;
+  __syncthreads();
+  if (slice > 2 || !(a.wants >> slice & 1) || c >= a.C) return;
+  float total = 0.f;
+  for (int g = 0; g < a.groups; ++g) total += of_groups[slice][g][lane];
+  if (slice == 0 && a.dweight) a.dweight[c] = total;
+  if (slice == 2 && a.dpost_weight) a.dpost_weight[c] = total;
 }
 
 // dw and dw_post: sums over the groups, each times its conditioning.
 __global__ void __launch_bounds__(kGradColumns * kGradSlices) norm_weight_grad_kernel(GradArgs a) {
-  __shared__ float sums[2][kGradSlices][kGradColumns + 1];
+  __shared__ float sums[2][kGradSlices / 4][kGradColumns];
   const int32_t lane = threadIdx.x, slice = threadIdx.y;
   const int32_t c = blockIdx.x * kGradColumns + lane;
   float dw = 0.f, dw_post = 0.f;
@@ -581,12 +582,17 @@ __global__ void __launch_bounds__(kGradColumns * kGradSlices) norm_weight_grad_k
       if (a.dpost_weight) dw_post += a.of_group[(g * 2 + 1) * a.C + c] * (a.gate ? a.gate[g * a.mod_stride + c] : 1.f);
     }
   }
-  sums[0][slice][lane] = dw;
-  sums[1][slice][lane] = dw_post;
+  dw = over_four(dw);
+  dw_post = over_four(dw_post);
+  if (slice % 4 == 0) sums[0][slice / 4][lane] = dw;
+  if (slice % 4 == 1) sums[1][slice / 4][lane] = dw_post;
   __syncthreads();
-  if (c >= a.C) return;
-  if (slice == 0 && a.dweight) a.dweight[c] = over_slices(sums[0], lane);
-  if (slice == 1 && a.dpost_weight) a.dpost_weight[c] = over_slices(sums[1], lane);
+  if (slice > 1 || c >= a.C) return;
+  float total = 0.f;
+#pragma unroll
+  for (int i = 0; i < kGradSlices / 4; ++i) total += sums[slice][i][lane];
+  if (slice == 0 && a.dweight) a.dweight[c] = total;
+  if (slice == 1 && a.dpost_weight) a.dpost_weight[c] = total;
 }
 
 // ---- launches -----------------------------------------------------------------------------------
@@ -603,8 +609,9 @@ constexpr int32_t kNarrow = 512;  // channels up to which a row is a wave's or l
 // Channels of a thread of a wide team, in eights.
 int eights_of(int32_t C) { return C <= 4096 ? 1 : C <= 8192 ? 2 : 4; }
 
-// `rounds` times the workgroups that run at a time, by the waves that fit a compute unit, shared out over the groups; a workgroup has at least
-// `least` rows for each of its teams, since each loads the conditioning and, backward, writes its sums.
+// `rounds` times the workgroups that run at a time, by the waves that fit a compute unit, shared out over the groups; a workgroup has `least` rows or
+// more for each of its teams, since each loads the conditioning and, backward, writes its sums, but for fewer than 256 teams' worth of rows, where
+// what counts is how many rows come one after the other.
 Layout make_layout(const radial_norm_params& p, int32_t waves_of_unit, int32_t rounds, int32_t least) {
   Layout l;
   l.groups_of_batch = (int32_t)(((int64_t)p.N + p.group - 1) / p.group);
@@ -615,6 +622,8 @@ Layout make_layout(const radial_norm_params& p, int32_t waves_of_unit, int32_t r
   const int32_t teams = p.C <= 128 ? 16 : p.C <= 256 ? 8 : p.C <= kNarrow ? 4 : 1;
   const int64_t workgroups = (int64_t)256 * rounds * (waves_of_unit > waves ? waves_of_unit / waves : 1);
   int64_t chunks = workgroups / l.groups;
+  const int64_t rows_of_team = ((int64_t)p.B * p.N / teams + 255) / 256;
+  if (rows_of_team < least) least = rows_of_team < 1 ? 1 : (int32_t)rows_of_team;
   const int64_t most = ((int64_t)of_group + least * teams - 1) / (least * teams);
   if (chunks > most) chunks = most;
   if (chunks < 1) chunks = 1;
@@ -830,7 +839,6 @@ extern "C" int radial_norm_bwd(const radial_norm_params* params, radial_rows r, 
 
   GradArgs g = {};
   g.partial = a.partial;
-  constexpr int64_t kFewGroups = 4;
   const bool weights = dweight || dpost_weight, few = weights && l.groups <= kFewGroups;
   g.of_group = weights && !few ? a.partial + (size_t)l.groups * l.chunks * 3 * p.C : nullptr;
   g.gate = gate; g.post_weight = post_weight; g.weight = weight; g.scale = scale;
@@ -840,8 +848,8 @@ extern "C" int radial_norm_bwd(const radial_norm_params* params, radial_rows r, 
   const unsigned columns = (unsigned)((p.C + kGradColumns - 1) / kGradColumns);
   const dim3 block(kGradColumns, kGradSlices);
   const unsigned in_y = (unsigned)(l.groups < kMostInY ? l.groups : kMostInY), in_z = (unsigned)((l.groups + kMostInY - 1) / kMostInY);
-  if (few) norm_few_groups_kernel<<<dim3(columns), block, 0, (hipStream_t)hip_stream>>>(g);
-  else norm_grad_kernel<<<dim3(columns, in_y, in_z), block, 0, (hipStream_t)hip_stream>>>(g);
+  if (few) norm_grad_kernel<true><<<dim3(columns), block, 0, (hipStream_t)hip_stream>>>(g);
+  else norm_grad_kernel<false><<<dim3(columns, in_y, in_z), block, 0, (hipStream_t)hip_stream>>>(g);
   RADIAL_HIP_TRY(hipGetLastError());
   if (g.of_group) {
     norm_weight_grad_kernel<<<dim3(columns), block, 0, (hipStream_t)hip_stream>>>(g);
