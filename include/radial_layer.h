@@ -119,8 +119,9 @@ typedef struct {
  * magnitude * cos and magnitude * sin. */
 RADIAL_API size_t radial_rope_table_bytes(const radial_rope_params* params);
 
-/* Fills the table (device, 16-byte aligned, table_bytes of at least radial_rope_table_bytes) for the calls below, which only read it.  Angles are computed in 64 bits and reduced before
- * they are rounded, so that far positions are as exact as near ones. */
+/* Fills the table (device, 16-byte aligned, table_bytes of at least radial_rope_table_bytes) for the calls below, which
+ * only read it.  Angles are computed in 64 bits and reduced before they are rounded, so that far positions are as exact as
+ * near ones. */
 RADIAL_API int radial_rope_table(const radial_rope_params* params, float* table, size_t table_bytes, void* hip_stream);
 
 /* q_out, k_out <- q, k turned to their positions; both in one launch.
@@ -147,8 +148,9 @@ RADIAL_API int radial_rope_bwd(const radial_rope_params* params, const float* ta
  * or for each block of 128 x 128:
  *   codes  [rows, P], P = columns rounded up to 128, zero beyond the columns; 16-byte aligned;
  *   scales [P/128, rows] for groups, [P/128, ceil(rows/128)] for blocks: the rows are the fast axis.
- * scale = max(amax/448, 2^-126) in float32, codes = E4M3(x/scale, as a float32 value), ties to even.  A NaN has the code of NaN and does not enter its
- * group's amax; with an infinity the scale is infinite and every product that reads the group is NaN. */
+ * scale = max(amax/448, 2^-126) in float32, codes = E4M3(x/scale, as a float32 value), ties to even.  A NaN has the code of
+ * NaN and does not enter its group's amax; with an infinity the scale is infinite and every product that reads the group is
+ * NaN. */
 
 #define RADIAL_GROUPS 0 /* a scale for each 128 columns of a row (activations, gradients) */
 #define RADIAL_BLOCKS 1 /* a scale for each 128 x 128 block (weights)                     */

@@ -11,7 +11,8 @@
 // A team of lanes takes a row: 16, 32 or 64 lanes with eight channels each up to 512 channels, from there all waves of the workgroup.  A thread
 // has the same channels in all rows of its workgroup, so that it loads the conditioning row once and keeps the sums over tokens in registers; a
 // workgroup's rows are of one group.  The backward writes a workgroup's sums to the workspace, where a second kernel adds them up
-// in a fixed order (no atomics).
+// in a fixed order (no atomics).  32 760 x 5120 in bf16, residual and layer norm: forward 252 us (5.3 TB/s, what a large copy reaches), backward
+// 408 us (4.9 TB/s), with a second norm 261 and 418.
 #include <float.h>
 #include <math.h>
 
@@ -139,7 +140,7 @@ __device__ __forceinline__ void load_mod(float (&out)[8 * V], const float* row, 
 
 // Rows of a team and its sums.  kWide: the team is the workgroup; otherwise L lanes.  kFast: fewer instructions and waits for more registers (what the
 // waves left is read at once, channels are masked an eight at a time): the gradients at 5120 channels, where only eight waves fit a compute unit
-// anyway, take 443 us instead of 482; the forward, which loses a wave of four by it, 276 instead of 256, the gradients at 1536 channels 175 instead of 154.
+// anyway, took 443 us instead of 482; the forward, which loses a wave of four by it, 276 instead of 256, the gradients at 1536 channels 175 instead of 154.
 template <bool kWide, int L, bool kFast>
 struct Team {
   static constexpr bool kExchanges = kWide, kEights = kFast;
@@ -517,7 +518,7 @@ __device__ __forceinline__ float over_four(float x) {
 }
 
 // 16 channels of a group (kFew: of up to four groups, each with its share of the slices): 64 slices of its workgroups' sums each, then the slices' sums.
-// (64 channels and 16 slices: 30 us of a small call.)  With few groups the gradients of the weights come along, instead of from another launch.
+// (With 64 channels and 16 slices the gradients of 2 x 1237 x 1000 took 41 us instead of 26.)  With few groups the gradients of the weights come along, instead of from another launch.
 template <bool kFew>
 __global__ void __launch_bounds__(kGradColumns * kGradSlices) norm_grad_kernel(GradArgs a) {
   __shared__ float sums[3][kGradSlices / 4][kGradColumns], of_groups[3][kFewGroups][kGradColumns];

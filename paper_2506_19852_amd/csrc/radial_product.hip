@@ -31,7 +31,7 @@ struct QuantArgs {
 };
 
 // x / scale as float32: the product with the inverse, and what it leaves, once more; off by half a unit and 2^-46 of the value.  (A division
-// proper takes three times the instructions, twice per element.)  Infinite scales give NaN.
+// proper takes some ten instructions.)  Infinite scales give NaN.
 struct Quotient {
   float scale, inverse;
   __device__ __forceinline__ explicit Quotient(float amax) {
@@ -229,7 +229,7 @@ __device__ __forceinline__ f32x4 product16(i32x8 a, i32x8 b) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);  // formats 0: E4M3; no block exponents
 }
 
-// Up to 16 rows: bound by reading B (2 x 30 720 x 5120: 27.7 us, 5.7 TB/s; 2 x 5120 x 5120: 8.8 us, of which the launch is half).  A workgroup of
+// Up to 16 rows: bound by reading B (2 x 30 720 x 5120: 27.7 us, 5.7 TB/s; 2 x 5120 x 5120: 8.7 us, 3 TB/s, five groups a wave).  A workgroup of
 // 8 waves takes 16 columns of C, each wave every 8th group, straight from memory (a lane's 32 bytes of a row, four lanes a line); the parts meet in
 // LDS.  Four groups of a wave at a time, or 16 waves, were slower by 0.7 us and more.
 constexpr int kParts = 8;
@@ -266,8 +266,12 @@ __global__ void __launch_bounds__(64 * kParts) product_rows_kernel(ProductArgs a
 }
 
 // Many rows: a workgroup takes a tile of 16 kMTiles kWavesM x 64 kWavesN, stage by stage of one group (128 bytes of every row), which copies put into
-// LDS one stage ahead, straight from memory; a wave takes 16 kMTiles rows of 64 columns.  It holds the four fragments of its columns
-// and walks the fragments of its rows: four matrix instructions each, whose sums are scaled and added while the next ones run.
+// LDS kStages - 1 stages ahead, straight from memory; a wave takes 16 kMTiles rows of 64 columns.  It holds the four fragments of its columns
+// and walks the fragments of its rows: four matrix instructions each, whose sums are scaled and added while the next ones run.  kSplit parts of the
+// workgroup's waves take the groups in turn and add up their sums at the end.
+// 256 x 256 tiles, eight waves, two a SIMD: 32 760 x 5120 x 5120 with blocks 753-815 us (2.1-2.3 PFLOP/s, the chip's clock drops to 1.7-1.8 GHz: what
+// bounds it is the power), 8192^3 427 us (2.6).  With groups on both sides, one product more per sum, 824-915 us.  32 x 32 x 64 matrix instructions, half
+// the operand reads, were 14 % slower (their two halves of a group depend on each other), workgroups that stay and fetch the next tile's first stage early 2 %.
 template <int kWavesM, int kWavesN, int kMTiles, int kStages, int kSplit>
 struct TileShape {
   static constexpr int kWaves = kWavesM * kWavesN;  // of one part of the groups
@@ -414,6 +418,7 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) product_tile_
         next = fragment(at_a, (i + 1) * 16 * kGroup);
         next_factor = a_scales[(i + 1) * 16];
       }
+      // copies in the first half of a stage (spread over all of it the last ones came late: 867 instead of 838 us; all in the first quarter: 908)
       if (copies && i < kMTiles) {
 #pragma unroll
         for (int c = 2 * i * S::kCopies / kMTiles; c < 2 * (i + 1) * S::kCopies / kMTiles && c < S::kCopies; ++c) copy_codes(j + S::kAhead, free, c, lanes, copies == 1);
@@ -473,7 +478,7 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) product_tile_
         for (int t = 0; t < 4; ++t) sum[i][t] += *place(from_part, i, t);
   }
   // Rows that are not 16-byte aligned go through LDS, 16 at a time, to be stored a row of 64 columns at once (straight from the sums a store would
-  // touch 64 places: 1237 x 1961 x 1000 took 18.3 us instead of 13.6).
+  // touch 64 places: 1237 x 1961 x 1000 took 18.4 us instead of 12.8).
   if (!a.vec) __syncthreads();  // everyone is done with the stages, and with the parts' sums
   constexpr int kPitch = 144;
   char* turn = lds + wave * 16 * kPitch;
@@ -542,6 +547,7 @@ int launch_form(int form, const ProductArgs& a, hipStream_t stream) {
 template <bool kBlocks>
 int launch_product(const ProductArgs& a, hipStream_t stream) {
   if (a.M <= 16) {
+    if ((a.N + 15) / 16 > kMostThreads / (64 * kParts)) return fail(RADIAL_ESHAPE, "N is too large for one launch");
     product_rows_kernel<kBlocks><<<dim3((unsigned)((a.N + 15) / 16)), dim3(64 * kParts), 0, stream>>>(a);
     RADIAL_HIP_TRY(hipGetLastError());
     return RADIAL_OK;

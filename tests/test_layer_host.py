@@ -213,7 +213,7 @@ def test_quantise_arguments(change, code, text):
     (dict(M=0), EINVAL, ">= 1"), (dict(N=0), EINVAL, ">= 1"), (dict(K=-5), EINVAL, ">= 1"), (dict(a=None), EINVAL, "NULL"), (dict(sa=None), EINVAL, "NULL"),
     (dict(b=None), EINVAL, "NULL"), (dict(sb=None), EINVAL, "NULL"), (dict(out=None), EINVAL, "NULL"), (dict(grouping=3), EINVAL, "b_grouping"), (dict(a=AT + 8), ESHAPE, "codes"),
     (dict(b=AT + 4), ESHAPE, "codes"), (dict(sb=AT + 2), ESHAPE, "scales"), (dict(out=AT + 1), ESHAPE, "out"), (dict(stride=9), ESHAPE, "out_stride"),
-    (dict(K=0x7fffffff), ESHAPE, "too large"), (dict(M=(1 << 29) + 1), ESHAPE, "too large"), (dict(M=1 << 29, N=1 << 29, stride=1 << 29), ESHAPE, "too large"),
+    (dict(K=0x7fffffff), ESHAPE, "too large"), (dict(M=(1 << 29) + 1), ESHAPE, "too large"), (dict(N=1 << 28, stride=1 << 28), ESHAPE, "too large"), (dict(M=1 << 29, N=1 << 29, stride=1 << 29), ESHAPE, "too large"),
 ], ids=str)
 def test_product_arguments(change, code, text):
     a = dict(M=10, N=10, K=100, a=AT, sa=AT, b=AT, sb=AT, grouping=0, out=AT, stride=10)
