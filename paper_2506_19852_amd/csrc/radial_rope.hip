@@ -93,9 +93,8 @@ __device__ __forceinline__ Place place_of(const RopeArgs& a, int32_t b, int32_t 
   return p;
 }
 
-// Turn of a pair: cos and sin, or 1 and 0 where nothing turns.
+// Turn of a pair: cos and sin.
 __device__ __forceinline__ f32x2 turn_of(const RopeArgs& a, const Place& p, int32_t pair) {
-  if (!p.on || pair >= a.pairs) return f32x2{1.f, 0.f};
   const int axis = (pair >= a.pair_end[0]) + (pair >= a.pair_end[1]);
   const int32_t base = axis == 0 ? 0 : a.pair_end[axis - 1];
   const int64_t row = axis == 0 ? p.row[0] : axis == 1 ? p.row[1] : p.row[2];
@@ -123,9 +122,11 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, int32_t interleav
   constexpr int kPairs = kPieces == Pieces::kInterleaved ? 4 : kPieces == Pieces::kHalf ? 8 : 1;
   const int32_t pair0 = unit * kPairs;
   const bool stays = kPieces != Pieces::kInterleaved && pair0 >= a.pairs;  // a piece behind the pairs
+  // Pairs of the piece that turn.  The rest is copied, not turned by 1 and 0, which would carry an infinity from one of a pair to the other.
+  const int32_t turning = place.on ? max(0, min(kPairs, a.pairs - pair0)) : 0;
   f32x2 turn[kPairs];
 #pragma unroll
-  for (int i = 0; i < kPairs; ++i) turn[i] = stays ? f32x2{1.f, 0.f} : turn_of(a, place, pair0 + i);
+  for (int i = 0; i < kPairs; ++i) turn[i] = i < turning ? turn_of(a, place, pair0 + i) : f32x2{1.f, 0.f};
   // dimensions of the piece's first and second part
   int32_t one, two = 0;
   if (kPieces == Pieces::kInterleaved) one = 8 * unit;
@@ -167,8 +168,8 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, int32_t interleav
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float x = v[2 * i], y = v[2 * i + 1];
-          v[2 * i] = x * turn[i][0] - y * turn[i][1];
-          v[2 * i + 1] = x * turn[i][1] + y * turn[i][0];
+          v[2 * i] = i < turning ? x * turn[i][0] - y * turn[i][1] : x;
+          v[2 * i + 1] = i < turning ? x * turn[i][1] + y * turn[i][0] : y;
         }
         Eight<T>::store(out[j] + one, v);
       } else if constexpr (kPieces == Pieces::kHalf) {
@@ -183,8 +184,8 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, int32_t interleav
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const float x = u[i], y = v[i];
-            u[i] = x * turn[i][0] - y * turn[i][1];
-            v[i] = x * turn[i][1] + y * turn[i][0];
+            u[i] = turning ? x * turn[i][0] - y * turn[i][1] : x;
+            v[i] = turning ? x * turn[i][1] + y * turn[i][0] : y;
           }
           Eight<T>::store(out[j] + one, u);
           Eight<T>::store(out[j] + two, v);
@@ -194,8 +195,8 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, int32_t interleav
           out[j][one] = single[j][0];
         } else {
           const float x = (float)single[j][0], y = (float)single[j][1];
-          out[j][one] = (T)(x * turn[0][0] - y * turn[0][1]);
-          out[j][two] = (T)(x * turn[0][1] + y * turn[0][0]);
+          out[j][one] = (T)(turning ? x * turn[0][0] - y * turn[0][1] : x);
+          out[j][two] = (T)(turning ? x * turn[0][1] + y * turn[0][0] : y);
         }
       }
     }
@@ -301,14 +302,14 @@ int turn(const radial_rope_params* params, const float* table, size_t table_byte
   const bool interleaved = p.layout == RADIAL_ROPE_INTERLEAVED;
   const Pieces pieces = interleaved ? Pieces::kInterleaved : a.pairs % 8 == 0 ? Pieces::kHalf : Pieces::kSingles;
   a.units = pieces == Pieces::kInterleaved ? D / 8 : pieces == Pieces::kHalf ? a.pairs / 8 + (D - 2 * a.pairs) / 8 : a.pairs + D - 2 * a.pairs;
-  const int32_t heads = q_heads + k_heads;
+  const int64_t heads = (int64_t)q_heads + k_heads;
   if ((int64_t)B * N > kMostThreads / a.units) return fail(RADIAL_ESHAPE, "B*N*D is too large for one launch");
   const int64_t lanes = (int64_t)B * N * a.units;
   a.heads_each = 8;
   const int64_t groups = (lanes + 255) / 256;
   // few tokens: heads over more lanes, until there are some for every compute unit
   while (a.heads_each > 1 && groups * ((heads + a.heads_each - 1) / a.heads_each) < 1024) a.heads_each /= 2;
-  const int32_t parts = (heads + a.heads_each - 1) / a.heads_each;
+  const int64_t parts = (heads + a.heads_each - 1) / a.heads_each;
   if (parts > 65535) return fail(RADIAL_ESHAPE, "too many heads for one launch");
   const dim3 grid((unsigned)groups, (unsigned)parts);
   if (type == RADIAL_F32) launch<float>(a, pieces, interleaved, grid, (hipStream_t)hip_stream);

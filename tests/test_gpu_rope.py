@@ -130,3 +130,26 @@ def test_more_than_2_to_the_31_elements():
     want = torch.empty_like(some)
     rl.radial_rope_fwd(p, table, some, want, first=N - 7)
     assert torch.equal(out[:, :, -7:], want) and not torch.equal(want, some)
+
+
+@pytest.mark.parametrize("gradient", [False, True], ids=["fwd", "bwd"])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("dims,D,layout", [([16, 14], 48, "interleaved"), ([16, 16], 48, "half"), ([10, 10], 48, "half")], ids=str)
+def test_what_is_not_turned_is_copied(dims, D, layout, dtype, gradient):
+    """Text, padding and the dimensions behind the turned ones keep their values beside infinities, and the sign of a zero."""
+    p, table = _table([4, 5], dims, layout=layout)
+    R, N = sum(dims), 20
+    x = rounded(np.random.default_rng(8).normal(size=(1, 3, N, D)), dtype).astype(np.float32)
+    for at, value in ((1, np.inf), (2, -np.inf), (5, np.nan), (8, -0.0), (9, -1.0), (24, -np.inf)):
+        x[..., 3, at] = value            # the token off the grid
+        if R + at < D:
+            x[..., R + at] = value       # behind the turned dimensions, of every token
+    positions = torch.arange(N, dtype=torch.int32, device=DEV).view(1, N).clone()
+    positions[0, 3] = -1
+    q = torch.tensor(x, dtype=dtype, device=DEV)
+    out = torch.empty_like(q)
+    (rl.radial_rope_bwd if gradient else rl.radial_rope_fwd)(p, table, q, out, positions=positions)
+    got, want = out.float().cpu(), torch.tensor(x)
+    for a, b in ((got[..., 3, :], want[..., 3, :]), (got[..., R:], want[..., R:])):
+        assert torch.equal(a.isnan(), b.isnan())
+        assert torch.equal(a.nan_to_num(7.0, 8.0, 9.0), b.nan_to_num(7.0, 8.0, 9.0)) and torch.equal(a.signbit() & ~b.isnan(), b.signbit() & ~b.isnan())
