@@ -40,7 +40,7 @@ typedef struct {
 } radial_rows;
 
 typedef struct {
-  int32_t B, N, C;      /* >= 1; C <= 16384; B*N < 2^31                                                        */
+  int32_t B, N, C;      /* >= 1; C <= 16384; B*N < 2^31 - 1024                                                 */
   int32_t group;        /* tokens that share a row of conditioning: token n of batch b has row b*G + n/group,  */
                         /*   G = ceil(N/group): N for one row per batch, tokens per frame for one per frame    */
   int32_t post, pre;    /* RADIAL_NORM_*: of the branch y; of the new residual r (NONE: no z)                  */

@@ -682,7 +682,8 @@ bool is_norm(int32_t kind) { return kind == RADIAL_NORM_LAYER || kind == RADIAL_
 int check_params(const radial_norm_params* p) {
   if (!p) return fail(RADIAL_EINVAL, "params is NULL");
   if (p->B < 1 || p->N < 1 || p->C < 1 || p->group < 1) return fail(RADIAL_EINVAL, "B, N, C, group must be >= 1");
-  if ((int64_t)p->B * p->N > 0x7fffffffLL) return fail(RADIAL_EINVAL, "B*N must be below 2^31");
+  // a workgroup's teams step over its last row by up to 32 before they stop
+  if ((int64_t)p->B * p->N > 0x7fffffffLL - 1024) return fail(RADIAL_EINVAL, "B*N must be below 2^31 - 1024");
   if (p->C > kMaxChannels) return fail(RADIAL_EUNSUPPORTED, "C must be at most %d (got %d)", kMaxChannels, p->C);
   if (p->post != RADIAL_NORM_NONE && !is_norm(p->post)) return fail(RADIAL_EINVAL, "post must be a RADIAL_NORM_ value (got %d)", p->post);
   if (p->pre != RADIAL_NORM_NONE && !is_norm(p->pre)) return fail(RADIAL_EINVAL, "pre must be a RADIAL_NORM_ value (got %d)", p->pre);

@@ -70,6 +70,7 @@ def _norm(direction="fwd", params=None, **change):
 @pytest.mark.parametrize("params, code, text", [
     (dict(B=0), EINVAL, ">= 1"), (dict(N=0), EINVAL, ">= 1"), (dict(C=0), EINVAL, ">= 1"), (dict(group=0), EINVAL, ">= 1"), (dict(group=-3), EINVAL, ">= 1"),
     (dict(B=1 << 16, N=1 << 15), EINVAL, "2^31"), (dict(C=16385), EUNSUPPORTED, "16384"), (dict(post=3), EINVAL, "post"), (dict(pre=-1), EINVAL, "pre"),
+    (dict(B=1, N=(1 << 31) - 1), EINVAL, "2^31"), (dict(B=1, N=(1 << 31) - 1024), EINVAL, "2^31"),  # rows behind the last would pass 32 bits
     (dict(eps=0.0), EINVAL, "eps"), (dict(eps=float("nan")), EINVAL, "eps"), (dict(eps=float("inf")), EINVAL, "eps"),
     (dict(residual_scale=float("inf")), EINVAL, "residual_scale"),
 ], ids=str)
