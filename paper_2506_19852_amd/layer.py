@@ -110,6 +110,10 @@ def _mods(B, G, C, device, **named):
     return out
 
 
+def _too_large(what):
+    raise ValueError(f"{what} must be below 2^31")  # ctypes would keep the low 32 bits
+
+
 def _bytes(t, name, device):
     if t.get_device() != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous tensor on the current CUDA device")
@@ -118,7 +122,7 @@ def _bytes(t, name, device):
 
 def _group(group, N) -> int:
     """Tokens that share a row of conditioning: all without `group`, and where it is larger."""
-    return N if group is None or group > N else group
+    return N if group is None or group > N else max(group, 0)
 
 
 def _channels(t, name, C, device):
@@ -138,6 +142,8 @@ def radial_norm_fwd(x, r, z, *, y=None, gate=None, post_weight=None, weight=None
     lib = _lib or load()
     shape, device = x.shape, _device()
     B, N, C = shape
+    if (B * N | C) >> 31:
+        _too_large("B*N and C")
     group = _group(group, N)
     gate, scale, shift, step = _mods(B, -(-N // max(group, 1)), C, device, gate=gate, scale=scale, shift=shift)
     p = radial_norm_params(B, N, C, group, post, pre, eps, residual_scale, step, step)
@@ -146,6 +152,8 @@ def radial_norm_fwd(x, r, z, *, y=None, gate=None, post_weight=None, weight=None
 
 
 def radial_norm_bwd_workspace(B: int, N: int, C: int, *, group=None, post=RADIAL_NORM_NONE, pre=RADIAL_NORM_LAYER) -> int:
+    if (B | N | C) >> 31:
+        _too_large("B, N and C")
     p = radial_norm_params(B, N, C, _group(group, N), post, pre, 1e-6, 1.0, C, C)
     return int((_lib or load()).radial_norm_bwd_workspace(byref(p)))
 
@@ -159,6 +167,8 @@ def radial_norm_bwd(r, dz, dx, workspace, *, dr=None, y=None, dy=None, gate=None
     lib = _lib or load()
     shape, device = dx.shape, _device()
     B, N, C = shape
+    if (B * N | C) >> 31:
+        _too_large("B*N and C")
     group = _group(group, N)
     G = -(-N // max(group, 1))
     gate, scale, step = _mods(B, G, C, device, gate=gate, scale=scale)
@@ -200,6 +210,8 @@ def rope_params(sizes, dims, *, layout="interleaved", scaling="none", factor=1.0
     p.layout = _LAYOUTS[layout]
     per_axis = zip(sizes, dims, of_axes(scaling, "scaling"), of_axes(factor, "factor"), of_axes(original, "original"))
     for i, (size, dim, how, by, before) in enumerate(per_axis):
+        if max(size, dim, before) >> 31:
+            _too_large("sizes, dims and original")
         if how not in _SCALINGS:
             raise ValueError(f"scaling must be one of {', '.join(_SCALINGS)}")
         p.size[i], p.dims[i], p.scaling[i], p.factor[i], p.original[i] = size, dim, _SCALINGS[how], by, before
@@ -235,6 +247,8 @@ def _heads(t, name, shape, dtype, device) -> radial_tensor:
 def _rope(call, names, params, table, q, q_out, k, k_out, positions, first, stream):
     shape, device = q.shape, _device()
     B, q_heads, N, D = shape
+    if (B * N | D | q_heads) >> 31:
+        _too_large("B*N, D and the heads")
     dtype = q.dtype
     kind = _types.get(dtype)
     if kind is None:
@@ -245,6 +259,8 @@ def _rope(call, names, params, table, q, q_out, k, k_out, positions, first, stre
             raise ValueError(f"{names[2]} and {names[3]} go together")
         k_shape = k.shape
         k_heads = k_shape[1]
+        if k_heads >> 31:
+            _too_large("the heads")
         if k_shape != shape and k_shape != (B, k_heads, N, D):
             raise ValueError(f"{names[2]} must have {names[0]}'s shape but for the heads")
         k_in, k_to = _heads(k, names[2], k_shape, dtype, device), _heads(k_out, names[3], k_shape, dtype, device)
@@ -253,8 +269,8 @@ def _rope(call, names, params, table, q, q_out, k, k_out, positions, first, stre
         if positions.dtype is not _i32 or positions.get_device() != device or not positions.is_contiguous() or positions.shape != (B, N):
             raise ValueError("positions must be a contiguous CUDA int32 tensor [B, N]")
         at = positions.data_ptr()
-    elif first >= 1 << 31:
-        raise ValueError("first must be below 2^31")
+    elif first >= 1 << 31 or first < -1:
+        raise ValueError("first must be below 2^31 and not negative")
     _check_table(table, device)
     _check(call(byref(params), table.data_ptr(), table.numel() * 4, B, N, D, q_heads, _heads(q, names[0], shape, dtype, device),
                 _heads(q_out, names[1], shape, dtype, device), k_heads, k_in, k_to, kind, at, first, _stream_ptr(stream)))
@@ -295,6 +311,8 @@ def radial_quantize_groups_fp8(x, codes=None, scales=None, codes_t=None, scales_
     if kind is None or x.get_device() != device or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError("x must be a CUDA bf16 or float32 tensor [rows, cols] with unit stride in cols")
     rows, cols = shape
+    if (rows | cols) >> 31:
+        _too_large("rows and cols")
     blocks = grouping == RADIAL_BLOCKS
     c, s = _codes(codes, scales, "", rows, cols, -(-rows // 128) if blocks else rows, device)
     ct, st = _codes(codes_t, scales_t, "transposed ", cols, rows, -(-cols // 128) if blocks else cols, device)
@@ -310,6 +328,8 @@ def radial_product_fp8(a_codes, a_scales, b_codes, b_scales, out, stream=None):
         raise ValueError("out must be a CUDA bf16 tensor [M, N] with unit stride in N")
     M, N = shape
     K = a_codes.shape[-1]
+    if (M | N | K) >> 31:
+        _too_large("M, N and K")
     a, sa = _codes(a_codes, a_scales, "a_", M, K, M, device)
     blocks = b_scales.shape[-1] != N
     b, sb = _codes(b_codes, b_scales, "b_", N, K, -(-N // 128) if blocks else N, device)

@@ -303,3 +303,40 @@ def test_tensors_of_another_device_or_of_none_are_refused(one_device):
 def test_numpy_numbers_and_defaults():
     p = rl.rope_params(np.array([3, 4]), [8, np.int64(8)], scaling=["linear", "none"], factor=[4.0, 1.0])
     assert list(p.size)[:2] == [3, 4] and list(p.scaling)[:2] == [1, 0] and p.theta == 1e4
+
+
+def test_sizes_beyond_32_bits_are_refused_not_cut(one_device):
+    bf16, f32, u8 = torch.bfloat16, torch.float32, torch.uint8
+    more = (1 << 32) + 8
+    for shape in ((2, more, 64), (1 << 16, 1 << 15, 64), (more, 8, 64), (2, 8, more)):
+        x = _fake(bf16, *shape)
+        with pytest.raises(ValueError, match="2\\^31"):
+            rl.radial_norm_fwd(x, None, x, stream=1)
+        with pytest.raises(ValueError, match="2\\^31"):
+            rl.radial_norm_bwd(x, x, x, _fake(u8, 1 << 20), stream=1)
+    for shape in ((more, 8, 64), (2, more, 64), (2, 8, more)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            rl.radial_norm_bwd_workspace(*shape)
+    x = _fake(bf16, 2, 8, 64)
+    with pytest.raises(rb.RadialError, match=">= 1"):
+        rl.radial_norm_fwd(x, None, x, group=4 - (1 << 32), stream=1)
+    p, table, q = rl.rope_params([8], [64]), _fake(f32, 512), _fake(bf16, 1, 2, 8, 64)
+    for shape in ((more, 2, 8, 64), (1, more, 8, 64), (1, 2, more, 64), (1, 2, 8, more)):
+        big = _fake(bf16, *shape)
+        with pytest.raises(ValueError, match="2\\^31"):
+            rl.radial_rope_fwd(p, table, big, big, stream=1)
+    keys = _fake(bf16, 1, more, 8, 64)
+    with pytest.raises(ValueError, match="2\\^31"):
+        rl.radial_rope_fwd(p, table, q, q, keys, keys, stream=1)
+    for first in (1 << 31, more, 8 - (1 << 32)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            rl.radial_rope_fwd(p, table, q, q, first=first, stream=1)
+    for bad in (dict(sizes=[more]), dict(dims=[more]), dict(original=more)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            rl.rope_params(**{**dict(sizes=[8], dims=[64]), **bad})
+    for rows, cols in ((more, 128), (128, more)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            rl.radial_quantize_groups_fp8(_fake(bf16, rows, cols), _fake(u8, rows, cols), _fake(f32, -(-cols // 128), rows), stream=1)
+    for M, N, K in ((more, 128, 128), (128, more, 128), (128, 128, (1 << 32) + 128)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            rl.radial_product_fp8(_fake(u8, M, K), _fake(f32, K // 128, M), _fake(u8, N, K), _fake(f32, K // 128, N), _fake(bf16, M, N), stream=1)
