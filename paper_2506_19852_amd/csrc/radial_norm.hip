@@ -49,13 +49,13 @@ struct Meeting {
   f32x4 place[2][kMaxWaves];
 };
 
-// The channels of a thread: 8 V of them.  Vectors: eight in a row, V times, a workgroup's width apart; single elements: each a
-// width apart (rows that are not 16-byte aligned).
+// The channels of a thread: 8 V of them, eight in a row, V times, a team's width apart.  kVec: rows are 16-byte aligned and of whole eights;
+// otherwise they start anywhere and the last eight may be fewer.
 template <bool kVec, int V>
 struct Channels {
   int32_t first, width, C;
-  __device__ __forceinline__ int32_t at(int v, int e) const { return kVec ? (v * width + first) * 8 + e : (v * 8 + e) * width + first; }
-  __device__ __forceinline__ bool has(int v, int e) const { return at(v, kVec ? 0 : e) < C; }  // vectors: all eight or none
+  __device__ __forceinline__ int32_t at(int v, int e) const { return (v * width + first) * 8 + e; }
+  __device__ __forceinline__ bool has(int v, int e) const { return at(v, kVec ? 0 : e) < C; }
   __device__ __forceinline__ int32_t count() const {
     int32_t n = 0;
 #pragma unroll
@@ -69,41 +69,34 @@ struct Channels {
 // A thread's channels of a row, as they lie in memory.
 template <class T, bool kVec, int V>
 struct Held {
-  Eight<T> piece[kVec ? V : 1];
-  T single[kVec ? 1 : 8 * V];
+  Eight<T> piece[V];
   __device__ __forceinline__ void load(const T* row, const Channels<kVec, V>& ch) {
-    if constexpr (kVec) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
+    for (int v = 0; v < V; ++v) {
+      if constexpr (kVec) {
         if (ch.has(v, 0)) piece[v].load(row + ch.at(v, 0));
         else piece[v].clear();
+      } else if (ch.C < 8) {
+        piece[v].load_some(row + ch.at(v, 0), ch.C - ch.at(v, 0));
+      } else {
+        if (ch.has(v, 0)) piece[v].load_any(row + min(ch.at(v, 0), ch.C - 8));
+        else piece[v].clear();
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8 * V; ++i) single[i] = ch.has(i / 8, i % 8) ? row[ch.at(i / 8, i % 8)] : (T)0.f;
     }
   }
   __device__ __forceinline__ void clear() {
-    if constexpr (kVec) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) piece[v].clear();
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8 * V; ++i) single[i] = (T)0.f;
-    }
+    for (int v = 0; v < V; ++v) piece[v].clear();
   }
-  __device__ __forceinline__ void get(float (&out)[8 * V]) const {
-    if constexpr (kVec) {
+  __device__ __forceinline__ void get(float (&out)[8 * V], const Channels<kVec, V>& ch) const {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float e8[8];
-        piece[v].get(e8);
+    for (int v = 0; v < V; ++v) {
+      float e8[8];
+      Eight<T> eight = piece[v];
+      if (!kVec && ch.C >= 8 && ch.has(v, 0) && ch.at(v, 8) > ch.C) eight.drop(ch.at(v, 8) - ch.C);
+      eight.get(e8);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) out[8 * v + e] = e8[e];
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8 * V; ++i) out[i] = (float)single[i];
+      for (int e = 0; e < 8; ++e) out[8 * v + e] = e8[e];
     }
   }
 };
@@ -112,15 +105,13 @@ template <class T, bool kVec, int V>
 __device__ __forceinline__ void store_row(T* row, const float (&val)[8 * V], const Channels<kVec, V>& ch) {
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    if constexpr (kVec) {
-      float e8[8];
+    float e8[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) e8[e] = val[8 * v + e];
+    for (int e = 0; e < 8; ++e) e8[e] = val[8 * v + e];
+    if constexpr (kVec) {
       if (ch.has(v, 0)) Eight<T>::store(row + ch.at(v, 0), e8);
     } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (ch.has(v, e)) row[ch.at(v, e)] = (T)val[8 * v + e];
+      Eight<T>::store_some(row + ch.at(v, 0), e8, ch.C - ch.at(v, 0));
     }
   }
 }
@@ -131,7 +122,7 @@ __device__ __forceinline__ void load_mod(float (&out)[8 * V], const float* row, 
   if (row) {
     Held<float, kVec, V> h;
     h.load(row, ch);
-    h.get(out);
+    h.get(out, ch);
   } else {
 #pragma unroll
     for (int i = 0; i < 8 * V; ++i) out[i] = missing;
@@ -325,10 +316,10 @@ __global__ void __launch_bounds__(kWide ? 512 : 256) norm_fwd_kernel(NormArgs a)
     y = next_y;
     fetch(n + s.teams);
     float r[E];
-    x.get(r);
+    x.get(r, s.ch);
     if (a.y.ptr) {
       float u[E];
-      y.get(u);
+      y.get(u, s.ch);
       if (a.post != RADIAL_NORM_NONE) {
         float mean, inverse;
         statistics<kVec, V>(u, a.post, a.eps, s.team, s.ch, s.own_count, s.of_own, mean, inverse);
@@ -404,15 +395,15 @@ __global__ void __launch_bounds__(kWide ? 512 : 256) norm_bwd_kernel(NormArgs a)
     const Row& now = held[0];
     float D[E];
     if (a.dr.ptr) {
-      now.dr.get(D);
+      now.dr.get(D, s.ch);
     } else {
 #pragma unroll
       for (int i = 0; i < E; ++i) D[i] = 0.f;
     }
     if (has_z) {
       float n[E], d[E];
-      now.r.get(n);
-      now.dz.get(d);
+      now.r.get(n, s.ch);
+      now.dz.get(d, s.ch);
       float mean, inverse;
       statistics<kVec, V>(n, a.pre, a.eps, s.team, s.ch, s.own_count, s.of_own, mean, inverse);
       float along = 0.f, flat = 0.f;
@@ -441,7 +432,7 @@ __global__ void __launch_bounds__(kWide ? 512 : 256) norm_bwd_kernel(NormArgs a)
     }
     if (has_y) {
       float m[E];
-      now.y.get(m);
+      now.y.get(m, s.ch);
       float inverse = 1.f;
       if (a.post != RADIAL_NORM_NONE) {
         float mean;
@@ -653,26 +644,26 @@ int launch_one(const NormArgs& a, bool backward, int64_t grid, hipStream_t strea
   return RADIAL_OK;
 }
 
-template <class XT, class YT>
-int launch_types(const NormArgs& a, bool vec, bool backward, int64_t grid, hipStream_t stream) {
+template <class XT, class YT, bool kVec>
+int launch_types(const NormArgs& a, bool backward, int64_t grid, hipStream_t stream) {
   const int eights = eights_of(a.C);
-  if (!vec) {
-    if (eights == 1) return launch_one<XT, YT, false, 1, true, 64>(a, backward, grid, stream);
-    if (eights == 2) return launch_one<XT, YT, false, 2, true, 64>(a, backward, grid, stream);
-    return launch_one<XT, YT, false, 4, true, 64>(a, backward, grid, stream);
-  }
-  if (a.C <= 128) return launch_one<XT, YT, true, 1, false, 16>(a, backward, grid, stream);
-  if (a.C <= 256) return launch_one<XT, YT, true, 1, false, 32>(a, backward, grid, stream);
-  if (a.C <= kNarrow) return launch_one<XT, YT, true, 1, false, 64>(a, backward, grid, stream);
-  if (eights == 1) return launch_one<XT, YT, true, 1, true, 64>(a, backward, grid, stream);
-  if (eights == 2) return launch_one<XT, YT, true, 2, true, 64>(a, backward, grid, stream);
-  return launch_one<XT, YT, true, 4, true, 64>(a, backward, grid, stream);
+  if (a.C <= 128) return launch_one<XT, YT, kVec, 1, false, 16>(a, backward, grid, stream);
+  if (a.C <= 256) return launch_one<XT, YT, kVec, 1, false, 32>(a, backward, grid, stream);
+  if (a.C <= kNarrow) return launch_one<XT, YT, kVec, 1, false, 64>(a, backward, grid, stream);
+  if (eights == 1) return launch_one<XT, YT, kVec, 1, true, 64>(a, backward, grid, stream);
+  if (eights == 2) return launch_one<XT, YT, kVec, 2, true, 64>(a, backward, grid, stream);
+  return launch_one<XT, YT, kVec, 4, true, 64>(a, backward, grid, stream);
+}
+
+template <bool kVec>
+int launch_rows(const NormArgs& a, int32_t x_type, int32_t y_type, bool backward, int64_t grid, hipStream_t stream) {
+  if (x_type == RADIAL_F32)
+    return y_type == RADIAL_F32 ? launch_types<float, float, kVec>(a, backward, grid, stream) : launch_types<float, __bf16, kVec>(a, backward, grid, stream);
+  return y_type == RADIAL_F32 ? launch_types<__bf16, float, kVec>(a, backward, grid, stream) : launch_types<__bf16, __bf16, kVec>(a, backward, grid, stream);
 }
 
 int launch(const NormArgs& a, int32_t x_type, int32_t y_type, bool vec, bool backward, int64_t grid, hipStream_t stream) {
-  if (x_type == RADIAL_F32)
-    return y_type == RADIAL_F32 ? launch_types<float, float>(a, vec, backward, grid, stream) : launch_types<float, __bf16>(a, vec, backward, grid, stream);
-  return y_type == RADIAL_F32 ? launch_types<__bf16, float>(a, vec, backward, grid, stream) : launch_types<__bf16, __bf16>(a, vec, backward, grid, stream);
+  return vec ? launch_rows<true>(a, x_type, y_type, backward, grid, stream) : launch_rows<false>(a, x_type, y_type, backward, grid, stream);
 }
 
 // ---- checks -------------------------------------------------------------------------------------

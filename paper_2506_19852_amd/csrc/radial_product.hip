@@ -27,7 +27,6 @@ struct QuantArgs {
   uint8_t *codes, *codes_t;
   float *scales, *scales_t;
   int32_t col_tiles, row_tiles;
-  int32_t vec;  // rows start 16-byte aligned
 };
 
 // x / scale as float32: the product with the inverse, and what it leaves, once more; off by half a unit and 2^-46 of the value.  (A division
@@ -65,15 +64,7 @@ __global__ void __launch_bounds__(256) quantize_groups_kernel(QuantArgs a) {
     Eight<T> raw[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const T* p = (const T*)a.x + (int64_t)(r0 + i) * a.stride + c0;
-      if (r0 + i < a.rows && a.vec && c0 + 8 <= a.cols) {
-        raw[i].load(p);
-      } else {
-        T e[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = r0 + i < a.rows && c0 + j < a.cols ? p[j] : (T)0.f;
-        raw[i] = __builtin_bit_cast(Eight<T>, e);
-      }
+      raw[i].load_some((const T*)a.x + (int64_t)(r0 + i) * a.stride + c0, r0 + i < a.rows ? a.cols - c0 : 0);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) raw[i].get(v[i]);
@@ -166,14 +157,9 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(QuantArgs a) {
   const bool live = row < a.rows;
   const T* p = (const T*)a.x + (int64_t)(live ? row : 0) * a.stride + c0;
   float v[8];
-  if (a.vec && c0 + 8 <= a.cols) {
-    Eight<T> raw;
-    raw.load(p);
-    raw.get(v);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c0 + j < a.cols ? (float)p[j] : 0.f;
-  }
+  Eight<T> raw;
+  raw.load_some(p, a.cols - c0);
+  raw.get(v);
   float amax = 0.f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(v[j]));
@@ -214,7 +200,6 @@ struct ProductArgs {
   int32_t M, N, groups;
   int64_t sa_stride;  // scales of A from one group to the next
   int32_t b_blocks;  // 128-row blocks of B
-  int32_t vec;       // rows of out start 16-byte aligned
 };
 
 __device__ __forceinline__ i32x8 sixteen_rows(const uint8_t* row) {
@@ -477,11 +462,6 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) product_tile_
 #pragma unroll
         for (int t = 0; t < 4; ++t) sum[i][t] += *place(from_part, i, t);
   }
-  // Rows that are not 16-byte aligned go through LDS, 16 at a time, to be stored a row of 64 columns at once (straight from the sums a store would
-  // touch 64 places: 1237 x 1961 x 1000 took 18.4 us instead of 12.8).
-  if (!a.vec) __syncthreads();  // everyone is done with the stages, and with the parts' sums
-  constexpr int kPitch = 144;
-  char* turn = lds + wave * 16 * kPitch;
 #pragma unroll
   for (int i = 0; i < kMTiles; ++i) {
     uint32_t pair[8];
@@ -490,24 +470,13 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) product_tile_
       pair[2 * t] = pack_bf16(sum[i][t][0], sum[i][t][1]);
       pair[2 * t + 1] = pack_bf16(sum[i][t][2], sum[i][t][3]);
     }
-    const int32_t row0 = m0 + (wm * kMTiles + i) * 16, column0 = n0 + wn * 64;
-    if (!a.vec) {
-      *lds_cast<u32x4>(turn + l16 * kPitch + q * 32) = u32x4{pair[0], pair[1], pair[2], pair[3]};
-      *lds_cast<u32x4>(turn + l16 * kPitch + q * 32 + 16) = u32x4{pair[4], pair[5], pair[6], pair[7]};
-      asm volatile("" ::: "memory");  // one wave's accesses to LDS come in order
-      for (int r = 0; r < 16; ++r) {
-        const uint16_t v = *lds_cast<const uint16_t>(turn + r * kPitch + lane * 2);
-        if (row0 + r < a.M && column0 + lane < a.N) ((uint16_t*)a.out)[(row0 + r) * a.out_stride + column0 + lane] = v;
-      }
-      asm volatile("" ::: "memory");
-      continue;
-    }
-    const int32_t m = row0 + l16, n = column0 + q * 16;
+    // 16 neighbouring columns of a lane, wherever they lie (by way of LDS, to store whole rows of a tile, single elements were slower)
+    const int32_t m = m0 + (wm * kMTiles + i) * 16 + l16, n = n0 + wn * 64 + q * 16;
     if (m >= a.M) continue;
     __bf16* out = a.out + m * a.out_stride + n;
     if (n + 16 <= a.N) {
-      *(u32x4*)out = u32x4{pair[0], pair[1], pair[2], pair[3]};
-      *(u32x4*)(out + 8) = u32x4{pair[4], pair[5], pair[6], pair[7]};
+      *(u32x4_any*)out = u32x4{pair[0], pair[1], pair[2], pair[3]};
+      *(u32x4_any*)(out + 8) = u32x4{pair[4], pair[5], pair[6], pair[7]};
     } else {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
@@ -587,7 +556,6 @@ extern "C" int radial_quantize_groups_fp8(int32_t rows, int32_t cols, const void
   a.codes = codes; a.scales = scales; a.codes_t = codes_t; a.scales_t = scales_t;
   a.row_tiles = (int32_t)(((int64_t)rows + kGroup - 1) / kGroup);
   a.col_tiles = (int32_t)(((int64_t)cols + kGroup - 1) / kGroup);
-  a.vec = ((uintptr_t)x & 15u) == 0 && stride * size_of(type) % 16 == 0;
   const bool blocks = grouping == RADIAL_BLOCKS;
   return type == RADIAL_F32 ? launch_quantize<float>(a, blocks, (hipStream_t)hip_stream) : launch_quantize<__bf16>(a, blocks, (hipStream_t)hip_stream);
 }
@@ -608,7 +576,6 @@ extern "C" int radial_product_fp8(int32_t M, int32_t N, int32_t K, const uint8_t
   a.M = M; a.N = N; a.sa_stride = M;
   a.groups = (K + kGroup - 1) / kGroup;
   a.b_blocks = (N + kGroup - 1) / kGroup;
-  a.vec = ((uintptr_t)out & 15u) == 0 && out_stride % 8 == 0;
   hipStream_t stream = (hipStream_t)hip_stream;
   const bool blocks = b_grouping == RADIAL_BLOCKS;
   return blocks ? launch_product<true>(a, stream) : launch_product<false>(a, stream);

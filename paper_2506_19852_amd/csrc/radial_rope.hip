@@ -105,12 +105,12 @@ __device__ __forceinline__ f32x2 turn_of(const RopeArgs& a, const Place& p, int3
 enum class Pieces {
   kInterleaved,  // eight dimensions in a row: four pairs
   kHalf,         // eight pairs, dimensions 8u .. and R/2 + 8u ..; behind them eight dimensions that stay
-  kSingles,      // one pair, whatever the layout (halves that are not 16-byte aligned); behind them one dimension that stays
+  kHalfAny,      // the same where R/2 is no multiple of eight: the last of the pairs, and of the dimensions that stay, may be fewer, at any address
 };
 
 // One thread per token and piece of a head; heads heads_each at a time.  Turns are rounded once, at the end.
 template <class T, Pieces kPieces>
-__global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, int32_t interleaved) {
+__global__ void __launch_bounds__(256) rope_kernel(RopeArgs a) {
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (id >= (int64_t)a.B * a.N * a.units) return;
   const int32_t unit = (int32_t)(id % a.units);
@@ -119,7 +119,8 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, int32_t interleav
   const Place place = place_of(a, b, n);
   const int32_t rotated = 2 * a.pairs;
 
-  constexpr int kPairs = kPieces == Pieces::kInterleaved ? 4 : kPieces == Pieces::kHalf ? 8 : 1;
+  constexpr bool kAny = kPieces == Pieces::kHalfAny;
+  constexpr int kPairs = kPieces == Pieces::kInterleaved ? 4 : 8;
   const int32_t pair0 = unit * kPairs;
   const bool stays = kPieces != Pieces::kInterleaved && pair0 >= a.pairs;  // a piece behind the pairs
   // Pairs of the piece that turn.  The rest is copied, not turned by 1 and 0, which would carry an infinity from one of a pair to the other.
@@ -128,11 +129,11 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, int32_t interleav
 #pragma unroll
   for (int i = 0; i < kPairs; ++i) turn[i] = i < turning ? turn_of(a, place, pair0 + i) : f32x2{1.f, 0.f};
   // dimensions of the piece's first and second part
-  int32_t one, two = 0;
+  int32_t one, two = 0, count = 8;  // count: dimensions of either
   if (kPieces == Pieces::kInterleaved) one = 8 * unit;
-  else if (stays) one = rotated + (kPieces == Pieces::kHalf ? 8 : 1) * (unit - a.pairs / kPairs);
-  else if (interleaved) { one = 2 * pair0; two = one + 1; }
+  else if (stays) one = rotated + 8 * (unit - (a.pairs + 7) / 8);
   else { one = pair0; two = a.pairs + pair0; }
+  if (kAny) count = min(8, stays ? a.D - one : a.pairs - pair0);
 
   const int32_t all = a.heads[0] + a.heads[1];
   const int32_t h0 = blockIdx.y * a.heads_each, h1 = min(h0 + a.heads_each, all);
@@ -141,7 +142,6 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, int32_t interleav
     const T* in[kAtOnce];
     T* out[kAtOnce];
     Eight<T> lo[kAtOnce], hi[kAtOnce];
-    T single[kAtOnce][2];
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j) {
       const int32_t head = min(h + j, h1 - 1);
@@ -151,9 +151,15 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, int32_t interleav
       in[j] = (const T*)x.in + b * x.isb + hh * x.ish + n * x.isn;
       out[j] = (T*)x.out + b * x.osb + hh * x.osh + n * x.osn;
       if (h + j >= h1) continue;
-      if constexpr (kPieces == Pieces::kSingles) {
-        single[j][0] = in[j][one];
-        if (!stays) single[j][1] = in[j][two];
+      if constexpr (kAny) {
+        const int32_t whole = stays ? a.D - rotated : a.pairs, back = whole < 8 ? 0 : 8 - count;
+        if (whole < 8) {
+          lo[j].load_some(in[j] + one, count);
+          hi[j].load_some(in[j] + two, stays ? 0 : count);
+        } else {
+          lo[j].load_any(in[j] + one - back);
+          if (!stays) hi[j].load_any(in[j] + two - back);
+        }
       } else {
         lo[j].load(in[j] + one);
         if (kPieces == Pieces::kHalf && !stays) hi[j].load(in[j] + two);
@@ -172,11 +178,16 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, int32_t interleav
           v[2 * i + 1] = i < turning ? x * turn[i][1] + y * turn[i][0] : y;
         }
         Eight<T>::store(out[j] + one, v);
-      } else if constexpr (kPieces == Pieces::kHalf) {
+      } else {
+        if (kAny && count < 8 && (stays ? a.D - rotated : a.pairs) >= 8) {
+          lo[j].drop(8 - count);
+          if (!stays) hi[j].drop(8 - count);
+        }
         if (stays) {
           float v[8];
           lo[j].get(v);
-          Eight<T>::store(out[j] + one, v);
+          if (kAny) Eight<T>::store_some(out[j] + one, v, count);
+          else Eight<T>::store(out[j] + one, v);
         } else {
           float u[8], v[8];
           lo[j].get(u);
@@ -187,16 +198,13 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, int32_t interleav
             u[i] = turning ? x * turn[i][0] - y * turn[i][1] : x;
             v[i] = turning ? x * turn[i][1] + y * turn[i][0] : y;
           }
-          Eight<T>::store(out[j] + one, u);
-          Eight<T>::store(out[j] + two, v);
-        }
-      } else {
-        if (stays) {
-          out[j][one] = single[j][0];
-        } else {
-          const float x = (float)single[j][0], y = (float)single[j][1];
-          out[j][one] = (T)(turning ? x * turn[0][0] - y * turn[0][1] : x);
-          out[j][two] = (T)(turning ? x * turn[0][1] + y * turn[0][0] : y);
+          if (kAny) {
+            Eight<T>::store_some(out[j] + one, u, count);
+            Eight<T>::store_some(out[j] + two, v, count);
+          } else {
+            Eight<T>::store(out[j] + one, u);
+            Eight<T>::store(out[j] + two, v);
+          }
         }
       }
     }
@@ -248,10 +256,10 @@ HeadsArg heads_arg(const radial_tensor& in, const radial_tensor& out) {
 }
 
 template <class T>
-void launch(const RopeArgs& a, Pieces pieces, bool interleaved, dim3 grid, hipStream_t stream) {
-  if (pieces == Pieces::kInterleaved) rope_kernel<T, Pieces::kInterleaved><<<grid, dim3(256), 0, stream>>>(a, interleaved);
-  else if (pieces == Pieces::kHalf) rope_kernel<T, Pieces::kHalf><<<grid, dim3(256), 0, stream>>>(a, interleaved);
-  else rope_kernel<T, Pieces::kSingles><<<grid, dim3(256), 0, stream>>>(a, interleaved);
+void launch(const RopeArgs& a, Pieces pieces, dim3 grid, hipStream_t stream) {
+  if (pieces == Pieces::kInterleaved) rope_kernel<T, Pieces::kInterleaved><<<grid, dim3(256), 0, stream>>>(a);
+  else if (pieces == Pieces::kHalf) rope_kernel<T, Pieces::kHalf><<<grid, dim3(256), 0, stream>>>(a);
+  else rope_kernel<T, Pieces::kHalfAny><<<grid, dim3(256), 0, stream>>>(a);
 }
 
 int check_table(const radial_rope_params& p, const float* table, size_t bytes) {
@@ -299,9 +307,8 @@ int turn(const radial_rope_params* params, const float* table, size_t table_byte
   }
   if (2 * a.pairs > D) return fail(RADIAL_ESHAPE, "the axes turn %d dimensions, the heads have %d", 2 * a.pairs, D);
   a.sign = gradient ? -1.f : 1.f;
-  const bool interleaved = p.layout == RADIAL_ROPE_INTERLEAVED;
-  const Pieces pieces = interleaved ? Pieces::kInterleaved : a.pairs % 8 == 0 ? Pieces::kHalf : Pieces::kSingles;
-  a.units = pieces == Pieces::kInterleaved ? D / 8 : pieces == Pieces::kHalf ? a.pairs / 8 + (D - 2 * a.pairs) / 8 : a.pairs + D - 2 * a.pairs;
+  const Pieces pieces = p.layout == RADIAL_ROPE_INTERLEAVED ? Pieces::kInterleaved : a.pairs % 8 == 0 ? Pieces::kHalf : Pieces::kHalfAny;
+  a.units = pieces == Pieces::kInterleaved ? D / 8 : (a.pairs + 7) / 8 + (D - 2 * a.pairs + 7) / 8;
   const int64_t heads = (int64_t)q_heads + k_heads;
   if ((int64_t)B * N > kMostThreads / a.units) return fail(RADIAL_ESHAPE, "B*N*D is too large for one launch");
   const int64_t lanes = (int64_t)B * N * a.units;
@@ -312,8 +319,8 @@ int turn(const radial_rope_params* params, const float* table, size_t table_byte
   const int64_t parts = (heads + a.heads_each - 1) / a.heads_each;
   if (parts > 65535) return fail(RADIAL_ESHAPE, "too many heads for one launch");
   const dim3 grid((unsigned)groups, (unsigned)parts);
-  if (type == RADIAL_F32) launch<float>(a, pieces, interleaved, grid, (hipStream_t)hip_stream);
-  else launch<__bf16>(a, pieces, interleaved, grid, (hipStream_t)hip_stream);
+  if (type == RADIAL_F32) launch<float>(a, pieces, grid, (hipStream_t)hip_stream);
+  else launch<__bf16>(a, pieces, grid, (hipStream_t)hip_stream);
   RADIAL_HIP_TRY(hipGetLastError());
   return RADIAL_OK;
 }

@@ -250,3 +250,14 @@ def test_more_than_2_to_the_31_elements():
     want = torch.empty(1, 5, C, dtype=BF16, device=DEV)
     rl.radial_norm_fwd(some[None], None, want)
     assert torch.equal(z[0, -5:], want[0])
+
+
+@pytest.mark.parametrize("C", [2, 6, 9, 12, 15, 100, 121, 131, 250, 254, 259, 383, 511, 513, 518, 1023, 1029, 2051, 4095, 4101, 8187])
+@pytest.mark.parametrize("types", [(BF16, BF16), (F32, F32), (F32, BF16)], ids=["bf16", "f32", "f32-bf16"])
+def test_rows_that_end_anywhere(C, types):
+    """The last eight channels are 1 to 8, rows start at any element's address."""
+    for lead in (8, 1 + C % 5):
+        case = (2, 7, C, 3, ol.LAYER if C % 2 else ol.RMS, ol.RMS if C % 3 else ol.LAYER, *types, lead)
+        test_forward(case, 0.0)
+        test_gradients(case)
+    test_in_place(case)

@@ -153,3 +153,14 @@ def test_what_is_not_turned_is_copied(dims, D, layout, dtype, gradient):
     for a, b in ((got[..., 3, :], want[..., 3, :]), (got[..., R:], want[..., R:])):
         assert torch.equal(a.isnan(), b.isnan())
         assert torch.equal(a.nan_to_num(7.0, 8.0, 9.0), b.nan_to_num(7.0, 8.0, 9.0)) and torch.equal(a.signbit() & ~b.isnan(), b.signbit() & ~b.isnan())
+
+
+@pytest.mark.parametrize("gradient", [False, True], ids=["fwd", "bwd"])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("dims,D", [([2], 8), ([6], 8), ([6], 16), ([12], 24), ([18], 24), ([22], 24), ([14, 8], 32), ([26], 40), ([30], 32), ([10, 20, 12], 48),
+                                    ([46], 64), ([78], 80), ([90], 96), ([122], 128)], ids=str)
+def test_halves_that_end_anywhere(dims, D, dtype, gradient):
+    """One to seven pairs, and dimensions that stay, in the last piece of each."""
+    case = ([3, 4, 5][:len(dims)], dims, D, "half", 2, 3, 1, 11, 1)
+    test_turns(case, dtype, gradient)
+    test_in_place_is_the_same(case)
