@@ -499,7 +499,7 @@ struct GradArgs {
 };
 
 constexpr int kGradColumns = 16, kGradSlices = 64;  // a wave: 16 channels, four slices
-constexpr int kFewGroups = 4;
+constexpr int kFewGroups = 16;
 constexpr int64_t kMostInY = 65535;
 
 // The sum over a wave's four slices, in all of them.
@@ -508,16 +508,23 @@ __device__ __forceinline__ float over_four(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// 16 channels of a group (kFew: of up to four groups, each with its share of the slices): 64 slices of its workgroups' sums each, then the slices' sums.
-// (With 64 channels and 16 slices the gradients of 2 x 1237 x 1000 took 41 us instead of 26.)  With few groups the gradients of the weights come along, instead of from another launch.
-template <bool kFew>
+// The gradients of a group's conditioning from its sums k: P, T, Q.
+__device__ __forceinline__ void store_grad(const GradArgs& a, int64_t group, int32_t c, int32_t k, float total) {
+  const int64_t mod = group * a.dmod_stride + c;
+  if (k == 0 && a.dscale) a.dscale[mod] = a.weight ? total * a.weight[c] : total;
+  if (k == 1) a.dshift[mod] = total;
+  if (k == 2 && a.dgate) a.dgate[mod] = a.post_weight ? total * a.post_weight[c] : total;
+}
+
+// Up to 16 groups: 16 channels of all of them, each group with its share of 64 slices, which add up its workgroups' sums; then the slices' sums, and the gradients
+// of the weights.  (With 64 channels and 16 slices the gradients of 2 x 1237 x 1000 took 41 us instead of 26.)
 __global__ void __launch_bounds__(kGradColumns * kGradSlices) norm_grad_kernel(GradArgs a) {
   __shared__ float sums[3][kGradSlices / 4][kGradColumns], of_groups[3][kFewGroups][kGradColumns];
   const int32_t lane = threadIdx.x, slice = threadIdx.y;
   const int32_t c = blockIdx.x * kGradColumns + lane;
-  const int32_t slices = !kFew || a.groups == 1 ? kGradSlices : a.groups == 2 ? kGradSlices / 2 : kGradSlices / 4;  // of a group
-  const int64_t group = kFew ? slice / slices : blockIdx.y + (int64_t)blockIdx.z * kMostInY;
-  if (!kFew && group >= a.groups) return;
+  int32_t slices = kGradSlices;  // of a group
+  while (slices * a.groups > kGradSlices) slices /= 2;
+  const int64_t group = slice / slices;
   float sum[3] = {0.f, 0.f, 0.f};
   if (c < a.C && group < a.groups) {
     const float* p = a.partial + group * a.chunks * 3 * a.C + c;
@@ -535,31 +542,56 @@ __global__ void __launch_bounds__(kGradColumns * kGradSlices) norm_grad_kernel(G
     if (slice % 4 == k) sums[k][slice / 4][lane] = sum[k];
   }
   __syncthreads();
-  // slice k (few groups: k of each group's slices) adds up P, T or Q
+  // slice k of each group's adds up P, T or Q
   const int32_t k = slice % slices;
-  const bool adds = k < 3 && c < a.C && group < a.groups && (a.wants >> k & 1);
-  if (adds) {
+  if (k < 3 && c < a.C && group < a.groups && (a.wants >> k & 1)) {
     float total = 0.f;
 #pragma unroll 4
     for (int i = 0; i < slices / 4; ++i) total += sums[k][slice / slices * (slices / 4) + i][lane];
-    const int64_t mod = group * a.dmod_stride + c;
-    if (k == 0 && a.dscale) a.dscale[mod] = a.weight ? total * a.weight[c] : total;
-    if (k == 1) a.dshift[mod] = total;
-    if (k == 2 && a.dgate) a.dgate[mod] = a.post_weight ? total * a.post_weight[c] : total;
-    if (!kFew && a.of_group && k != 1) a.of_group[(group * 2 + (k == 2)) * a.C + c] = total;
-    if (kFew) {
-      if (k == 0 && a.scale) total *= 1.f + a.scale[group * a.mod_stride + c];
-      if (k == 2 && a.gate) total *= a.gate[group * a.mod_stride + c];
-      of_groups[k][group][lane] = total;
-    }
+    store_grad(a, group, c, k, total);
+    if (k == 0 && a.scale) total *= 1.f + a.scale[group * a.mod_stride + c];
+    if (k == 2 && a.gate) total *= a.gate[group * a.mod_stride + c];
+    of_groups[k][group][lane] = total;
   }
-  if (!kFew) return;
   __syncthreads();
   if (slice > 2 || !(a.wants >> slice & 1) || c >= a.C) return;
   float total = 0.f;
   for (int g = 0; g < a.groups; ++g) total += of_groups[slice][g][lane];
   if (slice == 0 && a.dweight) a.dweight[c] = total;
   if (slice == 2 && a.dpost_weight) a.dpost_weight[c] = total;
+}
+
+// More groups, each with few sums: a wave for 64 channels of a group, or the four of a workgroup.  (With 1024 threads for
+// each group and 16 channels the gradients of 32 760 x 5120 in groups of 1560 took 454 us instead of 427, of 4 x 1000 x 1536 in groups of 20 116 (32), of 2 859 (60).)
+__global__ void __launch_bounds__(256) norm_grad_many_kernel(GradArgs a, int32_t waves_of_group) {
+  __shared__ float sums[3][4][64];
+  const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int32_t c = blockIdx.x * 64 + lane, first = wave % waves_of_group;
+  const int64_t group = (blockIdx.y + (int64_t)blockIdx.z * kMostInY) * (4 / waves_of_group) + wave / waves_of_group;
+  const bool live = c < a.C && group < a.groups;
+  float sum[3] = {0.f, 0.f, 0.f};
+  if (live) {
+    const float* p = a.partial + group * a.chunks * 3 * a.C + c;
+    for (int32_t i = first; i < a.chunks; i += waves_of_group) {
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        if (a.wants >> k & 1) sum[k] += p[(i * 3 + k) * (int64_t)a.C];
+    }
+  }
+  if (waves_of_group > 1) {
+#pragma unroll
+    for (int k = 0; k < 3; ++k) sums[k][wave][lane] = sum[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 3; ++k) sum[k] = (sums[k][0][lane] + sums[k][1][lane]) + (sums[k][2][lane] + sums[k][3][lane]);
+  }
+  if (!live || first) return;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    if (!(a.wants >> k & 1)) continue;
+    store_grad(a, group, c, k, sum[k]);
+    if (a.of_group && k != 1) a.of_group[(group * 2 + (k == 2)) * a.C + c] = sum[k];
+  }
 }
 
 // dw and dw_post: sums over the groups, each times its conditioning.
@@ -832,17 +864,22 @@ extern "C" int radial_norm_bwd(const radial_norm_params* params, radial_rows r, 
 
   GradArgs g = {};
   g.partial = a.partial;
-  const bool weights = dweight || dpost_weight, few = weights && l.groups <= kFewGroups;
-  g.of_group = weights && !few ? a.partial + (size_t)l.groups * l.chunks * 3 * p.C : nullptr;
+  const bool few = l.groups <= kFewGroups;
+  g.of_group = (dweight || dpost_weight) && !few ? a.partial + (size_t)l.groups * l.chunks * 3 * p.C : nullptr;
   g.gate = gate; g.post_weight = post_weight; g.weight = weight; g.scale = scale;
   g.dgate = dgate; g.dscale = dscale; g.dshift = dshift; g.dpost_weight = dpost_weight; g.dweight = dweight;
   g.C = p.C; g.chunks = l.chunks; g.groups = (int32_t)l.groups; g.wants = a.wants;
   g.mod_stride = p.mod_stride; g.dmod_stride = p.dmod_stride;
   const unsigned columns = (unsigned)((p.C + kGradColumns - 1) / kGradColumns);
   const dim3 block(kGradColumns, kGradSlices);
-  const unsigned in_y = (unsigned)(l.groups < kMostInY ? l.groups : kMostInY), in_z = (unsigned)((l.groups + kMostInY - 1) / kMostInY);
-  if (few) norm_grad_kernel<true><<<dim3(columns), block, 0, (hipStream_t)hip_stream>>>(g);
-  else norm_grad_kernel<false><<<dim3(columns, in_y, in_z), block, 0, (hipStream_t)hip_stream>>>(g);
+  if (few) {
+    norm_grad_kernel<<<dim3(columns), block, 0, (hipStream_t)hip_stream>>>(g);
+  } else {
+    const int32_t waves_of_group = l.chunks > 8 ? 4 : 1;
+    const int64_t rows = (l.groups * waves_of_group + 3) / 4;
+    const unsigned in_y = (unsigned)(rows < kMostInY ? rows : kMostInY), in_z = (unsigned)((rows + kMostInY - 1) / kMostInY);
+    norm_grad_many_kernel<<<dim3((unsigned)((p.C + 63) / 64), in_y, in_z), dim3(256), 0, (hipStream_t)hip_stream>>>(g, waves_of_group);
+  }
   RADIAL_HIP_TRY(hipGetLastError());
   if (g.of_group) {
     norm_weight_grad_kernel<<<dim3(columns), block, 0, (hipStream_t)hip_stream>>>(g);

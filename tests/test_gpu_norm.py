@@ -261,3 +261,11 @@ def test_rows_that_end_anywhere(C, types):
         test_forward(case, 0.0)
         test_gradients(case)
     test_in_place(case)
+
+
+@pytest.mark.parametrize("groups", [1, 2, 3, 4, 5, 8, 9, 16, 17, 40, 700])
+@pytest.mark.parametrize("C", [24, 1000])
+def test_gradients_of_weights_over_many_groups(C, groups):
+    """However the groups are added up: in shares of one launch, one after the other, or in a launch of their own."""
+    test_gradients((1, 3 * groups - (groups > 1), C, 3, ol.RMS, ol.LAYER, F32, BF16, 8))
+    test_gradients((2, 5 * groups, C, 5, ol.RMS, ol.LAYER, BF16, BF16, 8))
