@@ -214,15 +214,19 @@ __device__ __forceinline__ f32x4 product16(i32x8 a, i32x8 b) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);  // formats 0: E4M3; no block exponents
 }
 
-// Up to 16 rows: bound by reading B (2 x 30 720 x 5120: 27.7 us, 5.7 TB/s; 2 x 5120 x 5120: 8.7 us, 3 TB/s, five groups a wave).  A workgroup of
-// 8 waves takes 16 columns of C, each wave every 8th group, straight from memory (a lane's 32 bytes of a row, four lanes a line); the parts meet in
+// Up to 16 rows: bound by reading B (2 x 30 720 x 5120: 27.7 us, 5.7 TB/s; 2 x 5120 x 5120: 8.7 us, 3 TB/s, five groups a wave).  Few results: by how
+// long the groups take one after the other.  A workgroup of 8 waves takes 16 x 16 of C, each wave every 8th group, straight from memory (a lane's 32 bytes of a row, four lanes a line); the parts meet in
 // LDS.  Four groups of a wave at a time, or 16 waves, were slower by 0.7 us and more.
 constexpr int kParts = 8;
 template <bool kBlocks>
-__global__ void __launch_bounds__(64 * kParts) product_rows_kernel(ProductArgs a) {
+__global__ void __launch_bounds__(64 * kParts) product_pieces_kernel(ProductArgs a) {
   __shared__ f32x4 parts[kParts][64];
   const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int32_t n0 = blockIdx.x * 16, m = lane & 15, row = min(m, a.M - 1);
+  int32_t m0, n0;
+  tile_of(blockIdx.x, (a.M + 15) / 16, (a.N + 15) / 16, m0, n0);
+  m0 *= 16;
+  n0 *= 16;
+  const int32_t m = m0 + (lane & 15), row = min(m, a.M - 1);
   const int64_t bytes = (int64_t)a.groups * kGroup;
   const uint8_t* b_row = a.b + min(n0 + (lane & 15), a.N - 1) * bytes + (lane >> 4) * 32;
   const uint8_t* a_row = a.a + row * bytes + (lane >> 4) * 32;
@@ -515,9 +519,10 @@ int launch_form(int form, const ProductArgs& a, hipStream_t stream) {
 
 template <bool kBlocks>
 int launch_product(const ProductArgs& a, hipStream_t stream) {
-  if (a.M <= 16) {
-    if ((a.N + 15) / 16 > kMostThreads / (64 * kParts)) return fail(RADIAL_ESHAPE, "N is too large for one launch");
-    product_rows_kernel<kBlocks><<<dim3((unsigned)((a.N + 15) / 16)), dim3(64 * kParts), 0, stream>>>(a);
+  if (takes_pieces(a.M, a.N)) {
+    const int64_t tiles = pieces_of(a.M) * pieces_of(a.N);
+    if (tiles > kMostThreads / (64 * kParts)) return fail(RADIAL_ESHAPE, "N is too large for one launch");
+    product_pieces_kernel<kBlocks><<<dim3((unsigned)tiles), dim3(64 * kParts), 0, stream>>>(a);
     RADIAL_HIP_TRY(hipGetLastError());
     return RADIAL_OK;
   }

@@ -68,6 +68,12 @@ inline ProductPlan plan_product(int32_t M, int32_t N, int32_t groups) {
   return plan;
 }
 
+// Few rows or few results: pieces of 16 x 16, whose eight waves share the groups and read them straight from memory, as long as each piece has a compute
+// unit of its own.  (256 x 128 x 20 519, 128 pieces: 21 us, in tiles 33; 512 x 128 x 20 480, 256: 21, 41; 128 x 128 x 2048: 4.6, 7.4; with 264 pieces 14.1
+// either way; 403 x 384 x 7296, 624: 22, 15; 1024 x 1024 x 2048: 32, 8.)
+inline int64_t pieces_of(int32_t n) { return ((int64_t)n + 15) / 16; }
+inline bool takes_pieces(int32_t M, int32_t N) { return M <= 16 || pieces_of(M) * pieces_of(N) <= kComputeUnits; }
+
 // Tile of a workgroup.  XCD x of 8 (workgroup id mod 8) gets a run of neighbouring tiles, in bands of 8 rows of tiles, column by column: the 32 that
 // it works on at a time are 8 x 4, whose codes it fetches into its L2 once.
 __host__ __device__ __forceinline__ void tile_of(uint32_t id, int32_t tiles_m, int32_t tiles_n, int32_t& m, int32_t& n) {

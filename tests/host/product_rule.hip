@@ -1,5 +1,6 @@
 // The rules of the 8-bit product (radial_product_rule.h) on the host.  Input lines:
 //   form M N groups    -> index, rows, columns, parts of the tiles chosen; rows of M in them, index of the form of the rest
+//   small M N          -> 1 where pieces of 16 x 16 are taken
 //   tiles TM TN        -> "m n" of every workgroup
 //   pieces B           -> byte offset of piece p of row r, r below 256, p below 8, of operand A (0) or B (1), and whether 16 lanes that read one piece meet 16 banks
 #include <stdio.h>
@@ -40,6 +41,8 @@ int main() {
       const ProductPlan plan = plan_product(a, b, c);
       const TileForm& f = kTileForms[plan.form];
       printf("%d %d %d %d %d %d\n", plan.form, f.rows, f.columns, f.split, plan.rows, plan.rest);
+    } else if (!strcmp(what, "small") && scanf("%d %d", &a, &b) == 2) {
+      printf("%d\n", takes_pieces(a, b));
     } else if (!strcmp(what, "tiles") && scanf("%d %d", &a, &b) == 2) {
       for (uint32_t id = 0; id < (uint32_t)a * b; ++id) {
         int32_t m, n;

@@ -177,3 +177,13 @@ def test_more_than_2_to_the_31_elements():
     few = _buffers(70, N, 70)
     rl.radial_quantize_groups_fp8(last, *few)
     assert torch.equal(codes[-70:], few[0]) and torch.equal(scales[:, -70:], few[1])
+
+
+# few results of many groups, in pieces of 16 x 16; tiles of every form that are too many for that
+MORE_SIZES = [(17, 2048, 384), (256, 128, 20519), (128, 127, 2048), (250, 250, 130), (31, 33, 8000), (65, 1111, 128), (600, 120, 4100), (333, 333, 2000)]
+
+
+@pytest.mark.parametrize("blocks", [False, True], ids=["groups", "blocks"])
+@pytest.mark.parametrize("size", MORE_SIZES, ids=str)
+def test_product_of_few_results(size, blocks):
+    test_product(size, blocks)

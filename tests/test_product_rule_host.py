@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 
 from paper_2506_19852_amd import build as hip_build
-from test_gpu_product import SIZES
+from test_gpu_product import MORE_SIZES, SIZES
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -68,3 +68,12 @@ def test_pieces(rule, operand):
     for r in rows:
         assert (at[r + step] - at[r] == step * 128).all()
     assert conflicts == [0]
+
+
+def test_every_form_is_reached_by_a_tested_size_that_is_not_small(rule):
+    small = [r[0] for r in rule([f"small {m} {n}" for m, n, _ in SIZES])]
+    assert {0, 1} == set(small)
+    tested = [s for s, is_small in zip(SIZES, small) if not is_small]
+    forms = {f[0] for f in rule([f"form {m} {n} {-(-k // 128)}" for m, n, k in tested + MORE_SIZES])}
+    assert forms == set(range(8)), forms
+    assert [r[0] for r in rule(["small 16 100000", "small 17 2048", "small 17 2064", "small 512 128", "small 1000 1000"])] == [1, 1, 0, 1, 0]
