@@ -27,7 +27,8 @@ typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef f32x2 f32x2_any __attribute__((aligned(4)));
 
 // Eight consecutive elements as they lie in memory.  load and store want 16-byte alignment; load_any takes any element's address; load_some and store_some the
-// first `count` from there (the others are zero, and are not touched).  A row's last eight, where they are fewer, are better read as the eight that
+// first `count` from there (the others are zero, and are not touched).  set rounds eight values to T, set_pair elements 2 i and
+// 2 i + 1 where `on`, and put writes them as they lie: elements that were loaded and not set keep their bits, a NaN's among them.  A row's last eight, where they are fewer, are better read as the eight that
 // end with the row and moved down by drop() when they are used: a load whose value is put together from single elements is waited for.
 template <class T>
 struct Eight;
@@ -43,8 +44,18 @@ struct Eight<__bf16> {
       v[2 * i + 1] = __builtin_bit_cast(float, raw[i] & 0xffff0000u);
     }
   }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+    raw = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+  }
+  __device__ __forceinline__ void set_pair(int i, bool on, float a, float b) {
+    const uint32_t two = pack_bf16(a, b);
+    raw[i] = on ? two : raw[i];
+  }
+  __device__ __forceinline__ void put(__bf16* p) const { *(u32x4*)p = raw; }
   __device__ static __forceinline__ void store(__bf16* p, const float (&v)[8]) {
-    *(u32x4*)p = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+    Eight<__bf16> e;
+    e.set(v);
+    e.put(p);
   }
   __device__ __forceinline__ void load_any(const __bf16* p) { raw = *(const u32x4_any*)p; }
   // Element i <- element i + n, zero behind; 0 <= n < 8.
@@ -62,9 +73,13 @@ struct Eight<__bf16> {
     for (int i = 0; i < 4; ++i) raw[i] = e[2 * i] | e[2 * i + 1] << 16;
   }
   __device__ static __forceinline__ void store_some(__bf16* p, const float (&v)[8], int count) {
-    const uint32_t raw[4] = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+    Eight<__bf16> e;
+    e.set(v);
+    e.put_some(p, count);
+  }
+  __device__ __forceinline__ void put_some(__bf16* p, int count) const {
     if (count >= 8) {
-      *(u32x4_any*)p = u32x4{raw[0], raw[1], raw[2], raw[3]};
+      *(u32x4_any*)p = raw;
       return;
     }
     if (count <= 0) return;
@@ -90,9 +105,24 @@ struct Eight<float> {
       v[4 + i] = hi[i];
     }
   }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+    lo = f32x4{v[0], v[1], v[2], v[3]};
+    hi = f32x4{v[4], v[5], v[6], v[7]};
+  }
+  __device__ __forceinline__ void set_pair(int i, bool on, float a, float b) {
+    f32x4& half = i < 2 ? lo : hi;
+    const int at = 2 * (i & 1);
+    half[at] = on ? a : half[at];
+    half[at + 1] = on ? b : half[at + 1];
+  }
+  __device__ __forceinline__ void put(float* p) const {
+    *(f32x4*)p = lo;
+    *(f32x4*)(p + 4) = hi;
+  }
   __device__ static __forceinline__ void store(float* p, const float (&v)[8]) {
-    *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
-    *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    Eight<float> e;
+    e.set(v);
+    e.put(p);
   }
   __device__ __forceinline__ void load_any(const float* p) {
     lo = *(const f32x4_any*)p;
@@ -121,16 +151,19 @@ struct Eight<float> {
     }
   }
   __device__ static __forceinline__ void store_some(float* p, const float (&v)[8], int count) {
+    Eight<float> e;
+    e.set(v);
+    e.put_some(p, count);
+  }
+  __device__ __forceinline__ void put_some(float* p, int count) const {
     if (count >= 8) {
-      *(f32x4_any*)p = f32x4{v[0], v[1], v[2], v[3]};
-      *(f32x4_any*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+      *(f32x4_any*)p = lo;
+      *(f32x4_any*)(p + 4) = hi;
       return;
     }
     if (count <= 0) return;
-    if (count & 4) *(f32x4_any*)p = f32x4{v[0], v[1], v[2], v[3]};
-    Eight<float> rest;  // moved by drop(), which leaves it in registers; choosing from v by a condition put it into scratch memory
-    rest.lo = f32x4{v[0], v[1], v[2], v[3]};
-    rest.hi = f32x4{v[4], v[5], v[6], v[7]};
+    if (count & 4) *(f32x4_any*)p = lo;
+    Eight<float> rest = *this;  // moved by drop(), which leaves it in registers; choosing elements by a condition put them into scratch memory
     rest.drop(count & 4);
     if (count & 2) *(f32x2_any*)(p + (count & 4)) = f32x2{rest.lo[0], rest.lo[1]};
     rest.drop(count & 2);

@@ -164,3 +164,26 @@ def test_halves_that_end_anywhere(dims, D, dtype, gradient):
     case = ([3, 4, 5][:len(dims)], dims, D, "half", 2, 3, 1, 11, 1)
     test_turns(case, dtype, gradient)
     test_in_place_is_the_same(case)
+
+
+@pytest.mark.parametrize("gradient", [False, True], ids=["fwd", "bwd"])
+@pytest.mark.parametrize("dims,layout", [([24], "interleaved"), ([6, 14], "interleaved"), ([16], "half"), ([20], "half"), ([64], "half")], ids=str)
+def test_copies_keep_every_bit(dims, layout, gradient):
+    """Of every bf16 pattern, NaNs that signal and carry a payload among them, and of float32 ones."""
+    p, table = _table([4] * len(dims), dims, layout=layout)
+    R, D = sum(dims), 64
+    patterns = np.arange(1 << 16, dtype=np.uint16).view(np.int16)
+    words = np.random.default_rng(9).integers(0, 1 << 32, 1 << 16, dtype=np.uint32)
+    words[1::2] |= 0x7f800000                       # infinities and NaNs
+    call = rl.radial_rope_bwd if gradient else rl.radial_rope_fwd
+    for whole, dtype in ((patterns, BF16), (words.view(np.int32), F32)):
+        bits = torch.tensor(whole.reshape(1, 1, -1, D), device=DEV)
+        x = bits.view(dtype)
+        N = x.shape[2]
+        for on in (0, 1):
+            positions = torch.full((1, N), 1 if on else -1, dtype=torch.int32, device=DEV)
+            for in_place in (False, True):
+                out = x.clone() if in_place else torch.empty_like(x)
+                call(p, table, out if in_place else x, out, positions=positions)
+                from_ = R if on else 0
+                assert torch.equal(out.view(bits.dtype)[..., from_:], bits[..., from_:]), (dtype, on, in_place)
