@@ -50,6 +50,12 @@ __device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float 
   return (uint32_t)v;
 }
 
+// The bytes of eight codes that belong to the first `count`: beside an infinity the quotients of what lies behind the matrix are NaN, not zero.
+__device__ __forceinline__ u32x2 first_codes(int32_t count) {
+  const uint32_t n[2] = {(uint32_t)max(0, min(count, 4)), (uint32_t)max(0, min(count - 4, 4))};
+  return u32x2{n[0] == 4 ? ~0u : (1u << 8 * n[0]) - 1, n[1] == 4 ? ~0u : (1u << 8 * n[1]) - 1};
+}
+
 // One workgroup per 128 x 128 tile; a thread holds eight rows of eight columns.  Codes along the rows go out as they are (16 lanes, 128 bytes); those of the
 // transpose pass through LDS in pieces of eight rows, exchanged by column so that the pieces of one write lie in different banks.
 template <class T, bool kBlocks, bool kRows, bool kCols>
@@ -117,10 +123,11 @@ __global__ void __launch_bounds__(256) quantize_groups_kernel(QuantArgs a) {
   const int32_t row_tile = row0 / kGroup, col_tile = col0 / kGroup;
   u32x2 along[8];  // codes of a row's eight columns (blocks: the transpose's codes are these)
   if constexpr (kRows) {
+    const u32x2 of_matrix = first_codes(a.cols - c0);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const Quotient q(of_row[i]);
-      along[i] = u32x2{four_codes(q(v[i][0]), q(v[i][1]), q(v[i][2]), q(v[i][3])), four_codes(q(v[i][4]), q(v[i][5]), q(v[i][6]), q(v[i][7]))};
+      along[i] = u32x2{four_codes(q(v[i][0]), q(v[i][1]), q(v[i][2]), q(v[i][3])), four_codes(q(v[i][4]), q(v[i][5]), q(v[i][6]), q(v[i][7]))} & of_matrix;
       if (r0 + i < a.rows) {
         *(u32x2*)(a.codes + ((int64_t)(r0 + i) * a.col_tiles + col_tile) * kGroup + tc * 8) = along[i];
         if (!kBlocks && tc == 0) a.scales[(int64_t)col_tile * a.rows + r0 + i] = q.scale;
@@ -129,12 +136,13 @@ __global__ void __launch_bounds__(256) quantize_groups_kernel(QuantArgs a) {
     }
   }
   if constexpr (kCols) {
+    const u32x2 of_matrix = first_codes(a.rows - r0);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const Quotient q(of_col[j]);
       const int32_t c = tc * 8 + j;
       turned[c * 16 + (tr ^ tc)] =
-          u32x2{four_codes(q(v[0][j]), q(v[1][j]), q(v[2][j]), q(v[3][j])), four_codes(q(v[4][j]), q(v[5][j]), q(v[6][j]), q(v[7][j]))};
+          u32x2{four_codes(q(v[0][j]), q(v[1][j]), q(v[2][j]), q(v[3][j])), four_codes(q(v[4][j]), q(v[5][j]), q(v[6][j]), q(v[7][j]))} & of_matrix;
       if (!kBlocks && tr == 0 && col0 + c < a.cols) a.scales_t[(int64_t)row_tile * a.cols + col0 + c] = q.scale;
       if (kBlocks && threadIdx.x == 0 && j == 0) a.scales_t[(int64_t)row_tile * a.col_tiles + col_tile] = q.scale;
     }
@@ -170,7 +178,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(QuantArgs a) {
   const Quotient q(amax);
   if (!live) return;
   *(u32x2*)(a.codes + ((int64_t)row * a.col_tiles + col_tile) * kGroup + tc * 8) =
-      u32x2{four_codes(q(v[0]), q(v[1]), q(v[2]), q(v[3])), four_codes(q(v[4]), q(v[5]), q(v[6]), q(v[7]))};
+      u32x2{four_codes(q(v[0]), q(v[1]), q(v[2]), q(v[3])), four_codes(q(v[4]), q(v[5]), q(v[6]), q(v[7]))} & first_codes(a.cols - c0);
   if (tc == 0) a.scales[(int64_t)col_tile * a.rows + row] = q.scale;
 }
 

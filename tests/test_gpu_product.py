@@ -187,3 +187,33 @@ MORE_SIZES = [(17, 2048, 384), (256, 128, 20519), (128, 127, 2048), (250, 250, 1
 @pytest.mark.parametrize("size", MORE_SIZES, ids=str)
 def test_product_of_few_results(size, blocks):
     test_product(size, blocks)
+
+
+@pytest.mark.parametrize("blocks", [False, True], ids=["groups", "blocks"])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(4, 130), (130, 130), (129, 257), (300, 7), (7, 300)], ids=str)
+def test_codes_behind_the_matrix_are_zero_beside_an_infinity(shape, dtype, blocks):
+    """An infinite scale makes NaN of its whole group, but of the group's columns alone."""
+    rows, cols = shape
+    a = rounded(np.random.default_rng(37).normal(size=shape), dtype).astype(np.float32)
+    a[-1, -1], a[1, 2], a[2, -1] = np.inf, -np.inf, np.nan
+    x = torch.tensor(a, dtype=dtype, device=DEV)
+    scale_rows = lambda n: -(-n // 128) if blocks else n  # noqa: E731
+    for both in ((True, True), (True, False), (False, True)):
+        straight, turned = _buffers(rows, cols, scale_rows(rows)), _buffers(cols, rows, scale_rows(cols))
+        rl.radial_quantize_groups_fp8(x, *(straight if both[0] else (None, None)), *(turned if both[1] else (None, None)),
+                                      grouping=rl.RADIAL_BLOCKS if blocks else rl.RADIAL_GROUPS)
+        for there, (codes, scales), m in zip(both, (straight, turned), (a, a.T)):
+            if not there:
+                continue
+            R, P = -(-m.shape[0] // 128) * 128, codes.shape[1]
+            full = np.zeros((R, P), np.float32)
+            full[:m.shape[0], :m.shape[1]] = m
+            tiles = np.isinf(full).reshape(R // 128, 128, P // 128, 128).any((1, 3) if blocks else 3)
+            infinite = np.repeat(np.repeat(tiles, 128, 0) if blocks else tiles.reshape(R, -1), 128, 1)[:m.shape[0]]
+            got = codes.cpu().numpy()
+            assert not got[:, m.shape[1]:].any()
+            assert (((got & 0x7f) == 0x7f) == ((infinite | np.isnan(full[:m.shape[0]])) & (np.arange(P) < m.shape[1]))).all()
+            clean, _ = ol.quantize(np.where(infinite[:, :m.shape[1]], 0, m).astype(np.float32), blocks)
+            ok = ~infinite & ~np.isnan(full[:m.shape[0]])
+            assert np.array_equal(got[ok], clean[ok])
