@@ -295,10 +295,6 @@ struct TileShape {
 // Until at most kLeft copies of this wave are under way.
 template <int kLeft>
 __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLeft) : "memory"); }
-// 256 bytes from memory to LDS, 4 to a lane; see copy16_to_lds_sv.
-__device__ __forceinline__ void copy4_to_lds_sv(const void* base, uint32_t byte_offset, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_addr), "v"(byte_offset), "s"(base) : "memory", "m0");
-}
 
 template <int kWavesM, int kWavesN, int kMTiles, int kStages, int kSplit, bool kBlocks>
 __global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) product_tile_kernel(ProductArgs a) {
