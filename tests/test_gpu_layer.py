@@ -198,3 +198,75 @@ def test_the_benchmark_times_a_layer(capsys):
     line = json.loads(capsys.readouterr().out.strip().split("\n")[-1])
     assert line["unit"] == "ms" and line["steps"] == 2 and len(line["ms"]) == 8 and all(t > 0 for t in line["ms"].values())
     assert line["value"] == pytest.approx(sum(line["ms"].values()), rel=1e-2)
+
+
+INPUTS = {"x", "dr", "dz", "mod", "w", "q8", "params", "table", "mask"}
+
+
+def _clear(L):
+    """NaN, or bytes of ones, into everything that a pass writes: results, codes, scales and workspaces."""
+    def each(v):
+        if isinstance(v, torch.Tensor):
+            yield v
+        elif isinstance(v, (tuple, dict)):
+            for part in v.values() if isinstance(v, dict) else v:
+                yield from each(part)
+    cleared = [t for name, v in vars(L).items() if name not in INPUTS for t in each(v)]
+    for t in cleared:
+        t.fill_(255 if t.dtype == torch.uint8 else float("nan"))
+    return cleared
+
+
+def test_every_result_is_cleared():
+    L = Layer(6)
+    L.forward(); L.backward()  # noqa: E702
+    assert len(_clear(L)) == 10 + 2 + 4 + 2 + 2 + 16 + 2 and all(r.isnan().all() for r in L.results())
+
+
+@pytest.mark.parametrize("by_argument", [True, False], ids=["argument", "current"])
+def test_every_result_on_a_stream_of_its_own(by_argument):
+    """The stream is busy when the calls are made, and everything is cleared behind that work: a launch on another stream comes before its inputs, and its
+    results are lost."""
+    L = Layer(7)
+    L.forward(); L.backward()  # noqa: E702
+    want = L.results()
+    busy = torch.zeros(1 << 28, device=DEV)
+    _clear(L)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(30):
+            busy.add_(1.0)
+        _clear(L)
+        if not by_argument:
+            L.forward(); L.backward()  # noqa: E702
+    if by_argument:
+        L.forward(stream=side)
+        L.backward(stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(L.results(), want))
+
+
+def test_every_result_of_a_replay():
+    """Each replay alone leaves every result: nothing is left over from the eager pass."""
+    layers = [Layer(8), Layer(9, frames=3)]
+    graphs = []
+    for L in layers:
+        L.forward(); L.backward()  # noqa: E702
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            L.forward(); L.backward()  # noqa: E702
+        graphs.append(graph)
+    other = Layer(10)
+    for turn in range(4):
+        for L, graph in zip(layers, graphs):
+            L.x.mul_(1.1).add_(0.01 * turn)
+            L.dz.neg_()
+            L.forward(); L.backward()  # noqa: E702
+            want = L.results()
+            _clear(L)
+            other.forward(); other.backward()  # noqa: E702
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(L.results(), want)), turn
