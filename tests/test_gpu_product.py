@@ -217,3 +217,44 @@ def test_codes_behind_the_matrix_are_zero_beside_an_infinity(shape, dtype, block
             clean, _ = ol.quantize(np.where(infinite[:, :m.shape[1]], 0, m).astype(np.float32), blocks)
             ok = ~infinite & ~np.isnan(full[:m.shape[0]])
             assert np.array_equal(got[ok], clean[ok])
+
+
+# rows that two launches share: whole rounds in one of the two largest forms, the rest in a large one or a small one
+TWO_LAUNCHES = [(12919, 1822, 6000), (10838, 2091, 3400), (13249, 2624, 1000), (10862, 1305, 2750), (12580, 2832, 2400)]
+
+
+@pytest.mark.parametrize("blocks", [False, True], ids=["groups", "blocks"])
+@pytest.mark.parametrize("size", [(3, 1961, 1000), (16, 2000, 520), (250, 250, 1000), (257, 255, 130), (1024, 1024, 1024), *TWO_LAUNCHES], ids=str)
+def test_results_are_off_by_little_more_than_their_rounding(size, blocks):
+    """Random codes and scales, against the products of their values in float64.  One by one as in test_product; and as a whole, where what is dropped, of
+    either sign as the codes are, adds up as squares: from each eight products at most 7 parts of 2^-13 of the largest, whose square is at most that of all
+    eight together, sqrt(7) 2^-13 of the result in all.  1 % is for what the two errors have in common."""
+    M, N, K = size
+    g = torch.Generator(device=DEV).manual_seed(38)
+    v = torch.tensor(ol.e4m3_values(), device=DEV)
+    P = -(-K // 128) * 128
+
+    def operand(rows, scale_rows):
+        codes = torch.randint(0, 254, (rows, P), generator=g, device=DEV, dtype=torch.int32)
+        codes = codes + (codes >= 127)                 # all but 0x7f and 0xff
+        codes[:, K:] = 0
+        scales = torch.randn((P // 128, scale_rows), generator=g, device=DEV).exp()
+        full = scales.t().double().repeat_interleave(128, 0)[:rows] if scale_rows != rows else scales.t().double()
+        values = v[codes.long()].view(rows, -1, 128) * full[..., None]
+        return codes.to(torch.uint8), scales, values.view(rows, P)
+
+    (ac, asc, av), (bc, bs, bv) = operand(M, M), operand(N, -(-N // 128) if blocks else N)
+    lead = 8 if N % 8 == 0 else 3
+    whole = torch.full((M + 1, N + 2 * lead), 7.5, dtype=BF16, device=DEV)
+    out = whole[:M, lead:lead + N]
+    rl.radial_product_fp8(ac, asc, bc, bs, out)
+    want = av @ bv.t()
+    size_ = av.abs() @ bv.abs().t()
+    largest = lambda m: m.abs().view(len(m), -1, 8).amax(2)  # noqa: E731
+    bound = HALF_STEP[BF16] * want.abs() + 7 * 2.0 ** -13 * torch.minimum(largest(av) @ largest(bv).t(), size_) + (20 + P // 128) * 2.0 ** -23 * size_
+    off = out.double() - want
+    assert off.isfinite().all() and (off.abs() <= bound).all(), float((off.abs() / bound).max())
+    rounding = (want.to(BF16).double() - want).norm()
+    assert off.norm() <= 1.01 * (rounding ** 2 + 7 * 2.0 ** -26 * want.norm() ** 2) ** 0.5, (float(off.norm() / rounding))
+    out.fill_(7.5)
+    assert (whole == 7.5).all()

@@ -77,3 +77,20 @@ def test_every_form_is_reached_by_a_tested_size_that_is_not_small(rule):
     forms = {f[0] for f in rule([f"form {m} {n} {-(-k // 128)}" for m, n, k in tested + MORE_SIZES])}
     assert forms == set(range(8)), forms
     assert [r[0] for r in rule(["small 16 100000", "small 17 2048", "small 17 2064", "small 512 128", "small 1000 1000"])] == [1, 1, 0, 1, 0]
+
+
+def test_the_tiles_of_every_launch_are_those_of_a_tested_size(rule):
+    """Of sizes that take tiles: each form for all rows, and pairs of forms that share the rows, large ones for the rest among them."""
+    from test_gpu_product import TWO_LAUNCHES
+
+    def tiled(sizes):
+        small = rule([f"small {m} {n}" for m, n, _ in sizes])
+        return [(m, n, k) for (m, n, k), (is_small,) in zip(sizes, small) if not is_small]
+
+    sizes = tiled(SIZES + MORE_SIZES + TWO_LAUNCHES)
+    assert len(tiled(MORE_SIZES)) == 3 and len(tiled(TWO_LAUNCHES)) == len(TWO_LAUNCHES)
+    alone, shared = set(), set()
+    for (m, _, _), (form, _, _, _, of_form, rest) in zip(sizes, rule([f"form {m} {n} {-(-k // 128)}" for m, n, k in sizes])):
+        alone.add(form) if of_form == m else shared.add((form, rest))
+    assert alone == set(range(8)), alone
+    assert shared == {(0, 6), (0, 1), (0, 2), (0, 3), (1, 3), (1, 7)}, shared
