@@ -258,3 +258,37 @@ def test_results_are_off_by_little_more_than_their_rounding(size, blocks):
     assert off.norm() <= 1.01 * (rounding ** 2 + 7 * 2.0 ** -26 * want.norm() ** 2) ** 0.5, (float(off.norm() / rounding))
     out.fill_(7.5)
     assert (whole == 7.5).all()
+
+
+@pytest.mark.parametrize("M", [1, 16, 300], ids=["one row", "few rows", "tiles"])
+def test_what_is_left_where_large_products_cancel(M):
+    """256 - 256 + p: beside neither of the two (another eight of the 128) p is exact, in float32's reach; beside one of them it is exact down to 2^-13 of it,
+    and what is smaller is off by at most itself."""
+    v = ol.e4m3_values()
+    values = {v[c]: c for c in range(127)}
+    N, cases = 300, []
+    for first, second in ((0, 127), (64, 65), (13, 40)):
+        for spot in (1, 5, 7, 8, 12, 33, 66, 71, 72, 120, 126):
+            for e in range(0, 18):
+                x = 2.0 ** max(-6, 4 - e // 2)
+                if spot not in (first, second):
+                    cases.append((first, second, spot, x, 2.0 ** (8 - e) / x))
+    a, b = np.zeros((len(cases), 128), np.uint8), np.zeros((len(cases), 128), np.uint8)
+    for i, (first, second, spot, x, y) in enumerate(cases):
+        a[i, [first, second, spot]] = values[16.0], values[16.0], values[x]
+        b[i, [first, second, spot]] = values[16.0], values[16.0] | 128, values[y]
+    one = lambda n: torch.ones((1, n), device=DEV)  # noqa: E731
+    for at in range(0, len(cases), M):
+        # row m of A against all columns: its own is the case, wherever it lies in the tile
+        rows, some = a[at:at + M], b[at:at + M]
+        columns = np.resize(some, (N, 128)) if M < N else some
+        out = torch.empty((len(rows), len(columns)), dtype=BF16, device=DEV)
+        rl.radial_product_fp8(torch.tensor(rows, device=DEV), one(len(rows)), torch.tensor(columns, device=DEV), one(len(columns)), out)
+        for i, (first, second, spot, x, y) in enumerate(cases[at:at + M]):
+            p, beside = x * y, spot // 8 in (first // 8, second // 8)
+            got = to64(out[i, i::len(rows)])
+            assert len(got) and (got == got[0]).all()
+            if not beside or p >= 256 * 2.0 ** -13:
+                assert got[0] == p, (first, second, spot, p, got[0])
+            else:
+                assert abs(got[0] - p) <= p, (first, second, spot, p, got[0])
