@@ -7,12 +7,17 @@
 //     P = sum dz n, T = sum dz, Q = sum D m over a group's tokens:
 //     ds = P w,  dt = T,  dg = Q w_post,  dw = sum over groups P (1 + s),  dw_post = sum over groups Q g.
 //
-// Both passes are bound by memory: each tensor is read or written once and a row stays in registers between its statistics and its results.
+// Both passes are bound by memory up to 8192 channels: each tensor is read or written once and a row stays in registers between its statistics and its results.
 // A team of lanes takes a row: 16, 32 or 64 lanes with eight channels each up to 512 channels, from there all waves of the workgroup.  A thread
 // has the same channels in all rows of its workgroup, so that it loads the conditioning row once and keeps the sums over tokens in registers; a
 // workgroup's rows are of one group.  The backward writes a workgroup's sums to the workspace, where a second kernel adds them up
-// in a fixed order (no atomics).  32 760 x 5120 in bf16, residual and layer norm: forward 252 us (5.3 TB/s, what a large copy reaches), backward
-// 408 us (4.9 TB/s), with a second norm 261 and 418.
+// in a fixed order (no atomics).  32 760 x 5120 in bf16, residual and layer norm: forward 251-267 us (5.0-5.3 TB/s, what a large copy reaches), backward
+// 408-413 us (4.9 TB/s), with a second norm 261 and 418; 20 475 x 8192, the same bytes, 259 and 418.
+//
+// From 8193 to 16 384 channels a thread has 32 of them, and the gradients' sums, conditioning and rows do not fit its 256 registers: 470 to 640 bytes of a lane's values
+// (550 to 800 where rows are not aligned) go through scratch memory for every token.  The gradients of 20 455 x 8200 take 1597 us against a copy's 380,
+// of 13 650 x 12 288 1208, of 10 237 x 16 384 1057 (bf16; float32 2676, 2028, 1984 against 760).  The forward fits but for float32 branches (up to 100 bytes): 285, 273, 274 us of 253
+// (650, 593, 585 of 506).  Gradients of float32 rows of more than 4096 channels keep eight bytes there, which costs nothing (813-818 us of 760 at 8192).
 #include <float.h>
 #include <math.h>
 
