@@ -4,6 +4,7 @@ There is no fallback: a missing library or a failing call raises."""
 from __future__ import annotations
 
 import ctypes
+import numbers
 from ctypes import POINTER, byref, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
 
 from . import binding
@@ -199,7 +200,7 @@ def rope_params(sizes, dims, *, layout="interleaved", scaling="none", factor=1.0
         raise ValueError("sizes and dims need one entry for each of one to three axes")
 
     def of_axes(v, name):
-        v = [v] * axes if isinstance(v, (str, int, float)) else list(v)
+        v = [v] * axes if isinstance(v, (str, numbers.Real)) else list(v)
         if len(v) != axes:
             raise ValueError(f"{name} needs one value, or one for each axis")
         return v

@@ -340,3 +340,10 @@ def test_sizes_beyond_32_bits_are_refused_not_cut(one_device):
     for M, N, K in ((more, 128, 128), (128, more, 128), (128, 128, (1 << 32) + 128)):
         with pytest.raises(ValueError, match="2\\^31"):
             rl.radial_product_fp8(_fake(u8, M, K), _fake(f32, K // 128, M), _fake(u8, N, K), _fake(f32, K // 128, N), _fake(bf16, M, N), stream=1)
+
+
+@pytest.mark.parametrize("change", [dict(original=np.int64(100)), dict(factor=np.float32(2.0)), dict(factor=np.int32(2)), dict(scaling=np.str_("linear"), factor=2)], ids=str)
+def test_one_number_of_numpy_is_for_all_axes(change):
+    p = rl.rope_params([3, 4], [8, 8], **change)
+    q = rl.rope_params([3, 4], [8, 8], **{k: [v, v] for k, v in change.items()})
+    assert bytes(p) == bytes(q)
