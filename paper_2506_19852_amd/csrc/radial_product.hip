@@ -231,7 +231,7 @@ __device__ __forceinline__ f32x4 product16(i32x8 a, i32x8 b) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);  // formats 0: E4M3; no block exponents
 }
 
-// Up to 16 rows: bound by reading B (2 x 30 720 x 5120: 27.7 us, 5.7 TB/s; 2 x 5120 x 5120: 8.7 us, 3 TB/s, five groups a wave).  Few results: by how
+// Up to 16 rows: bound by reading B (2 x 30 720 x 5120: 27.7-30.1 us, 5.2-5.7 TB/s; 2 x 5120 x 5120: 8.9 us, 3 TB/s, five groups a wave).  Few results: by how
 // long the groups take one after the other.  A workgroup of 8 waves takes 16 x 16 of C, each wave every 8th group, straight from memory (a lane's 32 bytes of a row, four lanes a line); the parts meet in
 // LDS.  Four groups of a wave at a time, or 16 waves, were slower by 0.7 us and more.
 constexpr int kParts = 8;
@@ -275,8 +275,9 @@ __global__ void __launch_bounds__(64 * kParts) product_pieces_kernel(ProductArgs
 // LDS kStages - 1 stages ahead, straight from memory; a wave takes 16 kMTiles rows of 64 columns.  It holds the four fragments of its columns
 // and walks the fragments of its rows: four matrix instructions each, whose sums are scaled and added while the next ones run.  kSplit parts of the
 // workgroup's waves take the groups in turn and add up their sums at the end.
-// 256 x 256 tiles, eight waves, two a SIMD: 32 760 x 5120 x 5120 with blocks 753-815 us (2.1-2.3 PFLOP/s, the chip's clock drops to 1.7-1.8 GHz: what
-// bounds it is the power), 8192^3 427 us (2.6).  With groups on both sides, one product more per sum, 824-915 us.  32 x 32 x 64 matrix instructions, half
+// 256 x 256 tiles, eight waves, two a SIMD: 32 760 x 5120 x 5120 with blocks 740-815 us over boxes (2.1-2.3 PFLOP/s) once some 30 launches have let the board settle
+// its clock, 1.7-1.8 GHz (what bounds it is the power; the launches before take 750 to 1035), 8192^3 427-504 us (2.2-2.6).  With groups on both sides, one
+// product more per sum, 824-915 us.  32 x 32 x 64 matrix instructions, half
 // the operand reads, were 14 % slower (their two halves of a group depend on each other), workgroups that stay and fetch the next tile's first stage early 2 %.
 template <int kWavesM, int kWavesN, int kMTiles, int kStages, int kSplit>
 struct TileShape {

@@ -9,7 +9,8 @@ namespace radial {
 // Tiles of a product.  What a launch takes is put together from the time of a stage (of each part) and of what a tile does besides, in us, as measured
 // with the chip full of that tile, or with one on each compute unit where two fit (5120 x 5120, 100 to 14 040 rows, and others): large tiles move the
 // fewest codes per product, but a launch of a few of them leaves compute units idle, and a workgroup alone on its unit spends more than half of a small
-// tile's stage waiting, which parts of the groups at the same time make up for.
+// tile's stage waiting, which parts of the groups at the same time make up for.  With few groups, where the start and the end of a tile are most of it, the
+// estimate is too low: 1237 x 1961 x 1000, eight groups, 8.0 us of 11.4 to 12.2.
 struct TileForm {
   int32_t rows, columns, at_once, split;
   float stage_full, stage_one, besides;
