@@ -4,9 +4,11 @@
  *
  *   1. gated residual and norms:  r = residual_scale x + gate N_post(y),  z = N_pre(r) (1 + scale) + shift;
  *   2. rotary positions of queries and keys over one to three axes (frames, rows, columns);
- *   3. products in 8-bit floating point with a scale for each 128 values (the projections).
+ *   3. products in 8-bit floating point with a scale for each 128 values (the projections);
+ *   4. products in 8-bit integers with a scale for each token and each channel, and the projection made of them;
+ *   5. what a tuning step does with the gradients: their common norm, and AdamW over many tensors at once.
  *
- * Each has its forward and its gradients.  Conventions as in radial.h: functions return RADIAL_OK or a negative
+ * Each of 1 to 4 has its forward and its gradients.  Conventions as in radial.h: functions return RADIAL_OK or a negative
  * radial_status, nothing throws, radial_last_error() describes a failure; hip_stream is a hipStream_t as
  * void*; calls are asynchronous on that stream, allocate nothing and keep nothing (they can be captured into a
  * HIP graph); the caller owns all memory, which belongs to the current HIP device; every output is fully overwritten
@@ -177,6 +179,138 @@ RADIAL_API int radial_quantize_groups_fp8(int32_t rows, int32_t cols, const void
  * 2^23), EHIP. */
 RADIAL_API int radial_product_fp8(int32_t M, int32_t N, int32_t K, const uint8_t* a_codes, const float* a_scales, const uint8_t* b_codes,
                                   const float* b_scales, int32_t b_grouping, void* out, int64_t out_stride, void* hip_stream);
+
+/* ---- products in 8-bit integers ----------------------------------------------------------------
+ *
+ * A matrix [rows, columns] is held as whole numbers with one float32 scale for each row (a token's activations, a channel's
+ * weights):
+ *   codes  [rows, P] int8, P = columns rounded up to 128, zero beyond the columns; 16-byte aligned;
+ *   scales [rows].
+ * scale = max(amax/127, 2^-126) in float32, code = x/scale, as a float32 value, to the nearest whole number, ties to even.  A
+ * row that holds an infinity or a NaN has codes 0 and the scale NaN: every result that reads it is NaN.  Sums of products are
+ * whole numbers of 32 bits and exact. */
+
+/* Bytes of device workspace that radial_quantize_rows_i8 needs for codes_t or sums_t (0 on invalid arguments). */
+RADIAL_API size_t radial_quantize_rows_i8_workspace(int32_t rows, int32_t cols);
+
+/* Quantises x [rows, cols] (device, `type`, rows `stride` elements apart, stride >= cols) and, or, its transpose:
+ *   codes, scales     : of x; both NULL: not wanted;
+ *   codes_t, scales_t : of the transpose [cols, rows], with a scale for each column of x; both NULL: not wanted;
+ *   sums_t            : device float [cols], the sum of each column of x, or NULL; accumulate != 0 adds to what it holds;
+ *   workspace         : radial_quantize_rows_i8_workspace(rows, cols) bytes, 256-byte aligned, contents ignored and undefined
+ *                       afterwards; may be NULL where only codes and scales are wanted.
+ * Errors: EINVAL (NULL, sizes < 1, type, workspace), ESHAPE (stride, alignment, sizes), EHIP. */
+RADIAL_API int radial_quantize_rows_i8(int32_t rows, int32_t cols, const void* x, int32_t type, int64_t stride, int8_t* codes, float* scales,
+                                       int8_t* codes_t, float* scales_t, float* sums_t, int32_t accumulate, void* workspace, size_t workspace_bytes,
+                                       void* hip_stream);
+
+/* out[m, n] = a_scales[m] b_scales[n] (sum over k of a[m, k] b[n, k]) + bias[n]: A B^T + bias, a [M, K] and b [N, K] as above.
+ *   bias       : device float [N], or NULL;
+ *   out        : device, out_type, rows out_stride elements apart, out_stride >= N; rounded once;
+ *   accumulate : != 0: out, which is float32, <- out + the result.
+ * With X, W and the gradient dY of Y = X W^T:  Y: (X, W); dX: (dY, W transposed); dW: (dY transposed, X transposed).
+ * Up to K = 131 071 the sum is exact, for codes of -128 too.  A longer one is taken in parts of 130 944 columns that are added
+ * in float32, so that out has to be float32.  Products of two scales have to be finite in float32.
+ * Errors: EINVAL (NULL, sizes < 1, types, accumulate), EUNSUPPORTED (K above 131 071 with bf16), ESHAPE (stride, alignment, M or
+ * N above 2^29, K above 2^23), EHIP. */
+RADIAL_API int radial_product_i8(int32_t M, int32_t N, int32_t K, const int8_t* a_codes, const float* a_scales, const int8_t* b_codes,
+                                 const float* b_scales, const float* bias, void* out, int32_t out_type, int64_t out_stride, int32_t accumulate,
+                                 void* hip_stream);
+
+/* A projection y = x W^T + bias, x [M, K], W [N, K], in 8-bit integers: x is quantised by rows and multiplied.
+ *   w_codes, w_scales : of W (radial_quantize_rows_i8 of W, after each update of it);
+ *   workspace         : radial_linear_i8_fwd_workspace(M, N, K) bytes, 256-byte aligned, contents ignored and undefined afterwards.
+ * The other arguments and the errors are those of the two calls above. */
+RADIAL_API size_t radial_linear_i8_fwd_workspace(int32_t M, int32_t N, int32_t K);
+RADIAL_API int radial_linear_i8_fwd(int32_t M, int32_t N, int32_t K, const void* x, int32_t type, int64_t x_stride, const int8_t* w_codes,
+                                    const float* w_scales, const float* bias, void* y, int32_t y_type, int64_t y_stride, void* workspace,
+                                    size_t workspace_bytes, void* hip_stream);
+
+/* Its gradients from dy [M, N]: dx = dy W with dy quantised by rows, dw = dy^T x with dy and x quantised by columns, and
+ * dbias = the column sums of dy, which are not quantised (the rounding to codes is passed over, as if it were not there).
+ *   wt_codes, wt_scales, dx : of W transposed (codes_t of W), and dx [M, K]; dx NULL: not wanted, then the codes are not read;
+ *   x, dw                   : the forward's x [M, K] of dy's type, and dw [N, K]; dw NULL: not wanted, then x is not read;
+ *   dbias                   : device float [N], or NULL: not wanted;
+ *   accumulate              : != 0: dw, which is float32, and dbias are added to;
+ *   workspace               : radial_linear_i8_bwd_workspace(M, N, K) bytes, 256-byte aligned, contents ignored and undefined afterwards. */
+RADIAL_API size_t radial_linear_i8_bwd_workspace(int32_t M, int32_t N, int32_t K);
+RADIAL_API int radial_linear_i8_bwd(int32_t M, int32_t N, int32_t K, const void* dy, int32_t type, int64_t dy_stride, const void* x,
+                                    int64_t x_stride, const int8_t* wt_codes, const float* wt_scales, void* dx, int32_t dx_type, int64_t dx_stride,
+                                    void* dw, int32_t dw_type, int64_t dw_stride, float* dbias, int32_t accumulate, void* workspace,
+                                    size_t workspace_bytes, void* hip_stream);
+
+/* ---- AdamW over many tensors ---------------------------------------------------------------------
+ *
+ * One step for every value w of a tensor with gradient G, at step t = 1, 2, ...:
+ *   g = factor G,   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
+ *   w <- w (1 - lr decay) - lr/(1 - beta1^t) m / (sqrt(v)/sqrt(1 - beta2^t) + eps).
+ * Everything is computed in float32, w is rounded once to its type.
+ *
+ * States in 8 bits: m and sqrt(v) are held as E4M3 codes (as in radial.h) with a float32 scale for each block of 128 values of
+ * the tensor, the last block the rest: scale = amax/448, code = E4M3(m (448/amax)), all 0 where amax is 0.  (sqrt(v) spans half of
+ * the powers of two that v does.)  A positive sqrt(v) never becomes 0, but the smallest code: what a step divides by is not lost
+ * beside larger neighbours.  A NaN has the code of NaN and does not enter amax; with an infinity the block's state is NaN.  Codes and
+ * scales begin as zeros.  Rounding to nearest keeps a slowly changing state where it is (beta2 = 0.999 moves sqrt(v) by less than half
+ * a step of its code, 3 to 6 %, unless a gradient is 8 times it); RADIAL_ROUND_RANDOM rounds up with the probability of what is left over, so
+ * that a state is right on average: the magnitude's code is floor(y + u), y in steps of the code, u = (16 bits)/2^16.  The bits of
+ * value i of tensor j are the low (m) and the high half (sqrt(v)) of h(h(k ^ j) ^ i), k = h(h(h(seed) ^ seed/2^32) ^ t) by 32-bit words,
+ * h(x): x ^= x >> 16; x *= 0x9E3779B1; x ^= x >> 15; x *= 0x6A09E667; x ^= x >> 16  (for i from 2^32 on h(h(k ^ j) ^ i/2^32) takes h(k ^ j)'s place). */
+
+#define RADIAL_ROUND_NEAREST 0
+#define RADIAL_ROUND_RANDOM 1
+
+/* A tensor of n values, all its parts contiguous on the device, at any address that fits their elements. */
+typedef struct {
+  void* weight;        /* updated in place                                                              */
+  void* copy;          /* bf16, gets the updated weight rounded, or NULL                                */
+  const void* grad;
+  void* first;         /* m: float32, or E4M3 codes with scales                                         */
+  void* second;        /* v: float32, or E4M3 codes of sqrt(v) with scales                              */
+  float* first_scales; /* ceil(n/128), both NULL for float32 states                                     */
+  float* second_scales;
+  int64_t n;           /* >= 0, < 2^40                                                                  */
+  int32_t weight_type, grad_type; /* RADIAL_BF16, RADIAL_F32                                            */
+  double decay;        /* >= 0 and finite                                                               */
+} radial_adamw_tensor;
+
+/* What a table of tensors is: how many, pieces of 4096 values of all of them, bytes of the table. */
+typedef struct {
+  int32_t count;
+  int32_t pieces;
+  size_t table_bytes;
+} radial_adamw_plan_info;
+
+/* Checks `count` tensors (host memory) and says how large their table is.  Errors: EINVAL (NULL, sizes, types, scales, decay), ESHAPE
+ * (alignment, more than 2^23 pieces). */
+RADIAL_API int radial_adamw_plan(const radial_adamw_tensor* tensors, int32_t count, radial_adamw_plan_info* plan);
+
+/* Fills the table (device, 16-byte aligned, table_bytes of at least plan->table_bytes) for the calls below, which only read it.  It
+ * holds the tensors' addresses: they stay where they are as long as it is used, and nothing that is written overlaps anything else. */
+RADIAL_API int radial_adamw_table(const radial_adamw_tensor* tensors, const radial_adamw_plan_info* plan, void* table, size_t table_bytes, void* hip_stream);
+
+/* Bytes of device workspace radial_grad_norm needs (0 on invalid arguments). */
+RADIAL_API size_t radial_grad_norm_workspace(const radial_adamw_plan_info* plan);
+
+/* norm[0] <- scale |G|, the length of the vector of all gradients (squares and sums in 64 bits), norm[1] <- the factor that takes
+ * it to max_norm at most: scale min(1, max_norm/norm[0]); NaN if a gradient is not finite.
+ *   scale    : > 0, finite (1/loss scale);   max_norm : > 0 (infinity: no limit);
+ *   norm     : device float [2];   workspace : radial_grad_norm_workspace(plan) bytes, 8-byte aligned, contents ignored and undefined afterwards. */
+RADIAL_API int radial_grad_norm(const radial_adamw_plan_info* plan, const void* table, size_t table_bytes, float scale, float max_norm, float* norm,
+                                void* workspace, size_t workspace_bytes, void* hip_stream);
+
+typedef struct {
+  double lr, beta1, beta2, eps; /* lr >= 0; 0 <= beta < 1; eps > 0; all finite                                      */
+  int64_t step;                 /* t >= 1                                                                            */
+  uint64_t seed;                /* of RADIAL_ROUND_RANDOM                                                            */
+  int32_t rounding;             /* RADIAL_ROUND_*, of states in 8 bits                                              */
+  const float* factor;          /* device, or NULL (1).  While it is not finite a step changes nothing at all       */
+  const float* lr_at;           /* device, read in place of lr, or NULL                                              */
+  const int64_t* step_at;       /* device, read in place of step, or NULL: a captured step counts on in replays     */
+} radial_adamw_params;
+
+/* One step for all tensors of the table.  Errors: EINVAL, ESHAPE (alignment), EHIP. */
+RADIAL_API int radial_adamw_step(const radial_adamw_params* params, const radial_adamw_plan_info* plan, const void* table, size_t table_bytes,
+                                 void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,485 @@
+// What a tuning step does with the gradients, for gfx950: their common norm, and AdamW over many tensors in one launch, with states in float32 or in E4M3
+// codes with a scale for each 128 values.  Both are bound by memory: 28 bytes a value with float32 weights, gradients and states, 14 with states
+// in 8 bits and bf16 gradients.
+//
+// A table on the device names the tensors and, for every piece of 4096 values of one of them, which it is: a workgroup takes one piece, so that one launch
+// serves tensors of any number and size.
+#include <math.h>
+
+#include "radial_layer_common.h"
+
+namespace radial {
+namespace {
+
+constexpr int kBlock = 128;             // values that share a scale
+constexpr int kPiece = 4096;            // values of a workgroup
+constexpr int kMostPieces = 1 << 23;    // the launch's threads stay below 2^32
+constexpr int kNormGroups = 1024;       // workgroups of the norm at most: four a compute unit
+constexpr float kLargest = 448.f;       // of E4M3
+
+struct Tensor {
+  void* weight;
+  __bf16* copy;
+  const void* grad;
+  void *first, *second;
+  float *first_scales, *second_scales;
+  int64_t n;
+  float decay;
+  int32_t kind;
+};
+// bits of kind
+constexpr int kWeightF32 = 1, kGradF32 = 2, kCodes = 4;
+
+struct Piece {
+  int32_t tensor, index;
+};
+
+// The table: `count` tensors, then `pieces` pieces.
+inline size_t table_bytes_of(int64_t count, int64_t pieces) { return (size_t)count * sizeof(Tensor) + (size_t)pieces * sizeof(Piece); }
+__host__ __device__ __forceinline__ const Piece* pieces_of_table(const void* table, int32_t count) { return (const Piece*)((const Tensor*)table + count); }
+
+// ---- table ------------------------------------------------------------------------------------------
+
+constexpr int kTensorsAtOnce = 32;  // arguments of a launch, 2.6 KB
+struct TableArgs {
+  void* table;
+  int32_t count, first;
+  int32_t piece0[kTensorsAtOnce];
+  Tensor tensors[kTensorsAtOnce];
+};
+static_assert(sizeof(TableArgs) <= 4096, "arguments of a launch");
+
+__global__ void __launch_bounds__(256) write_table_kernel(TableArgs a) {
+  const int32_t i = blockIdx.x;
+  const Tensor t = a.tensors[i];
+  if (threadIdx.x == 0) ((Tensor*)a.table)[a.first + i] = t;
+  Piece* pieces = (Piece*)pieces_of_table(a.table, a.count) + a.piece0[i];
+  const int32_t count = (int32_t)((t.n + kPiece - 1) / kPiece);
+  for (int32_t p = threadIdx.x; p < count; p += 256) pieces[p] = Piece{a.first + i, p};
+}
+
+// ---- four values at a time --------------------------------------------------------------------------
+
+__device__ __forceinline__ f32x4 load_four(const float* p, int64_t count) {
+  if (count >= 4) return *(const f32x4_any*)p;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (e < count) v[e] = p[e];
+  return v;
+}
+__device__ __forceinline__ f32x4 load_four(const __bf16* p, int64_t count) {
+  if (count >= 4) {
+    const u32x2 r = *(const u32x2_any*)p;
+    return f32x4{__builtin_bit_cast(float, r[0] << 16), __builtin_bit_cast(float, r[0] & 0xffff0000u), __builtin_bit_cast(float, r[1] << 16),
+                 __builtin_bit_cast(float, r[1] & 0xffff0000u)};
+  }
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (e < count) v[e] = (float)p[e];
+  return v;
+}
+typedef uint32_t u32_byte_any __attribute__((aligned(1)));
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int64_t count) {
+  if (count >= 4) return *(const u32_byte_any*)p;
+  uint32_t v = 0;
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (e < count) v |= (uint32_t)p[e] << 8 * e;
+  return v;
+}
+__device__ __forceinline__ void store_four(float* p, f32x4 v, int64_t count) {
+  if (count >= 4) {
+    *(f32x4_any*)p = v;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (e < count) p[e] = v[e];
+}
+__device__ __forceinline__ void store_four(__bf16* p, f32x4 v, int64_t count) {
+  if (count >= 4) {
+    *(u32x2_any*)p = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (e < count) p[e] = (__bf16)v[e];
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, uint32_t v, int64_t count) {
+  if (count >= 4) {
+    *(u32_byte_any*)p = v;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (e < count) p[e] = (uint8_t)(v >> 8 * e);
+}
+
+// ---- norm -------------------------------------------------------------------------------------------
+
+// Squares and sums in 64 bits: a float32 square passes its range from 2^64 on, and 10^8 of them lose three digits.  Each workgroup writes its sum; a second launch adds
+// them up in order.
+template <class T>
+__device__ __forceinline__ double squares_of_piece(const T* g, int64_t count) {
+  f32x4 v[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int32_t at = (j * 256 + (int)threadIdx.x) * 4;
+    v[j] = load_four(g + at, count - at);
+  }
+  double sum = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum = __builtin_fma((double)v[j][e], (double)v[j][e], sum);
+  return sum;
+}
+
+__device__ __forceinline__ double block_sum(double x) {
+  __shared__ double of_wave[4];
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+  if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return (of_wave[0] + of_wave[1]) + (of_wave[2] + of_wave[3]);
+}
+
+__global__ void __launch_bounds__(256) grad_squares_kernel(const void* table, int32_t count, int32_t pieces, double* sums) {
+  const Piece* all = pieces_of_table(table, count);
+  double sum = 0;
+  for (int32_t p = blockIdx.x; p < pieces; p += gridDim.x) {
+    const Piece piece = all[p];
+    const Tensor& t = ((const Tensor*)table)[piece.tensor];
+    const int64_t at = (int64_t)piece.index * kPiece, left = t.n - at;
+    sum += t.kind & kGradF32 ? squares_of_piece((const float*)t.grad + at, left) : squares_of_piece((const __bf16*)t.grad + at, left);
+  }
+  sum = block_sum(sum);
+  if (threadIdx.x == 0) sums[blockIdx.x] = sum;
+}
+
+__global__ void __launch_bounds__(256) finish_norm_kernel(const double* sums, int32_t count, float scale, float max_norm, float* norm) {
+  double sum = 0;
+  for (int32_t i = threadIdx.x; i < count; i += 256) sum += sums[i];
+  sum = block_sum(sum);
+  if (threadIdx.x) return;
+  const double length = (double)scale * sqrt(sum);
+  norm[0] = (float)length;
+  norm[1] = !(sum <= 1.7976931348623157e308) ? __builtin_nanf("") : length > (double)max_norm ? (float)((double)scale * ((double)max_norm / length)) : scale;
+}
+
+// ---- step -------------------------------------------------------------------------------------------
+
+struct StepArgs {
+  const void* table;
+  int32_t count;
+  int32_t rounding;
+  float lr, beta1, of_grad1, beta2, of_grad2, eps, by_first, by_second;
+  double lr_wide;
+  float log_beta1, log_beta2;
+  int64_t step;
+  uint64_t seed;
+  const float* factor;
+  const float* lr_at;
+  const int64_t* step_at;
+};
+
+__host__ __device__ __forceinline__ uint32_t mixed(uint32_t x) {
+  x ^= x >> 16;
+  x *= 0x9E3779B1u;
+  x ^= x >> 15;
+  x *= 0x6A09E667u;
+  return x ^ x >> 16;
+}
+
+// The largest of each 32 neighbouring lanes, in all of them.
+__device__ __forceinline__ float max_of_32(float x) {
+  x = max_dpp<kSwapOnes>(x);
+  x = max_dpp<kSwapTwos>(x);
+  x = max_dpp<kHalfRowMirror>(x);
+  x = max_dpp<kRowMirror>(x);
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto sw = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t first = sw[0], second = sw[1];
+  return fmaxf(__builtin_bit_cast(float, first), __builtin_bit_cast(float, second));
+}
+
+__device__ __forceinline__ f32x4 decode_four(uint32_t codes, float scale) {
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+  return f32x4{lo[0] * scale, lo[1] * scale, hi[0] * scale, hi[1] * scale};
+}
+__device__ __forceinline__ uint32_t nearest_codes(f32x4 y) {
+  int v = 0;  // v_cvt_pk_fp8_f32 rounds to nearest even
+  v = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], v, false);
+  v = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], v, true);
+  return (uint32_t)v;
+}
+// Towards zero or one code further, by sixteen random bits.  Times 2^-120 E4M3's smallest normal number is float32's, so that the codes are the upper bits of the
+// product, subnormal ones too, and a carry moves on into the exponent.
+__device__ __forceinline__ uint32_t random_code(float y, uint32_t bits16) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, y), magnitude = __builtin_bit_cast(uint32_t, fabsf(y) * 0x1p-120f);
+  const uint32_t code = min((magnitude + (bits16 << 4)) >> 20, 0x7eu);
+  return (y == y ? code : 0x7fu) | (u >> 31) << 7;
+}
+
+// Codes and scale of a block's values: 32 lanes, four each.
+template <bool kPositive>
+__device__ __forceinline__ uint32_t encode_four(f32x4 v, bool random, const uint32_t (&bits)[4], float& scale) {
+  float largest = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
+  largest = max_of_32(largest);
+  scale = largest / kLargest;
+  const float inverse = largest > 0.f ? kLargest / largest : 0.f;
+  const f32x4 y = {v[0] * inverse, v[1] * inverse, v[2] * inverse, v[3] * inverse};
+  uint32_t codes;
+  if (random) {
+    codes = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) codes |= random_code(y[e], kPositive ? bits[e] >> 16 : bits[e] & 0xffffu) << 8 * e;
+  } else {
+    codes = nearest_codes(y);
+  }
+  if (kPositive) {
+    // a positive value keeps a positive code
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (v[e] > 0.f && !(codes >> 8 * e & 0xffu)) codes |= 1u << 8 * e;
+  }
+  return codes;
+}
+
+// The step of a workgroup's piece: a wave takes 1024 neighbouring values, a lane four of every 256 (so that 32 lanes are one block of 128).  Products
+// and sums are rounded one by one, as the formula is written: a state's codes then do not depend on how a compiler joins them.
+template <class W, class G, bool kCoded>
+__device__ __forceinline__ void step_piece(const StepArgs& a, const Tensor& t, Piece piece, float factor, float keep, float by_first, float by_second) {
+#pragma clang fp contract(off)
+  const int64_t first = (int64_t)piece.index * kPiece + (threadIdx.x >> 6) * 1024 + (threadIdx.x & 63) * 4;
+  const int64_t left = t.n - first;
+  f32x4 w[4], g[4], m[4], v[4];
+  uint32_t m_codes[4], v_codes[4];
+  float m_scale[4], v_scale[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t at = first + j * 256, count = left - j * 256;
+    g[j] = load_four((const G*)t.grad + at, count);
+    w[j] = load_four((const W*)t.weight + at, count);
+    if constexpr (kCoded) {
+      m_codes[j] = load_codes((const uint8_t*)t.first + at, count);
+      v_codes[j] = load_codes((const uint8_t*)t.second + at, count);
+      m_scale[j] = count > 0 ? t.first_scales[at / kBlock] : 0.f;
+      v_scale[j] = count > 0 ? t.second_scales[at / kBlock] : 0.f;
+    } else {
+      m[j] = load_four((const float*)t.first + at, count);
+      v[j] = load_four((const float*)t.second + at, count);
+    }
+  }
+  const bool random = kCoded && a.rounding == RADIAL_ROUND_RANDOM;
+  uint32_t key = 0;
+  if (random) {
+    const int64_t step = a.step_at ? *a.step_at : a.step;
+    key = mixed(mixed(mixed((uint32_t)a.seed) ^ (uint32_t)(a.seed >> 32)) ^ (uint32_t)step);
+    key = mixed(key ^ (uint32_t)piece.tensor);
+    const uint32_t far = (uint32_t)(first >> 32);
+    if (far) key = mixed(key ^ far);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t at = first + j * 256, count = left - j * 256;
+    if constexpr (kCoded) {
+      m[j] = decode_four(m_codes[j], m_scale[j]);
+      v[j] = decode_four(v_codes[j], v_scale[j]);
+      v[j] = v[j] * v[j];
+    }
+    f32x4 root;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = g[j][e] * factor;
+      m[j][e] = m[j][e] * a.beta1 + x * a.of_grad1;
+      v[j][e] = v[j][e] * a.beta2 + x * x * a.of_grad2;
+      root[e] = sqrtf(v[j][e]);
+      w[j][e] = w[j][e] * keep - by_first * (m[j][e] / (root[e] * by_second + a.eps));
+    }
+    if (count > 0) {
+      store_four((W*)t.weight + at, w[j], count);
+      if (t.copy) store_four(t.copy + at, w[j], count);
+    }
+    if constexpr (kCoded) {
+      uint32_t bits[4] = {};
+      if (random) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bits[e] = mixed(key ^ ((uint32_t)at + e));
+      }
+      if (count < 4) {
+        // what lies behind the tensor counts for nothing in its block
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e >= count) m[j][e] = root[e] = 0.f;
+      }
+      float ms, vs;
+      const uint32_t mc = encode_four<false>(m[j], random, bits, ms), vc = encode_four<true>(root, random, bits, vs);
+      if (count > 0) {
+        store_codes((uint8_t*)t.first + at, mc, count);
+        store_codes((uint8_t*)t.second + at, vc, count);
+        if ((threadIdx.x & 31) == 0) {
+          t.first_scales[at / kBlock] = ms;
+          t.second_scales[at / kBlock] = vs;
+        }
+      }
+    } else if (count > 0) {
+      store_four((float*)t.first + at, m[j], count);
+      store_four((float*)t.second + at, v[j], count);
+    }
+  }
+}
+
+__global__ void __launch_bounds__(256) adamw_step_kernel(StepArgs a) {
+  const Piece piece = pieces_of_table(a.table, a.count)[blockIdx.x];
+  const Tensor t = ((const Tensor*)a.table)[piece.tensor];
+  const float factor = a.factor ? *a.factor : 1.f;
+  if (!(fabsf(factor) < __builtin_inff())) return;
+  float lr = a.lr, by_first = a.by_first, by_second = a.by_second, keep;
+  if (a.lr_at || a.step_at) {
+    // from the device: 1 - beta^t as -(e^(t log beta) - 1), which keeps its digits where beta^t is near 1
+    if (a.lr_at) lr = *a.lr_at;
+    const float step = (float)(a.step_at ? *a.step_at : a.step);
+    by_first = lr / (a.beta1 > 0.f ? -expm1f(step * a.log_beta1) : 1.f);
+    by_second = 1.f / sqrtf(a.beta2 > 0.f ? -expm1f(step * a.log_beta2) : 1.f);
+    keep = 1.f - lr * t.decay;
+  } else {
+    keep = (float)(1.0 - a.lr_wide * (double)t.decay);
+  }
+  switch (t.kind) {
+    case 0: return step_piece<__bf16, __bf16, false>(a, t, piece, factor, keep, by_first, by_second);
+    case 1: return step_piece<float, __bf16, false>(a, t, piece, factor, keep, by_first, by_second);
+    case 2: return step_piece<__bf16, float, false>(a, t, piece, factor, keep, by_first, by_second);
+    case 3: return step_piece<float, float, false>(a, t, piece, factor, keep, by_first, by_second);
+    case 4: return step_piece<__bf16, __bf16, true>(a, t, piece, factor, keep, by_first, by_second);
+    case 5: return step_piece<float, __bf16, true>(a, t, piece, factor, keep, by_first, by_second);
+    case 6: return step_piece<__bf16, float, true>(a, t, piece, factor, keep, by_first, by_second);
+    default: return step_piece<float, float, true>(a, t, piece, factor, keep, by_first, by_second);
+  }
+}
+
+// ---- host ---------------------------------------------------------------------------------------------
+
+int check_tensor(const radial_adamw_tensor& t, int32_t i) {
+  if (t.n < 0 || t.n >= 1LL << 40) return fail(RADIAL_EINVAL, "tensor %d: n must be >= 0 and below 2^40 (got %lld)", i, (long long)t.n);
+  if (!is_type(t.weight_type) || !is_type(t.grad_type)) return fail(RADIAL_EINVAL, "tensor %d: types must be RADIAL_BF16 or RADIAL_F32", i);
+  if (!(t.decay >= 0.0 && t.decay <= 3.4028234663852886e38)) return fail(RADIAL_EINVAL, "tensor %d: decay must be >= 0 and finite", i);
+  if (!t.first_scales != !t.second_scales) return fail(RADIAL_EINVAL, "tensor %d: first_scales and second_scales go together", i);
+  if (t.n && (!t.weight || !t.grad || !t.first || !t.second)) return fail(RADIAL_EINVAL, "tensor %d: weight, grad, first or second is NULL", i);
+  const uintptr_t states = t.first_scales ? 1 : 4;
+  if ((uintptr_t)t.weight % size_of(t.weight_type) || (uintptr_t)t.grad % size_of(t.grad_type) || (uintptr_t)t.copy & 1u || (uintptr_t)t.first % states ||
+      (uintptr_t)t.second % states || ((uintptr_t)t.first_scales | (uintptr_t)t.second_scales) & 3u)
+    return fail(RADIAL_ESHAPE, "tensor %d: a pointer is not aligned to its elements", i);
+  return RADIAL_OK;
+}
+int64_t pieces_of_tensor(const radial_adamw_tensor& t) { return (t.n + kPiece - 1) / kPiece; }
+
+int check_plan(const radial_adamw_plan_info* plan, const void* table, size_t table_bytes) {
+  if (!plan) return fail(RADIAL_EINVAL, "plan is NULL");
+  if (plan->count < 1 || plan->pieces < 0 || plan->pieces > kMostPieces || plan->table_bytes != table_bytes_of(plan->count, plan->pieces))
+    return fail(RADIAL_EINVAL, "plan is not one of radial_adamw_plan");
+  if (!table || table_bytes < plan->table_bytes)
+    return fail(RADIAL_EINVAL, "table is NULL or too small: %zu bytes needed, %zu given", plan->table_bytes, table ? table_bytes : (size_t)0);
+  if ((uintptr_t)table & 15u) return fail(RADIAL_ESHAPE, "table is not 16-byte aligned");
+  return RADIAL_OK;
+}
+int32_t norm_groups(int32_t pieces) { return pieces < 1 ? 1 : pieces < kNormGroups ? pieces : kNormGroups; }
+
+}  // namespace
+}  // namespace radial
+
+using namespace radial;
+
+extern "C" int radial_adamw_plan(const radial_adamw_tensor* tensors, int32_t count, radial_adamw_plan_info* plan) {
+  if (!tensors || !plan) return fail(RADIAL_EINVAL, "tensors or plan is NULL");
+  if (count < 1) return fail(RADIAL_EINVAL, "count must be >= 1");
+  int64_t pieces = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    if (int rc = check_tensor(tensors[i], i)) return rc;
+    pieces += pieces_of_tensor(tensors[i]);
+    if (pieces > kMostPieces) return fail(RADIAL_ESHAPE, "more than 2^23 pieces of 4096 values are too many for one launch");
+  }
+  plan->count = count;
+  plan->pieces = (int32_t)pieces;
+  plan->table_bytes = table_bytes_of(count, pieces);
+  return RADIAL_OK;
+}
+
+extern "C" int radial_adamw_table(const radial_adamw_tensor* tensors, const radial_adamw_plan_info* plan, void* table, size_t table_bytes, void* hip_stream) {
+  if (!tensors) return fail(RADIAL_EINVAL, "tensors is NULL");
+  if (int rc = check_plan(plan, table, table_bytes)) return rc;
+  radial_adamw_plan_info of_tensors;
+  if (int rc = radial_adamw_plan(tensors, plan->count, &of_tensors)) return rc;
+  if (of_tensors.pieces != plan->pieces) return fail(RADIAL_EINVAL, "plan is not that of the tensors");
+  int32_t piece = 0;
+  for (int32_t first = 0; first < plan->count; first += kTensorsAtOnce) {
+    const int32_t some = plan->count - first < kTensorsAtOnce ? plan->count - first : kTensorsAtOnce;
+    TableArgs a = {};
+    a.table = table; a.count = plan->count; a.first = first;
+    for (int32_t i = 0; i < some; ++i) {
+      const radial_adamw_tensor& t = tensors[first + i];
+      const int32_t kind = (t.weight_type == RADIAL_F32 ? kWeightF32 : 0) | (t.grad_type == RADIAL_F32 ? kGradF32 : 0) | (t.first_scales ? kCodes : 0);
+      a.tensors[i] = Tensor{t.weight, (__bf16*)t.copy, t.grad, t.first, t.second, t.first_scales, t.second_scales, t.n, (float)t.decay, kind};
+      a.piece0[i] = piece;
+      piece += (int32_t)pieces_of_tensor(t);
+    }
+    write_table_kernel<<<dim3((unsigned)some), dim3(256), 0, (hipStream_t)hip_stream>>>(a);
+    RADIAL_HIP_TRY(hipGetLastError());
+  }
+  return RADIAL_OK;
+}
+
+extern "C" size_t radial_grad_norm_workspace(const radial_adamw_plan_info* plan) {
+  return !plan || plan->count < 1 || plan->pieces < 0 || plan->pieces > kMostPieces ? 0 : (size_t)norm_groups(plan->pieces) * sizeof(double);
+}
+
+extern "C" int radial_grad_norm(const radial_adamw_plan_info* plan, const void* table, size_t table_bytes, float scale, float max_norm, float* norm,
+                                void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (int rc = check_plan(plan, table, table_bytes)) return rc;
+  if (!(scale > 0.f && scale <= 3.4028234663852886e38f)) return fail(RADIAL_EINVAL, "scale must be > 0 and finite");
+  if (!(max_norm > 0.f)) return fail(RADIAL_EINVAL, "max_norm must be > 0");
+  if (!norm) return fail(RADIAL_EINVAL, "norm is NULL");
+  if ((uintptr_t)norm & 3u) return fail(RADIAL_ESHAPE, "norm is not aligned to its elements");
+  const size_t needed = radial_grad_norm_workspace(plan);
+  if (!workspace || workspace_bytes < needed) return fail(RADIAL_EINVAL, "workspace is NULL or too small: %zu bytes needed, %zu given", needed, workspace ? workspace_bytes : (size_t)0);
+  if ((uintptr_t)workspace & 7u) return fail(RADIAL_ESHAPE, "workspace is not 8-byte aligned");
+  hipStream_t stream = (hipStream_t)hip_stream;
+  const int32_t groups = norm_groups(plan->pieces);
+  grad_squares_kernel<<<dim3((unsigned)groups), dim3(256), 0, stream>>>(table, plan->count, plan->pieces, (double*)workspace);
+  RADIAL_HIP_TRY(hipGetLastError());
+  finish_norm_kernel<<<dim3(1), dim3(256), 0, stream>>>((const double*)workspace, groups, scale, max_norm, norm);
+  RADIAL_HIP_TRY(hipGetLastError());
+  return RADIAL_OK;
+}
+
+extern "C" int radial_adamw_step(const radial_adamw_params* params, const radial_adamw_plan_info* plan, const void* table, size_t table_bytes,
+                                 void* hip_stream) {
+  if (!params) return fail(RADIAL_EINVAL, "params is NULL");
+  const radial_adamw_params& p = *params;
+  constexpr double kMost = 3.4028234663852886e38;
+  if (!(p.lr >= 0.0 && p.lr <= kMost)) return fail(RADIAL_EINVAL, "lr must be >= 0 and finite");
+  if (!(p.beta1 >= 0.0 && p.beta1 < 1.0) || !(p.beta2 >= 0.0 && p.beta2 < 1.0)) return fail(RADIAL_EINVAL, "beta1 and beta2 must be >= 0 and below 1");
+  if (!((float)p.eps > 0.f && p.eps <= kMost)) return fail(RADIAL_EINVAL, "eps must be > 0 and finite in float32");
+  if (p.step < 1 && !p.step_at) return fail(RADIAL_EINVAL, "step must be >= 1");
+  if (p.rounding != RADIAL_ROUND_NEAREST && p.rounding != RADIAL_ROUND_RANDOM)
+    return fail(RADIAL_EINVAL, "rounding must be RADIAL_ROUND_NEAREST or RADIAL_ROUND_RANDOM (got %d)", p.rounding);
+  if (((uintptr_t)p.factor | (uintptr_t)p.lr_at) & 3u || (uintptr_t)p.step_at & 7u) return fail(RADIAL_ESHAPE, "factor, lr_at or step_at is not aligned to its element");
+  if (int rc = check_plan(plan, table, table_bytes)) return rc;
+  if (!plan->pieces) return RADIAL_OK;
+  const double step = (double)(p.step < 1 ? 1 : p.step);
+  StepArgs a = {};
+  a.table = table; a.count = plan->count; a.rounding = p.rounding;
+  a.lr = (float)p.lr; a.lr_wide = p.lr; a.eps = (float)p.eps;
+  a.beta1 = (float)p.beta1; a.of_grad1 = (float)(1.0 - p.beta1);
+  a.beta2 = (float)p.beta2; a.of_grad2 = (float)(1.0 - p.beta2);
+  a.by_first = (float)(p.lr / (1.0 - pow(p.beta1, step)));
+  a.by_second = (float)(1.0 / sqrt(1.0 - pow(p.beta2, step)));
+  a.log_beta1 = p.beta1 > 0.0 ? (float)log(p.beta1) : 0.f;
+  a.log_beta2 = p.beta2 > 0.0 ? (float)log(p.beta2) : 0.f;
+  a.step = p.step; a.seed = p.seed; a.factor = p.factor; a.lr_at = p.lr_at; a.step_at = p.step_at;
+  adamw_step_kernel<<<dim3((unsigned)plan->pieces), dim3(256), 0, (hipStream_t)hip_stream>>>(a);
+  RADIAL_HIP_TRY(hipGetLastError());
+  return RADIAL_OK;
+}

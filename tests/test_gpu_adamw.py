@@ -1,0 +1,349 @@
+"""AdamW over many tensors and the norm of their gradients, against the oracle (run with -m gpu).
+
+Bounds.  u = 2^-24, the rounding of a float32 operation.  m: g factor, two constants, two products and their sum, at most 6u (|beta1 m| + |(1 - beta1) g|) =: em;
+v: likewise one product more, ev = 8u v.  The root takes u and half of ev, its product with a constant 2u, the sum with eps u, so the denominator d is off by
+8u d; the update c m/d (c with its rounding, division, product) by c/d (em + 11u |m|) and its square terms, 12u; the weight's product 2u |w|, the difference u.
+States in 8 bits: float32 operations one by one give the same bits in numpy, so codes and scales are equal."""
+import numpy as np
+import pytest
+import torch
+
+from layer_util import DEV, HALF_STEP, U32, assert_within, to64
+from oracle import layer as ol
+from oracle import step as os_
+from paper_2506_19852_amd import layer as rl
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+GUARD = 7.5
+LR, BETA1, BETA2, EPS = 3e-3, 0.9, 0.999, 1e-8
+
+
+class Group:
+    """Tensors of the given sizes one behind the other, `lead` elements into buffers with a guard on both sides."""
+
+    def __init__(self, sizes, weight=F32, grad=F32, coded=False, copy=False, decay=0.1, lead=1, seed=1, gap=0):
+        g = np.random.default_rng(seed)
+        self.sizes, self.coded, self.decay, self.copied = sizes, coded, decay, copy
+        self.whole, self.views = {}, {}
+
+        def lay(name, parts, dtype):
+            total = sum(len(p) + gap for p in parts) + 2 * lead + 4
+            fill = 0xA5 if dtype is torch.uint8 else GUARD
+            whole = torch.full((total,), fill, dtype=dtype, device=DEV)
+            at, views = lead, []
+            for p in parts:
+                view = whole[at:at + len(p)]
+                view.copy_(torch.as_tensor(p).to(dtype))
+                views.append(view)
+                at += len(p) + gap
+            self.whole[name], self.views[name] = whole, views
+
+        spread = [np.exp(g.normal(size=n) * 2) * 1e-3 for n in sizes]
+        lay("w", [g.normal(size=n) * 0.02 for n in sizes], weight)
+        lay("g", [g.normal(size=n) * s for n, s in zip(sizes, spread)], grad)
+        m, r = [0.3 * g.normal(size=n) * s for n, s in zip(sizes, spread)], [(0.1 + np.abs(g.normal(size=n))) * s for n, s in zip(sizes, spread)]
+        if coded:
+            for name, parts, positive in (("m", m, False), ("v", r, True)):
+                codes = [os_.encode(p.astype(np.float32), positive=positive) for p in parts]
+                lay(name, [c for c, _ in codes], torch.uint8)
+                lay(name + "s", [s for _, s in codes], F32)
+        else:
+            lay("m", m, F32)
+            lay("v", [x * x for x in r], F32)
+        if copy:
+            lay("c", [np.zeros(n) for n in sizes], BF16)
+        v = self.views
+        self.tensors = rl.adamw_tensors(v["w"], v["g"], v["m"], v["v"], first_scales=v.get("ms"), second_scales=v.get("vs"), copies=v.get("c"), decay=decay)
+        self.plan = rl.radial_adamw_plan(self.tensors)
+        self.table = torch.full((self.plan.table_bytes,), 255, dtype=torch.uint8, device=DEV)
+        rl.radial_adamw_table(self.tensors, self.plan, self.table)
+        self.norm = torch.full((2,), float("nan"), device=DEV)
+        self.work = torch.full((rl.radial_grad_norm_workspace(self.plan),), 255, dtype=torch.uint8, device=DEV)
+
+    def step(self, **kw):
+        rl.radial_adamw_step(self.plan, self.table, **{**dict(lr=LR, step=7, beta1=BETA1, beta2=BETA2, eps=EPS), **kw})
+
+    def grad_norm(self, **kw):
+        rl.radial_grad_norm(self.plan, self.table, self.norm, self.work, **kw)
+
+    def read(self):
+        return {k: [t.detach().cpu().clone() for t in v] for k, v in self.views.items()}
+
+    def guards_kept(self):
+        for name, whole in self.whole.items():
+            rest = whole.clone()
+            for t in self.views[name]:
+                at = (t.data_ptr() - whole.data_ptr()) // whole.element_size()
+                rest[at:at + len(t)] = 0xA5 if whole.dtype is torch.uint8 else GUARD
+            if not bool((rest == (0xA5 if whole.dtype is torch.uint8 else GUARD)).all()):
+                return False
+        return True
+
+
+def check(group, before, after, factor=np.float32(1), lr=LR, step=7, beta1=BETA1, beta2=BETA2, eps=EPS, rounding="nearest", seed=0, more=0.0):
+    """`more`: what by_first and by_second may be off besides, relative."""
+    decays = group.decay if isinstance(group.decay, list) else [group.decay] * len(group.sizes)
+    for i, n in enumerate(group.sizes):
+        if not n:
+            continue
+        of = lambda k: before[k][i].double().numpy()  # noqa: B023, E731
+        got = lambda k: after[k][i].double().numpy()  # noqa: B023, E731
+        w, g = of("w"), of("g") * np.float64(factor)
+        if group.coded:
+            x = (before["g"][i].float().numpy() * np.float32(factor)).astype(np.float32)
+            m32 = os_.decode(before["m"][i].numpy(), before["ms"][i].numpy(), np.float32)
+            r32 = os_.decode(before["v"][i].numpy(), before["vs"][i].numpy(), np.float32)
+            m1, v1 = os_.moments(x, m32, r32 * r32, beta1, beta2)
+            assert m1.dtype == v1.dtype == np.float32
+            r1 = np.sqrt(v1)
+            bits = os_.random_bits(seed, step, i, n) if rounding == "random" else (None, None)
+            for name, value, b, positive in (("m", m1, bits[0], False), ("v", r1, bits[1], True)):
+                codes, scales = os_.encode(value, b, positive)
+                assert np.array_equal(after[name + "s"][i].numpy(), scales), (name, i)
+                assert np.array_equal(after[name][i].numpy(), codes), (name, i, (after[name][i].numpy() != codes).sum())
+            m0, v0 = m32.astype(np.float64), np.square(r32.astype(np.float64))
+        else:
+            m0, v0 = of("m"), of("v")
+        m, v = os_.moments(g, m0, v0, beta1, beta2)
+        em = 6 * U32 * (np.abs(beta1 * m0) + np.abs((1 - beta1) * g)) + 1e-44
+        if not group.coded:
+            assert_within(got("m"), m, em, f"m {i}")
+            assert_within(got("v"), v, 8 * U32 * v + 1e-44, f"v {i}")
+        want = os_.update(w, m, v, lr, step, beta1, beta2, eps, decays[i])
+        c = lr / (1 - beta1 ** step)
+        d = np.sqrt(v / (1 - beta2 ** step)) + eps
+        off = c / d * (em + (12 * U32 + 2 * more) * np.abs(m)) + 3 * U32 * np.abs(w) + U32 * np.abs(want)
+        dtype = group.views["w"][i].dtype
+        assert_within(got("w"), want, off + (HALF_STEP[BF16] * (np.abs(want) + off) if dtype is BF16 else 0), f"w {i}")
+        if group.copied:
+            assert_within(got("c"), want, off + HALF_STEP[BF16] * (np.abs(want) + off), f"copy {i}")
+            if dtype is F32:
+                assert torch.equal(after["c"][i], after["w"][i].to(BF16))
+        assert torch.equal(before["g"][i], after["g"][i])
+    assert group.guards_kept()
+
+
+SIZES = [[1], [3, 1, 130, 127, 128, 129], [5120], [4095, 4096, 4097, 8193], [0, 5, 0, 700], [100_003]]
+
+
+@pytest.mark.parametrize("weight, grad", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)], ids=["f32-f32", "f32-bf16", "bf16-f32", "bf16-bf16"])
+@pytest.mark.parametrize("states", ["f32", "8bit", "random"])
+@pytest.mark.parametrize("sizes", SIZES, ids=str)
+def test_step(sizes, states, weight, grad):
+    for lead, gap, copy in ((1, 0, True), (4, 3, False)):
+        group = Group(sizes, weight, grad, states != "f32", copy, lead=lead, gap=gap)
+        before = group.read()
+        rounding = "random" if states == "random" else "nearest"
+        group.step(rounding=rounding, seed=0x123456789ABCDEF)
+        check(group, before, group.read(), rounding=rounding, seed=0x123456789ABCDEF)
+
+
+@pytest.mark.parametrize("coded", [False, True], ids=["f32", "8bit"])
+def test_many_tensors_with_decays_of_their_own_clipped(coded):
+    sizes = [37 * i % 5000 + 1 for i in range(200)]
+    group = Group(sizes, coded=coded, decay=[0.01 * (i % 3) for i in range(200)], copy=True)
+    before = group.read()
+    group.grad_norm(max_norm=0.25, scale=0.5)
+    group.step(factor=group.norm, step=1)
+    torch.cuda.synchronize()
+    norm, factor = group.norm.cpu().numpy()
+    length = 0.5 * np.sqrt(sum(float((g.double() ** 2).sum()) for g in before["g"]))
+    assert length > 0.25 and abs(norm - length) <= 2 * U32 * length and abs(factor - 0.5 * 0.25 / length) <= 2 * U32 * factor
+    check(group, before, group.read(), factor=factor, step=1)
+
+
+@pytest.mark.parametrize("params", [dict(beta1=0.0), dict(beta2=0.0), dict(lr=0.0), dict(step=1), dict(step=10 ** 9), dict(eps=1e-3, beta2=0.95), dict(beta1=0.0, beta2=0.0, step=1)], ids=str)
+def test_parameters(params):
+    for coded in (False, True):
+        group = Group([300, 4100], coded=coded)
+        before = group.read()
+        group.step(**params)
+        check(group, before, group.read(), **params)
+
+
+def test_states_that_begin_as_zeros():
+    group = Group([1000], coded=True)
+    for k in ("m", "v", "ms", "vs"):
+        group.views[k][0].zero_()
+    group.views["g"][0][:128] = 0    # a block without any gradient: weights stay but for their decay
+    before = group.read()
+    group.step(step=1)
+    after = group.read()
+    check(group, before, after, step=1)
+    assert not after["m"][0][:128].any() and not after["vs"][0][:1].any()
+
+
+def test_a_small_root_beside_a_large_one_is_not_lost():
+    """The next step divides by the root: it is the smallest code at least, and the update stays below what that allows."""
+    group = Group([128], coded=True, decay=0.0)
+    for k in ("m", "v", "ms", "vs"):
+        group.views[k][0].zero_()
+    group.views["g"][0].fill_(1e-9)
+    group.views["g"][0][5] = 1.0
+    group.step(step=1)
+    assert bool((group.views["v"][0] >= 1).all())
+    before = group.read()
+    group.step(step=2)
+    check(group, before, group.read(), step=2)
+    moved = (group.views["w"][0].cpu() - before["w"][0]).abs().max()
+    assert moved <= 1.1 * LR
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")], ids=str)
+def test_gradients_that_are_not_finite_change_nothing_behind_their_norm(bad):
+    for coded in (False, True):
+        group = Group([100, 5000], coded=coded, copy=True)
+        group.views["g"][1][4321] = bad
+        before = group.read()
+        group.grad_norm(max_norm=1.0)
+        group.step(factor=group.norm)
+        torch.cuda.synchronize()
+        assert not np.isfinite(float(group.norm[0])) and np.isnan(float(group.norm[1]))
+        after = group.read()
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for k in before for a, b in zip(before[k], after[k]))
+
+
+def test_a_gradient_of_nan_without_a_norm_stays_in_its_value_or_block():
+    for coded in (False, True):
+        group = Group([600], coded=coded)
+        group.views["g"][0][300] = float("nan")
+        group.step()
+        after = group.read()
+        w = after["w"][0]
+        assert w.isnan().sum() == 1 and w[300].isnan()
+        if coded:
+            assert np.isnan(ol.e4m3_values()[after["m"][0].numpy()]).sum() == 1 and torch.isfinite(after["ms"][0]).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("sizes", SIZES + [[7] * 3000, [9_000_001]], ids=lambda s: str(s)[:40])
+def test_norm(sizes, dtype):
+    group = Group(sizes, grad=dtype)
+    group.grad_norm()
+    want = np.sqrt(sum(float((g.double() ** 2).sum()) for g in group.read()["g"]))
+    norm, factor = to64(group.norm)
+    assert abs(norm - want) <= U32 * want * (1 + 1e-6) and factor == 1.0
+    group.grad_norm(max_norm=want * 2, scale=1.5)
+    norm, factor = to64(group.norm)
+    assert abs(norm - 1.5 * want) <= U32 * 1.5 * want * (1 + 1e-6) and factor == 1.5
+    assert group.guards_kept()
+
+
+def test_norm_of_values_whose_squares_leave_float32():
+    group = Group([1000])
+    group.views["g"][0].fill_(1e30)
+    group.grad_norm(max_norm=1.0)
+    norm, factor = to64(group.norm)
+    want = float(np.float32(1e30)) * np.sqrt(1000)
+    assert abs(norm - want) <= U32 * want and abs(factor * want - 1) <= 2 * U32
+    group.views["g"][0].zero_()
+    group.grad_norm(max_norm=1.0)
+    assert to64(group.norm).tolist() == [0.0, 1.0]
+
+
+def test_rounding_at_random_is_right_on_average():
+    """The mean of what the codes of 400 seeds stand for: each is off by less than a step of the code, with a variance below (step/2)^2; five standard deviations."""
+    n, seeds = 512, 400
+    group = Group([n], coded=True, decay=0.0)
+    before = group.read()
+    total = {"m": np.zeros(n), "v": np.zeros(n)}
+    for seed in range(seeds):
+        for k, v in before.items():
+            group.views[k][0].copy_(v[0])
+        group.step(rounding="random", seed=seed)
+        after = group.read()
+        for k in total:
+            total[k] += os_.decode(after[k][0].numpy(), after[k + "s"][0].numpy())
+    m0, r0 = (os_.decode(before[k][0].numpy(), before[k + "s"][0].numpy()) for k in ("m", "v"))
+    m, v = os_.moments(before["g"][0].double().numpy(), m0, r0 ** 2, BETA1, BETA2)
+    for k, want in (("m", m), ("v", np.sqrt(v))):
+        scale = np.repeat(after[k + "s"][0].double().numpy(), 128)[:n]
+        step = np.maximum(np.abs(want) * 2.0 ** -3, scale * 2.0 ** -9)
+        away = np.abs(total[k] / seeds - want)
+        assert (away <= 5 * step / 2 / np.sqrt(seeds) + step * 2.0 ** -15).mean() > 0.999, k
+    # nearest leaves most roots where they are
+    for k, v in before.items():
+        group.views[k][0].copy_(v[0])
+    group.views["g"][0].zero_()
+    group.step()
+    assert (group.read()["v"][0] == before["v"][0]).double().mean() > 0.99
+
+
+def test_random_bits_are_spread_evenly():
+    """Bits of the definition: each of 16 values of the upper four bits of either half, within five standard deviations, for neighbours, tensors and steps."""
+    for seed, step, tensor in ((0, 1, 0), (0, 2, 0), (0, 1, 1), (1 << 40, 1, 0)):
+        for half in os_.random_bits(seed, step, tensor, 1 << 16):
+            counts = np.bincount(half >> 12, minlength=16)
+            assert np.abs(counts - 4096).max() <= 5 * np.sqrt(4096)
+    a, b = os_.random_bits(0, 1, 0, 1 << 16)
+    assert abs(np.corrcoef(a, b)[0, 1]) <= 5 / 256 and abs(np.corrcoef(a[1:], a[:-1])[0, 1]) <= 5 / 256
+
+
+def test_step_and_rate_from_the_device_captured_and_replayed():
+    """A captured clipped step whose number counts on: every replay is the eager step of its number, also with other work between."""
+    lr, t = torch.tensor([LR], device=DEV), torch.tensor([0], device=DEV)
+    for coded in (False, True):
+        t.fill_(0)
+        group, eager = Group([300, 5000], coded=coded, copy=True), Group([300, 5000], coded=coded, copy=True)
+        how = dict(lr_at=lr, step_at=t, rounding="random" if coded else "nearest", seed=5)
+
+        def one(x):
+            x.grad_norm(max_norm=0.1)
+            x.step(factor=x.norm, **how)
+
+        warm = Group([300, 5000], coded=coded, copy=True)
+        t.add_(1)
+        one(warm)
+        t.fill_(0)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            t.add_(1)
+            one(group)
+        for turn in range(1, 5):
+            for x in (group, eager):
+                x.views["g"][0].mul_(1.5)
+            before = eager.read()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert int(t) == turn
+            one(eager)
+            torch.cuda.synchronize()
+            a, b = group.read(), eager.read()
+            assert all(torch.equal(p, q) for k in a for p, q in zip(a[k], b[k])), turn
+            # e^x - 1 in float32: two units of its own and the rounding of x, log beta and their product
+            check(eager, before, b, factor=eager.norm[1].cpu().numpy(), step=turn, rounding=how["rounding"], seed=5, more=6 * U32)
+            lr.mul_(1.0)
+
+
+def test_on_a_busy_stream_of_its_own():
+    for by_argument in (True, False):
+        group, eager = Group([9000]), Group([9000])
+        eager.grad_norm(max_norm=0.1)
+        eager.step(factor=eager.norm)
+        group.views["g"][0].mul_(2.0)
+        busy = torch.zeros(1 << 28, device=DEV)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            for _ in range(30):
+                busy.add_(1.0)
+            group.views["g"][0].mul_(0.5)
+            if not by_argument:
+                group.grad_norm(max_norm=0.1)
+                group.step(factor=group.norm)
+        if by_argument:
+            group.grad_norm(max_norm=0.1, stream=side)
+            group.step(factor=group.norm, stream=side)
+        side.synchronize()
+        a, b = group.read(), eager.read()
+        assert all(torch.equal(p, q) for k in a for p, q in zip(a[k], b[k]))
+
+
+def test_a_table_of_no_values():
+    group = Group([0, 0])
+    group.grad_norm(max_norm=1.0)
+    group.step(factor=group.norm)
+    torch.cuda.synchronize()
+    assert group.plan.pieces == 0 and to64(group.norm).tolist() == [0.0, 1.0] and group.guards_kept()
