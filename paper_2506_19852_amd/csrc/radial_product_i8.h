@@ -15,9 +15,9 @@ constexpr int32_t kMostCodeCols = 1 << 23;
 constexpr int32_t kExactCols = 131071;         // products of up to 2^14 each, summed below 2^31
 inline int64_t code_groups(int64_t n) { return (n + kCodeGroup - 1) / kCodeGroup; }
 
-inline int check_matrix(const void* p, int32_t type, int64_t stride, int64_t cols, const char* name, const char* stride_name, const char* cols_name) {
+inline int check_matrix(const void* p, int32_t type, int64_t stride, int64_t cols, const char* name) {
   if ((uintptr_t)p % size_of(type)) return fail(RADIAL_ESHAPE, "%s is not aligned to its elements", name);
-  if (stride < cols) return fail(RADIAL_ESHAPE, "%s must not be below %s", stride_name, cols_name);
+  if (stride < cols) return fail(RADIAL_ESHAPE, "the stride of %s must not be below its columns", name);
   return RADIAL_OK;
 }
 inline int check_workspace(const void* workspace, size_t bytes, size_t needed) {

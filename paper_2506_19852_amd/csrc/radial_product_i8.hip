@@ -357,7 +357,7 @@ int check_out(const void* out, int32_t type, int64_t stride, int64_t cols, int64
   if (accumulate && type != RADIAL_F32) return fail(RADIAL_EINVAL, "%s has to be float32 to be added to", name);
   if (depth > kExactCols && type != RADIAL_F32)
     return fail(RADIAL_EUNSUPPORTED, "sums of more than 131071 products are taken in parts: %s has to be float32", name);
-  return check_matrix(out, type, stride, cols, name, "its stride", "its columns");
+  return check_matrix(out, type, stride, cols, name);
 }
 int check_floats(const void* p, const char* name) {
   return (uintptr_t)p & 3u ? fail(RADIAL_ESHAPE, "%s is not aligned to its elements", name) : RADIAL_OK;
@@ -424,7 +424,7 @@ extern "C" int radial_linear_i8_fwd(int32_t M, int32_t N, int32_t K, const void*
   if (int rc = check_sizes(M, N, K)) return rc;
   if (!x) return fail(RADIAL_EINVAL, "x is NULL");
   if (!is_type(type)) return fail(RADIAL_EINVAL, "type must be RADIAL_BF16 or RADIAL_F32 (got %d)", type);
-  if (int rc = check_matrix(x, type, x_stride, K, "x", "x_stride", "K")) return rc;
+  if (int rc = check_matrix(x, type, x_stride, K, "x")) return rc;
   if (int rc = check_codes(w_codes, w_scales, "w")) return rc;
   if (int rc = check_out(y, y_type, y_stride, N, K, false, "y")) return rc;
   if (int rc = check_floats(bias, "bias")) return rc;
@@ -452,7 +452,7 @@ extern "C" int radial_linear_i8_bwd(int32_t M, int32_t N, int32_t K, const void*
     return fail(RADIAL_ESHAPE, "M and N must be at most 2^23 and K 2^29: larger ones are too large for one launch");
   if (!dy) return fail(RADIAL_EINVAL, "dy is NULL");
   if (!is_type(type)) return fail(RADIAL_EINVAL, "type must be RADIAL_BF16 or RADIAL_F32 (got %d)", type);
-  if (int rc = check_matrix(dy, type, dy_stride, N, "dy", "dy_stride", "N")) return rc;
+  if (int rc = check_matrix(dy, type, dy_stride, N, "dy")) return rc;
   if (!dx && !dw && !dbias) return fail(RADIAL_EINVAL, "none of dx, dw and dbias is given");
   const bool add = accumulate != 0;
   if (dx) {
@@ -461,7 +461,7 @@ extern "C" int radial_linear_i8_bwd(int32_t M, int32_t N, int32_t K, const void*
   }
   if (dw) {
     if (!x) return fail(RADIAL_EINVAL, "x is NULL");
-    if (int rc = check_matrix(x, type, x_stride, K, "x", "x_stride", "K")) return rc;
+    if (int rc = check_matrix(x, type, x_stride, K, "x")) return rc;
     if (int rc = check_out(dw, dw_type, dw_stride, K, M, add, "dw")) return rc;
   }
   if (int rc = check_floats(dbias, "dbias")) return rc;

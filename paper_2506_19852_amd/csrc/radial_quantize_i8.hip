@@ -290,7 +290,7 @@ extern "C" int radial_quantize_rows_i8(int32_t rows, int32_t cols, const void* x
   if (!codes != !scales || !codes_t != !scales_t) return fail(RADIAL_EINVAL, "codes and scales go together");
   if (!codes && !codes_t && !sums_t) return fail(RADIAL_EINVAL, "none of codes, codes_t and sums_t is given");
   if (rows > kMostCodeRows || cols > kMostCodeRows) return fail(RADIAL_ESHAPE, "rows and cols must be at most 2^29: x is too large for one launch");
-  if (int rc = check_matrix(x, type, stride, cols, "x", "stride", "cols")) return rc;
+  if (int rc = check_matrix(x, type, stride, cols, "x")) return rc;
   if (((uintptr_t)codes | (uintptr_t)codes_t) & 15u) return fail(RADIAL_ESHAPE, "codes are not 16-byte aligned");
   if (((uintptr_t)scales | (uintptr_t)scales_t | (uintptr_t)sums_t) & 3u) return fail(RADIAL_ESHAPE, "scales or sums_t are not aligned to their elements");
   if (codes_t || sums_t) {

@@ -535,9 +535,9 @@ def adamw_tensors(weights, grads, firsts, seconds, *, first_scales=None, second_
     lists = [of_tensors(v, name) for v, name in ((grads, "grads"), (firsts, "firsts"), (seconds, "seconds"), (first_scales, "first_scales"),
                                                  (second_scales, "second_scales"), (copies, "copies"), (decay, "decay"))]
     for i, (w, g, m, v, ms, vs, copy, by) in enumerate(zip(weights, *lists)):
-        n = w.numel()
+        n = w.numel() if w is not None else 0   # refused below
         e = out[i]
-        e.n, e.weight_type, e.grad_type, e.decay = n, _types.get(w.dtype, -1), _types.get(getattr(g, "dtype", None), -1), by
+        e.n, e.weight_type, e.grad_type, e.decay = n, _types.get(getattr(w, "dtype", None), -1), _types.get(getattr(g, "dtype", None), -1), by
         e.weight = part(w, f"weight {i}", n, (_bf16, _f32))
         e.grad = part(g, f"gradient {i}", n, (_bf16, _f32), False)
         coded = ms is not None or vs is not None
