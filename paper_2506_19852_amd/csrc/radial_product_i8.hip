@@ -5,7 +5,7 @@
 #include <type_traits>
 
 #include "radial_product_i8.h"
-#include "radial_product_rule.h"
+#include "radial_product_i8_rule.h"
 
 namespace radial {
 namespace {
@@ -17,7 +17,7 @@ struct ProductArgs {
   const float *sa, *sb, *bias;
   void* out;
   int64_t out_stride;
-  int64_t a_bytes, b_bytes;  // of a row
+  int64_t a_row, a_group, b_row, b_group;  // bytes from a row, a group of a row to the next
   int32_t M, N, groups;
   int32_t out_type, accumulate;
 };
@@ -66,25 +66,13 @@ __device__ __forceinline__ void put(const ProductArgs& a, int32_t m, int32_t n, 
   }
 }
 
-// Up to 16 rows, or few results: a workgroup of 8 waves takes 16 x 16 of C, each wave every 8th group, straight from memory (a lane's 32 bytes of a row, four
+// Few rows, or few results: a workgroup of 8 waves takes 16 x 16 of C, each wave every 8th group, straight from memory (a lane's 32 bytes of a row, four
 // lanes a line); the parts meet in LDS.
 constexpr int kParts = 8;
-__global__ void __launch_bounds__(64 * kParts) product_i8_pieces_kernel(ProductArgs a) {
-  __shared__ i32x4v parts[kParts][64];
+
+// The sums of the parts, scaled: wave 0 holds them, column n0 + 4 (lane / 16) on, row m.
+__device__ __forceinline__ void join_parts(const ProductArgs& a, i32x4v (&parts)[kParts][64], i32x4v sum, int32_t m, int32_t n0, float sa) {
   const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int32_t m0, n0;
-  tile_of(blockIdx.x, (a.M + 15) / 16, (a.N + 15) / 16, m0, n0);
-  m0 *= 16;
-  n0 *= 16;
-  const int32_t m = m0 + (lane & 15);
-  const int8_t* b_row = a.b + min(n0 + (lane & 15), a.N - 1) * a.b_bytes + (lane >> 4) * 32;
-  const int8_t* a_row = a.a + min(m, a.M - 1) * a.a_bytes + (lane >> 4) * 32;
-  i32x4v sum = {0, 0, 0, 0};
-  for (int32_t g = wave; g < a.groups; g += kParts) {
-    const int64_t at = (int64_t)g * kCodeGroup;
-    sum = multiply(*(const u32x4*)(b_row + at), *(const u32x4*)(a_row + at), sum);
-    sum = multiply(*(const u32x4*)(b_row + at + 16), *(const u32x4*)(a_row + at + 16), sum);
-  }
   parts[wave][lane] = sum;
   __syncthreads();
   if (wave) return;
@@ -92,20 +80,112 @@ __global__ void __launch_bounds__(64 * kParts) product_i8_pieces_kernel(ProductA
   for (int w = 1; w < kParts; ++w) sum += parts[w][lane];
   const int32_t n = n0 + 4 * (lane >> 4);
   if (m >= a.M) return;
-  const float sa = a.sa[m];
   float y[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) y[e] = result(sum[e], sa * a.sb[min(n + e, a.N - 1)], a.bias ? a.bias[min(n + e, a.N - 1)] : 0.f);
   put(a, m, n, y, a.N - n);
 }
 
-// Many rows: a workgroup takes a tile of 16 kMTiles kWavesM x 64 kNQuads kWavesN, stage by stage of one group (128 bytes of every row), which copies put into LDS
+__global__ void __launch_bounds__(64 * kParts) product_i8_pieces_kernel(ProductArgs a) {
+  __shared__ i32x4v parts[kParts][64];
+  const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int32_t m0, n0;
+  tile_of(blockIdx.x, (a.M + 15) / 16, (a.N + 15) / 16, m0, n0);
+  m0 *= 16;
+  n0 *= 16;
+  const int32_t m = m0 + (lane & 15), row = min(m, a.M - 1);
+  const int8_t* b_row = a.b + min(n0 + (lane & 15), a.N - 1) * a.b_row + (lane >> 4) * 32;
+  const int8_t* a_row = a.a + row * a.a_row + (lane >> 4) * 32;
+  i32x4v sum = {0, 0, 0, 0};
+  for (int32_t g = wave; g < a.groups; g += kParts) {
+    const int8_t *b = b_row + g * a.b_group, *of_a = a_row + g * a.a_group;
+    sum = multiply(*(const u32x4*)b, *(const u32x4*)of_a, sum);
+    sum = multiply(*(const u32x4*)(b + 16), *(const u32x4*)(of_a + 16), sum);
+  }
+  join_parts(a, parts, sum, m, n0, a.sa[row]);
+}
+
+// A projection of up to 4 rows of up to 8192 columns in one launch: every workgroup quantises the rows for itself, into LDS, while the first groups of its weights are under
+// way, and goes on as above.
+constexpr int kFewRows = 4, kFewCols = 8192, kUnderWay = 5;
+template <class T, int kRows>
+__global__ void __launch_bounds__(64 * kParts) linear_i8_few_kernel(ProductArgs a, const T* x, int64_t stride, int32_t cols) {
+  constexpr int kPieces = kFewCols / (64 * kParts * 8);  // of eight columns of a thread
+  __shared__ i32x4v parts[kParts][64];
+  __shared__ __align__(16) int8_t codes[kRows][kFewCols];
+  __shared__ uint32_t of_wave[kRows][kParts];
+  const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n0 = blockIdx.x * 16;
+  const int8_t* b_row = a.b + min(n0 + (lane & 15), a.N - 1) * a.b_row + (lane >> 4) * 32;
+  Eight<T> held[kRows][kPieces];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r)
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      const int32_t c = (p * 64 * kParts + (int32_t)threadIdx.x) * 8;
+      held[r][p].load_some(x + min(r, a.M - 1) * stride + c, cols - c);
+    }
+  u32x4 under_way[kUnderWay][2];
+#pragma unroll
+  for (int i = 0; i < kUnderWay; ++i) {
+    const int8_t* b = b_row + min(wave + i * kParts, a.groups - 1) * a.b_group;
+    under_way[i][0] = *(const u32x4*)b;
+    under_way[i][1] = *(const u32x4*)(b + 16);
+  }
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    uint32_t largest = 0;
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      float v[8];
+      held[r][p].get(v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) largest = max(largest, magnitude(v[j]));
+    }
+    largest = wave_max(largest);
+    if (lane == 0) of_wave[r][wave] = largest;
+  }
+  __syncthreads();
+  const int32_t mine = min(lane & 15, kRows - 1);
+  float sa = 0.f;
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    uint32_t largest = 0;
+#pragma unroll
+    for (int w = 0; w < kParts; ++w) largest = max(largest, of_wave[r][w]);
+    const Code code(largest);
+    if (r == mine) sa = code.scale;
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      float v[8];
+      held[r][p].get(v);
+      *(u32x2*)&codes[r][(p * 64 * kParts + threadIdx.x) * 8] = u32x2{code.four(v[0], v[1], v[2], v[3]), code.four(v[4], v[5], v[6], v[7])};
+    }
+  }
+  __syncthreads();
+  i32x4v sum = {0, 0, 0, 0};
+  auto add = [&](int32_t g, const u32x4 (&column)[2]) __attribute__((always_inline)) {
+    const int8_t* of_a = &codes[mine][g * kCodeGroup + (lane >> 4) * 32];
+    sum = multiply(column[0], *(const u32x4*)of_a, sum);
+    sum = multiply(column[1], *(const u32x4*)(of_a + 16), sum);
+  };
+#pragma unroll
+  for (int i = 0; i < kUnderWay; ++i)
+    if (wave + i * kParts < a.groups) add(wave + i * kParts, under_way[i]);
+  for (int32_t g = wave + kUnderWay * kParts; g < a.groups; g += kParts) {
+    const int8_t* b = b_row + g * a.b_group;
+    const u32x4 column[2] = {*(const u32x4*)b, *(const u32x4*)(b + 16)};
+    add(g, column);
+  }
+  join_parts(a, parts, sum, lane & 15, n0, sa);
+}
+
+// Many rows: a workgroup takes a tile of 16 kMTiles kWavesM x 64 kWavesN, stage by stage of one group (128 bytes of every row), which copies put into LDS
 // kStages - 1 stages ahead, straight from memory.  kSplit parts of the workgroup's waves take the groups in turn and add up their sums at the end.
-template <int kWavesM, int kWavesN, int kMTiles, int kNQuads, int kStages, int kSplit>
+template <int kWavesM, int kWavesN, int kMTiles, int kStages, int kSplit>
 struct TileShape {
   static constexpr int kWaves = kWavesM * kWavesN;  // of one part of the groups
-  static constexpr int kTileM = 16 * kMTiles * kWavesM, kTileN = 64 * kNQuads * kWavesN;
-  static constexpr int kNTiles = 4 * kNQuads;
+  static constexpr int kTileM = 16 * kMTiles * kWavesM, kTileN = 64 * kWavesN;
+  static constexpr int kNTiles = 4;
   static constexpr int kStage = (kTileM + kTileN) * kCodeGroup;                  // bytes of a stage: rows of A, then of B, 128 each
   static constexpr int kCopies = kStage / 1024 / kWaves;                         // of a wave
   static constexpr int kRing = kStages * kStage;                                 // of one part
@@ -120,9 +200,9 @@ struct TileShape {
 template <int kLeft>
 __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLeft) : "memory"); }
 
-template <int kWavesM, int kWavesN, int kMTiles, int kNQuads, int kStages, int kSplit>
-__global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) product_i8_tile_kernel(ProductArgs a) {
-  using S = TileShape<kWavesM, kWavesN, kMTiles, kNQuads, kStages, kSplit>;
+template <int kWavesM, int kWavesN, int kMTiles, int kStages, int kSplit>
+__global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) __attribute__((amdgpu_waves_per_eu(2))) product_i8_tile_kernel(ProductArgs a) {
+  using S = TileShape<kWavesM, kWavesN, kMTiles, kStages, kSplit>;
   extern __shared__ __align__(1024) char lds[];
   const int lane = threadIdx.x & 63, wave_of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int part = kSplit == 1 ? 0 : wave_of_all / S::kWaves, wave = wave_of_all - part * S::kWaves;
@@ -130,8 +210,8 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) product_i8_ti
   tile_of(blockIdx.x, (a.M + S::kTileM - 1) / S::kTileM, (a.N + S::kTileN - 1) / S::kTileN, m0, n0);
   m0 *= S::kTileM;
   n0 *= S::kTileN;
-  const int8_t* a_base = a.a + m0 * a.a_bytes;
-  const int8_t* b_base = a.b + n0 * a.b_bytes;
+  const int8_t* a_base = a.a + m0 * a.a_row;
+  const int8_t* b_base = a.b + n0 * a.b_row;
   const uint32_t lds0 = lds_address(lds) + part * S::kRing;
 
   // This wave's copies: 8 rows of 128 bytes each; a lane's source row and piece are those that belong at its place.  Rows beyond the matrix
@@ -144,13 +224,13 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) product_i8_ti
     const int place = (of_a ? copy : copy - S::kTileM / 8) * 64 + lane, line = place >> 4;
     const int source = (place & 15) ^ (of_a ? exchange_of<false>(line) : exchange_of<true>(line));
     const int32_t r = min(line * 2 + (source >> 3), (of_a ? a.M - m0 : a.N - n0) - 1);
-    from[i] = (uint32_t)r * (uint32_t)(of_a ? a.a_bytes : a.b_bytes) + (source & 7) * 16;
+    from[i] = (uint32_t)r * (uint32_t)(of_a ? a.a_row : a.b_row) + (source & 7) * 16;
   }
   // Stage j of the part is group j kSplit + part.
   constexpr uint64_t kAll = ~0ull;
   auto copy_codes = [&](int32_t j, uint32_t stage, int i, uint64_t lanes, bool all) __attribute__((always_inline)) {
     const int copy = wave * S::kCopies + i;
-    const int8_t* base = (copy * 8 < S::kTileM ? a_base : b_base) + (int64_t)(j * kSplit + part) * kCodeGroup;
+    const int8_t* base = copy * 8 < S::kTileM ? a_base + (j * kSplit + part) * a.a_group : b_base + (j * kSplit + part) * a.b_group;
     if (all) copy16_to_lds_sv(base, from[i], lds0 + stage + copy * 1024);
     else copy16_to_lds_sv_masked(base, from[i], lds0 + stage + copy * 1024, lanes);
   };
@@ -175,7 +255,7 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) product_i8_ti
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     a_at[h] = lds0 + wm * kMTiles * 16 * kCodeGroup + code_piece<false>(l16, q + 4 * h);
-    b_at[h] = lds0 + (S::kTileM + wn * 64 * kNQuads) * kCodeGroup + code_piece<true>((l16 >> 2) * 16 + (l16 & 3), q + 4 * h);
+    b_at[h] = lds0 + (S::kTileM + wn * 64) * kCodeGroup + code_piece<true>((l16 >> 2) * 16 + (l16 & 3), q + 4 * h);
   }
   auto piece = [&](uint32_t at, int distance) __attribute__((always_inline)) -> u32x4 { return *lds_pointer<const u32x4>(at + distance); };
   uint32_t stage = 0, free = S::kAhead * S::kStage;  // where the stage's codes lie, and where those of the stage kAhead later go
@@ -188,7 +268,7 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) product_i8_ti
     for (int h = 0; h < 2; ++h) {
       rows[h] = piece(a_at[h] + stage, 0);
 #pragma unroll
-      for (int t = 0; t < S::kNTiles; ++t) columns[t][h] = piece(b_at[h] + stage, (t >> 2) * 64 * kCodeGroup + (t & 3) * 4 * kCodeGroup);
+      for (int t = 0; t < S::kNTiles; ++t) columns[t][h] = piece(b_at[h] + stage, t * 4 * kCodeGroup);
     }
 #pragma unroll
     for (int i = 0; i < kMTiles; ++i) {
@@ -245,85 +325,86 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) product_i8_ti
 #pragma unroll
         for (int t = 0; t < S::kNTiles; ++t) sum[i][t] += *place(from_part, i, t);
   }
+  const int32_t n = n0 + wn * 64 + q * 16;
+  float sb[16], bias[16];
 #pragma unroll
-  for (int u = 0; u < kNQuads; ++u) {
-    const int32_t n = n0 + (wn * kNQuads + u) * 64 + q * 16;
-    float sb[16], bias[16];
+  for (int e = 0; e < 16; ++e) {
+    const int32_t at = min(n + e, a.N - 1);
+    sb[e] = a.sb[at];
+    bias[e] = a.bias ? a.bias[at] : 0.f;
+  }
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int32_t at = min(n + e, a.N - 1);
-      sb[e] = a.sb[at];
-      bias[e] = a.bias ? a.bias[at] : 0.f;
-    }
+  for (int i = 0; i < kMTiles; ++i) {
+    const int32_t m = m0 + (wm * kMTiles + i) * 16 + l16;
+    if (m >= a.M) continue;
+    const float sa = a.sa[m];
+    float y[16];
 #pragma unroll
-    for (int i = 0; i < kMTiles; ++i) {
-      const int32_t m = m0 + (wm * kMTiles + i) * 16 + l16;
-      if (m >= a.M) continue;
-      const float sa = a.sa[m];
-      float y[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] = result(sum[i][u * 4 + (e >> 2)][e & 3], sa * sb[e], bias[e]);
-      put(a, m, n, y, a.N - n);
-    }
+    for (int e = 0; e < 16; ++e) y[e] = result(sum[i][e >> 2][e & 3], sa * sb[e], bias[e]);
+    put(a, m, n, y, a.N - n);
   }
 }
 
-template <int kWavesM, int kWavesN, int kMTiles, int kNQuads, int kStages, int kSplit>
+template <int kWavesM, int kWavesN, int kMTiles, int kStages, int kSplit>
 int launch_tiles(const ProductArgs& a, hipStream_t stream) {
-  using S = TileShape<kWavesM, kWavesN, kMTiles, kNQuads, kStages, kSplit>;
+  using S = TileShape<kWavesM, kWavesN, kMTiles, kStages, kSplit>;
   const int64_t tiles = ((int64_t)a.M + S::kTileM - 1) / S::kTileM * (((int64_t)a.N + S::kTileN - 1) / S::kTileN);
   if (tiles > kMostThreads / (64 * S::kWaves * kSplit)) return fail(RADIAL_ESHAPE, "M*N is too large for one launch");
   if constexpr (S::kLds > 65536) {
     static DeviceOnce configured;
-    if (int rc = allow_dynamic_lds(configured, (const void*)product_i8_tile_kernel<kWavesM, kWavesN, kMTiles, kNQuads, kStages, kSplit>, S::kLds)) return rc;
+    if (int rc = allow_dynamic_lds(configured, (const void*)product_i8_tile_kernel<kWavesM, kWavesN, kMTiles, kStages, kSplit>, S::kLds)) return rc;
   }
-  product_i8_tile_kernel<kWavesM, kWavesN, kMTiles, kNQuads, kStages, kSplit><<<dim3((unsigned)tiles), dim3(64 * S::kWaves * kSplit), S::kLds, stream>>>(a);
+  product_i8_tile_kernel<kWavesM, kWavesN, kMTiles, kStages, kSplit><<<dim3((unsigned)tiles), dim3(64 * S::kWaves * kSplit), S::kLds, stream>>>(a);
   RADIAL_HIP_TRY(hipGetLastError());
   return RADIAL_OK;
 }
 
 int launch_form(int form, const ProductArgs& a, hipStream_t stream) {
   switch (form) {
-    case 0: return launch_tiles<2, 4, 8, 1, 2, 1>(a, stream);
-    case 1: return launch_tiles<2, 4, 6, 1, 2, 1>(a, stream);
-    case 2: return launch_tiles<2, 2, 4, 1, 2, 1>(a, stream);
-    case 3: return launch_tiles<2, 2, 4, 1, 2, 2>(a, stream);
-    case 4: return launch_tiles<2, 2, 2, 1, 3, 1>(a, stream);
-    case 5: return launch_tiles<2, 2, 2, 1, 3, 2>(a, stream);
-    case 6: return launch_tiles<2, 1, 2, 1, 2, 2>(a, stream);
-    default: return launch_tiles<2, 1, 2, 1, 2, 4>(a, stream);
+    case 0: return launch_tiles<2, 4, 8, 2, 1>(a, stream);
+    case 1: return launch_tiles<2, 4, 6, 2, 1>(a, stream);
+    case 2: return launch_tiles<2, 2, 4, 2, 1>(a, stream);
+    case 3: return launch_tiles<4, 2, 2, 3, 1>(a, stream);
+    case 4: return launch_tiles<2, 2, 3, 3, 1>(a, stream);
+    case 5: return launch_tiles<4, 2, 1, 3, 1>(a, stream);
+    case 6: return launch_tiles<4, 1, 1, 3, 1>(a, stream);
+    case 7: return launch_tiles<4, 1, 1, 3, 2>(a, stream);
+    case 8: return launch_tiles<2, 1, 1, 3, 2>(a, stream);
+    default: return launch_tiles<2, 1, 1, 3, 4>(a, stream);
   }
 }
 
 // One sum of whole numbers.
 int launch_product(const ProductArgs& a, hipStream_t stream) {
-  if (takes_pieces(a.M, a.N)) {
+  if (takes_pieces_i8(a.M, a.N)) {
     const int64_t tiles = pieces_of(a.M) * pieces_of(a.N);
     if (tiles > kMostThreads / (64 * kParts)) return fail(RADIAL_ESHAPE, "N is too large for one launch");
     product_i8_pieces_kernel<<<dim3((unsigned)tiles), dim3(64 * kParts), 0, stream>>>(a);
     RADIAL_HIP_TRY(hipGetLastError());
     return RADIAL_OK;
   }
-  const ProductPlan plan = plan_product(a.M, a.N, a.groups);
+  const ProductPlan plan = plan_product_i8(a.M, a.N, a.groups);
   ProductArgs part = a;
   part.M = plan.rows;
   if (int rc = launch_form(plan.form, part, stream)) return rc;
   if (plan.rows == a.M) return RADIAL_OK;
   part.M = a.M - plan.rows;
-  part.a += plan.rows * a.a_bytes;
+  part.a += plan.rows * a.a_row;
   part.sa += plan.rows;
   part.out = (char*)part.out + plan.rows * a.out_stride * size_of(a.out_type);
   return launch_form(plan.rest, part, stream);
 }
 
-int product_i8(int32_t M, int32_t N, int32_t K, const int8_t* a_codes, const float* a_scales, const int8_t* b_codes, const float* b_scales, const float* bias,
-               void* out, int32_t out_type, int64_t out_stride, bool accumulate, hipStream_t stream) {
+int product_i8(int32_t M, int32_t N, int32_t K, const int8_t* a_codes, int64_t a_pitch, const float* a_scales, const int8_t* b_codes, int64_t b_pitch,
+               const float* b_scales, const float* bias, void* out, int32_t out_type, int64_t out_stride, bool accumulate, hipStream_t stream) {
   ProductArgs a = {};
   a.a = a_codes; a.b = b_codes; a.sa = a_scales; a.sb = b_scales; a.bias = bias;
   a.out = out; a.out_type = out_type; a.out_stride = out_stride; a.accumulate = accumulate;
   a.M = M; a.N = N;
   int32_t groups = (int32_t)code_groups(K);
-  a.a_bytes = a.b_bytes = (int64_t)groups * kCodeGroup;
+  a.a_row = a_pitch;
+  a.b_row = b_pitch;
+  a.a_group = a.b_group = kCodeGroup;
   if (K <= kExactCols) {
     a.groups = groups;
     return launch_product(a, stream);
@@ -331,11 +412,22 @@ int product_i8(int32_t M, int32_t N, int32_t K, const int8_t* a_codes, const flo
   for (constexpr int32_t kMost = kExactCols / kCodeGroup; groups > 0; groups -= a.groups) {
     a.groups = groups < kMost ? groups : kMost;
     if (int rc = launch_product(a, stream)) return rc;
-    a.a += (int64_t)a.groups * kCodeGroup;
-    a.b += (int64_t)a.groups * kCodeGroup;
+    a.a += a.groups * a.a_group;
+    a.b += a.groups * a.b_group;
     a.bias = nullptr;
     a.accumulate = 1;
   }
+  return RADIAL_OK;
+}
+
+template <class T>
+int launch_few(const ProductArgs& a, const void* x, int64_t stride, int32_t cols, hipStream_t stream) {
+  const dim3 grid((unsigned)pieces_of(a.N)), threads(64 * kParts);
+  if (pieces_of(a.N) > kMostThreads / (64 * kParts)) return fail(RADIAL_ESHAPE, "N is too large for one launch");
+  if (a.M == 1) linear_i8_few_kernel<T, 1><<<grid, threads, 0, stream>>>(a, (const T*)x, stride, cols);
+  else if (a.M == 2) linear_i8_few_kernel<T, 2><<<grid, threads, 0, stream>>>(a, (const T*)x, stride, cols);
+  else linear_i8_few_kernel<T, kFewRows><<<grid, threads, 0, stream>>>(a, (const T*)x, stride, cols);
+  RADIAL_HIP_TRY(hipGetLastError());
   return RADIAL_OK;
 }
 
@@ -377,21 +469,21 @@ struct Parts {
 struct FwdParts {
   int8_t* codes;
   float* scales;
-  FwdParts(Parts& p, int32_t M, int32_t K) : codes(p.take<int8_t>(M * code_groups(K) * kCodeGroup)), scales(p.take<float>(M)) {}
+  FwdParts(Parts& p, int32_t M, int32_t K) : codes(p.take<int8_t>(M * odd_pitch(K))), scales(p.take<float>(M)) {}
 };
 struct BwdParts {
   int8_t *dy, *dy_t, *x_t;
   float *dy_scales, *dy_t_scales, *x_t_scales;
-  char* quantise;  // workspace of the quantiser, for dy and then for x
+  char* quantise[2];  // workspaces of the quantiser, for dy and x
   BwdParts(Parts& p, int32_t M, int32_t N, int32_t K) {
-    dy = p.take<int8_t>(M * code_groups(N) * kCodeGroup);
-    dy_t = p.take<int8_t>(N * code_groups(M) * kCodeGroup);
-    x_t = p.take<int8_t>(K * code_groups(M) * kCodeGroup);
+    dy = p.take<int8_t>(M * odd_pitch(N));
+    dy_t = p.take<int8_t>(N * odd_pitch(M));
+    x_t = p.take<int8_t>(K * odd_pitch(M));
     dy_scales = p.take<float>(M);
     dy_t_scales = p.take<float>(N);
     x_t_scales = p.take<float>(K);
-    const size_t of_dy = quantize_i8_workspace(M, N), of_x = quantize_i8_workspace(M, K);
-    quantise = p.take<char>((int64_t)(of_dy > of_x ? of_dy : of_x));
+    quantise[0] = p.take<char>((int64_t)quantize_i8_workspace(M, N));
+    quantise[1] = p.take<char>((int64_t)quantize_i8_workspace(M, K));
   }
 };
 
@@ -408,7 +500,8 @@ extern "C" int radial_product_i8(int32_t M, int32_t N, int32_t K, const int8_t* 
   if (int rc = check_codes(b_codes, b_scales, "b")) return rc;
   if (int rc = check_out(out, out_type, out_stride, N, K, accumulate != 0, "out")) return rc;
   if (int rc = check_floats(bias, "bias")) return rc;
-  return product_i8(M, N, K, a_codes, a_scales, b_codes, b_scales, bias, out, out_type, out_stride, accumulate != 0, (hipStream_t)hip_stream);
+  const int64_t pitch = code_groups(K) * kCodeGroup;
+  return product_i8(M, N, K, a_codes, pitch, a_scales, b_codes, pitch, b_scales, bias, out, out_type, out_stride, accumulate != 0, (hipStream_t)hip_stream);
 }
 
 extern "C" size_t radial_linear_i8_fwd_workspace(int32_t M, int32_t N, int32_t K) {
@@ -430,10 +523,20 @@ extern "C" int radial_linear_i8_fwd(int32_t M, int32_t N, int32_t K, const void*
   if (int rc = check_floats(bias, "bias")) return rc;
   if (int rc = check_workspace(workspace, workspace_bytes, radial_linear_i8_fwd_workspace(M, N, K))) return rc;
   hipStream_t stream = (hipStream_t)hip_stream;
+  if (M <= kFewRows && K <= kFewCols) {
+    ProductArgs a = {};
+    a.b = w_codes; a.sb = w_scales; a.bias = bias; a.b_row = code_groups(K) * kCodeGroup; a.b_group = kCodeGroup;
+    a.out = y; a.out_type = y_type; a.out_stride = y_stride;
+    a.M = M; a.N = N; a.groups = (int32_t)code_groups(K);
+    return type == RADIAL_F32 ? launch_few<float>(a, x, x_stride, K, stream) : launch_few<__bf16>(a, x, x_stride, K, stream);
+  }
   Parts p = {(char*)workspace};
   const FwdParts of(p, M, K);
-  if (int rc = quantize_i8(M, K, x, type, x_stride, of.codes, of.scales, nullptr, nullptr, nullptr, false, nullptr, stream)) return rc;
-  return product_i8(M, N, K, of.codes, of.scales, w_codes, w_scales, bias, y, y_type, y_stride, false, stream);
+  QuantI8 q = {};
+  q.x = x; q.stride = x_stride; q.rows = M; q.cols = K; q.codes = of.codes; q.pitch = odd_pitch(K); q.scales = of.scales;
+  char* none[1] = {nullptr};
+  if (int rc = quantize_i8(&q, 1, type, none, stream)) return rc;
+  return product_i8(M, N, K, of.codes, odd_pitch(K), of.scales, w_codes, code_groups(K) * kCodeGroup, w_scales, bias, y, y_type, y_stride, false, stream);
 }
 
 extern "C" size_t radial_linear_i8_bwd_workspace(int32_t M, int32_t N, int32_t K) {
@@ -469,12 +572,15 @@ extern "C" int radial_linear_i8_bwd(int32_t M, int32_t N, int32_t K, const void*
   hipStream_t stream = (hipStream_t)hip_stream;
   Parts p = {(char*)workspace};
   const BwdParts of(p, M, N, K);
-  if (int rc = quantize_i8(M, N, dy, type, dy_stride, dx ? of.dy : nullptr, dx ? of.dy_scales : nullptr, dw ? of.dy_t : nullptr,
-                           dw ? of.dy_t_scales : nullptr, dbias, add, of.quantise, stream)) return rc;
+  QuantI8 q[2] = {};
+  q[0].x = dy; q[0].stride = dy_stride; q[0].rows = M; q[0].cols = N; q[0].sums_t = dbias; q[0].accumulate = add;
+  if (dx) q[0].codes = of.dy, q[0].pitch = odd_pitch(N), q[0].scales = of.dy_scales;
+  if (dw) q[0].codes_t = of.dy_t, q[0].pitch_t = odd_pitch(M), q[0].scales_t = of.dy_t_scales;
+  q[1].x = x; q[1].stride = x_stride; q[1].rows = M; q[1].cols = K; q[1].codes_t = of.x_t; q[1].pitch_t = odd_pitch(M); q[1].scales_t = of.x_t_scales;
+  if (int rc = quantize_i8(q, dw ? 2 : 1, type, of.quantise, stream)) return rc;
   if (dx) {
-    if (int rc = product_i8(M, K, N, of.dy, of.dy_scales, wt_codes, wt_scales, nullptr, dx, dx_type, dx_stride, false, stream)) return rc;
+    if (int rc = product_i8(M, K, N, of.dy, odd_pitch(N), of.dy_scales, wt_codes, code_groups(N) * kCodeGroup, wt_scales, nullptr, dx, dx_type, dx_stride, false, stream)) return rc;
   }
   if (!dw) return RADIAL_OK;
-  if (int rc = quantize_i8(M, K, x, type, x_stride, nullptr, nullptr, of.x_t, of.x_t_scales, nullptr, false, of.quantise, stream)) return rc;
-  return product_i8(N, K, M, of.dy_t, of.dy_t_scales, of.x_t, of.x_t_scales, nullptr, dw, dw_type, dw_stride, add, stream);
+  return product_i8(N, K, M, of.dy_t, odd_pitch(M), of.dy_t_scales, of.x_t, odd_pitch(M), of.x_t_scales, nullptr, dw, dw_type, dw_stride, add, stream);
 }

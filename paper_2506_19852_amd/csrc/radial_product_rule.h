@@ -30,10 +30,10 @@ inline double tile_time(const TileForm& f, int32_t M, int32_t N, int32_t groups)
   return full * (stages * f.stage_full + f.besides) + last;
 }
 
-inline int choose_tiles(int32_t M, int32_t N, int32_t groups, double* time) {
+inline int choose_tiles(int32_t M, int32_t N, int32_t groups, double* time, const TileForm* forms = kTileForms, int count = kTileFormCount) {
   int best = 0;
-  for (int i = 0; i < kTileFormCount; ++i) {
-    const double t = tile_time(kTileForms[i], M, N, groups);
+  for (int i = 0; i < count; ++i) {
+    const double t = tile_time(forms[i], M, N, groups);
     if (i == 0 || t < *time) {
       best = i;
       *time = t;
@@ -48,18 +48,18 @@ inline int choose_tiles(int32_t M, int32_t N, int32_t groups, double* time) {
 struct ProductPlan {
   int32_t rows, form, rest;  // rows in `form`, those behind them in `rest`
 };
-inline ProductPlan plan_product(int32_t M, int32_t N, int32_t groups) {
+inline ProductPlan plan_product(int32_t M, int32_t N, int32_t groups, const TileForm* forms = kTileForms, int count = kTileFormCount) {
   constexpr double kLaunch = 8.0, kWorth = 0.95;  // us of another launch and its start; what the estimate has to promise
   double least = 0;
-  ProductPlan plan = {M, choose_tiles(M, N, groups, &least), 0};
+  ProductPlan plan = {M, choose_tiles(M, N, groups, &least, forms, count), 0};
   least *= kWorth;
   for (int form = 0; form < 2; ++form) {
-    const TileForm& f = kTileForms[form];
+    const TileForm& f = forms[form];
     const int64_t of_row = ((int64_t)N + f.columns - 1) / f.columns, tiles = ((int64_t)M + f.rows - 1) / f.rows * of_row;
     const int64_t rows = tiles / kComputeUnits * kComputeUnits / of_row * f.rows;
     if (rows < f.rows || rows >= M) continue;
     double rest_time = 0;
-    const int rest = choose_tiles((int32_t)(M - rows), N, groups, &rest_time);
+    const int rest = choose_tiles((int32_t)(M - rows), N, groups, &rest_time, forms, count);
     const double time = tile_time(f, (int32_t)rows, N, groups) + rest_time + kLaunch;
     if (time < least) {
       least = time;

@@ -117,7 +117,8 @@ def test_sums_are_added_to_what_is_there():
 # M, N, K
 SIZES = [(1, 1, 1), (1, 5120, 5120), (2, 300, 1000), (16, 128, 128), (17, 129, 256), (33, 64, 384), (64, 512, 1536), (65, 96, 128), (100, 1961, 1000),
          (128, 128, 128), (129, 4100, 300), (200, 333, 2049), (256, 2048, 640), (257, 257, 257), (512, 5120, 4096), (600, 1536, 1000), (1237, 1961, 1001),
-         (2000, 5120, 384), (3333, 2500, 130), (8200, 5000, 256)]
+         (2000, 5120, 384), (3333, 2500, 130), (8200, 5000, 256), (4, 700, 900), (5, 700, 900), (64, 5120, 2048), (64, 2048, 4096), (20, 5120, 640), (300, 2048, 4096),
+         (700, 5120, 256), (450, 5120, 900), (1560, 5120, 384), (5000, 2000, 300), (14040, 333, 130), (1560, 2000, 2048), (6000, 3000, 4096)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
@@ -202,7 +203,7 @@ def test_a_scale_of_nan_reaches_its_row_and_column_alone(M):
 
 # ---- projection -----------------------------------------------------------------------------------
 
-LINEAR = [(1, 64, 64), (2, 5120, 5120), (5, 100, 3000), (16, 40, 20000), (77, 640, 1000), (130, 257, 300), (1001, 333, 2049)]
+LINEAR = [(1, 64, 64), (2, 5120, 5120), (1, 333, 8192), (3, 77, 1000), (4, 130, 8191), (4, 40, 8193), (2, 16, 1), (5, 100, 3000), (16, 40, 20000), (77, 640, 1000), (130, 257, 300), (1001, 333, 2049)]
 
 
 def _linear(M, N, K, dtype, seed):

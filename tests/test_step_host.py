@@ -38,7 +38,7 @@ def test_structures_are_laid_out_as_the_header_says(tmp_path):
     (dict(codes=AT + 8), ESHAPE, "codes"), (dict(codes_t=AT + 1), ESHAPE, "codes"), (dict(scales=AT + 2), ESHAPE, "scales"), (dict(sums_t=AT + 1), ESHAPE, "sums_t"),
     (dict(workspace=None), EINVAL, "workspace"), (dict(bytes=10), EINVAL, "needed"), (dict(workspace=AT + 128), ESHAPE, "256-byte"),
     (dict(rows=0x7fffffff), ESHAPE, "too large"), (dict(cols=0x7fffffff, stride=1 << 40), ESHAPE, "too large"),
-    (dict(rows=1 << 28, codes_t=None, scales_t=None, sums_t=None), ESHAPE, "too large"), (dict(rows=1 << 29, cols=1 << 12, stride=1 << 12, codes=None, scales=None, bytes=1 << 50), ESHAPE, "too large"),
+    (dict(rows=1 << 28, codes_t=None, scales_t=None, sums_t=None), ESHAPE, "too large"), (dict(cols=1 << 29, rows=1 << 20, stride=1 << 29, codes=None, scales=None, codes_t=None, scales_t=None, bytes=1), EINVAL, "needed"),
 ], ids=str)
 def test_quantise_arguments(change, code, text):
     a = dict(rows=10, cols=100, x=AT, type=BF16, stride=100, codes=AT, scales=AT, codes_t=AT, scales_t=AT, sums_t=AT, accumulate=0, workspace=AT, bytes=1 << 30)
@@ -51,7 +51,7 @@ def test_quantise_arguments(change, code, text):
     (dict(b=None), EINVAL, "NULL"), (dict(sb=None), EINVAL, "NULL"), (dict(out=None), EINVAL, "NULL"), (dict(type=3), EINVAL, "type"), (dict(accumulate=1), EINVAL, "float32"),
     (dict(K=131072), EUNSUPPORTED, "float32"), (dict(a=AT + 8), ESHAPE, "codes"), (dict(b=AT + 4), ESHAPE, "codes"), (dict(sb=AT + 2), ESHAPE, "scales"),
     (dict(bias=AT + 2), ESHAPE, "bias"), (dict(out=AT + 1), ESHAPE, "out"), (dict(out=AT + 2, type=F32), ESHAPE, "out"), (dict(stride=9), ESHAPE, "stride"),
-    (dict(K=(1 << 23) + 1), ESHAPE, "too large"), (dict(M=(1 << 29) + 1), ESHAPE, "too large"), (dict(N=1 << 28, stride=1 << 28), ESHAPE, "too large"),
+    (dict(K=(1 << 23) + 1), ESHAPE, "too large"), (dict(M=(1 << 29) + 1), ESHAPE, "too large"), (dict(M=2, N=1 << 28, stride=1 << 28), ESHAPE, "too large"),
     (dict(M=1 << 29, N=1 << 29, stride=1 << 29), ESHAPE, "too large"),
 ], ids=str)
 def test_product_arguments(change, code, text):
