@@ -247,9 +247,9 @@ RADIAL_API int radial_linear_i8_bwd(int32_t M, int32_t N, int32_t K, const void*
  * Everything is computed in float32, w is rounded once to its type.
  *
  * States in 8 bits: m and sqrt(v) are held as E4M3 codes (as in radial.h) with a float32 scale for each block of 128 values of
- * the tensor, the last block the rest: scale = amax/448, code = E4M3(m (448/amax)), all 0 where amax is 0.  (sqrt(v) spans half of
- * the powers of two that v does.)  A positive sqrt(v) never becomes 0, but the smallest code: what a step divides by is not lost
- * beside larger neighbours.  A NaN has the code of NaN and does not enter amax; with an infinity the block's state is NaN.  Codes and
+ * the tensor, the last block the rest: scale = amax/448, code = E4M3(m (448/amax)), all 0 where amax is below 2^-100.  (sqrt(v) spans half of
+ * the powers of two that v does.)  Otherwise a positive sqrt(v) never becomes 0, but the smallest code: what a step divides by is not lost
+ * beside larger neighbours.  A NaN has the code of NaN and does not enter amax; an infinite m makes its block's first state NaN.  Codes and
  * scales begin as zeros.  Rounding to nearest keeps a slowly changing state where it is (beta2 = 0.999 moves sqrt(v) by less than half
  * a step of its code, 3 to 6 %, unless a gradient is 8 times it); RADIAL_ROUND_RANDOM rounds up with the probability of what is left over, so
  * that a state is right on average: the magnitude's code is floor(y + u), y in steps of the code, u = (16 bits)/2^16.  The bits of
@@ -299,7 +299,7 @@ RADIAL_API int radial_grad_norm(const radial_adamw_plan_info* plan, const void* 
                                 void* workspace, size_t workspace_bytes, void* hip_stream);
 
 typedef struct {
-  double lr, beta1, beta2, eps; /* lr >= 0; 0 <= beta < 1; eps > 0; all finite                                      */
+  double lr, beta1, beta2, eps; /* lr >= 0; 0 <= beta < 1; eps a positive normal number of float32; all finite      */
   int64_t step;                 /* t >= 1                                                                            */
   uint64_t seed;                /* of RADIAL_ROUND_RANDOM                                                            */
   int32_t rounding;             /* RADIAL_ROUND_*, of states in 8 bits                                              */

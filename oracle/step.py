@@ -65,6 +65,7 @@ def encode(v, bits=None, positive=False):
     n = len(v)
     b = _blocks(np.asarray(v, F32))
     amax = np.where(np.isnan(b), 0, np.abs(b)).max(1).astype(F32)
+    amax = np.where(amax < F32(2.0 ** -100), F32(0), amax)
     scale = (amax / F32(448)).astype(F32)
     with np.errstate(divide="ignore", invalid="ignore"):
         inverse = np.where(amax > 0, F32(448) / amax, F32(0)).astype(F32)
@@ -77,7 +78,7 @@ def encode(v, bits=None, positive=False):
         below = np.minimum(np.floor(np.where(np.isnan(a), 0, a) / step + bits / 65536.0) * step, 448.0)
         codes = np.where(np.isnan(y), 0x7f, ol.e4m3_codes(below) | np.where(np.signbit(y), 128, 0)).astype(np.uint8)
     if positive:
-        codes = np.where((np.asarray(v) > 0) & (codes == 0), 1, codes).astype(np.uint8)
+        codes = np.where((y > 0) & (codes == 0), 1, codes).astype(np.uint8)
     return codes, scale
 
 

@@ -1,8 +1,9 @@
 """AdamW over many tensors and the norm of their gradients, against the oracle (run with -m gpu).
 
 Bounds.  u = 2^-24, the rounding of a float32 operation.  m: g factor, two constants, two products and their sum, at most 6u (|beta1 m| + |(1 - beta1) g|) =: em;
-v: likewise one product more, ev = 8u v.  The root takes u and half of ev, its product with a constant 2u, the sum with eps u, so the denominator d is off by
-8u d; the update c m/d (c with its rounding, division, product) by c/d (em + 11u |m|) and its square terms, 12u; the weight's product 2u |w|, the difference u.
+v: (factor, square) 3u, its constant, product and the sum 3u more, ev = 6u v (8u are allowed).  The root takes u and half of ev, its product with a constant 2u, the sum with
+eps u, so the denominator d is off by 7u d; its inverse is one of the instruction that is off by a unit at most, 2u; the products with m and with c, and c's own rounding, 3u:
+the update c m/d is off by c/d (em + 12u |m|); the weight's product 2u |w|, the difference u.
 States in 8 bits: float32 operations one by one give the same bits in numpy, so codes and scales are equal."""
 import numpy as np
 import pytest
@@ -188,6 +189,31 @@ def test_a_small_root_beside_a_large_one_is_not_lost():
     check(group, before, group.read(), step=2)
     moved = (group.views["w"][0].cpu() - before["w"][0]).abs().max()
     assert moved <= 1.1 * LR
+
+
+@pytest.mark.parametrize("size", [1e-45, 1e-38, 1e-36, 3e-31, 1e-30, 1e-25, 1e-20, 1e-12, 1e18], ids=str)
+def test_gradients_of_any_size_leave_finite_states(size):
+    """Roots of v below 2^-126 are not held to the bound, but stay finite; 300 steps without a gradient take m through all sizes down to nothing."""
+    for coded in (False, True):
+        group = Group([300], coded=coded, decay=0.0)
+        for k in ("m", "v") + (("ms", "vs") if coded else ()):
+            group.views[k][0].zero_()
+        group.views["g"][0].copy_(torch.linspace(-size, size, 300))
+        before = group.read()
+        group.step(step=1)
+        after = group.read()
+        if size >= 1e-12:
+            check(group, before, after, step=1)
+        group.views["g"][0].zero_()
+        for t in range(2, 302):
+            group.step(step=t)
+        after = group.read()
+        assert torch.isfinite(after["w"][0]).all()
+        if coded:
+            assert not np.isnan(ol.e4m3_values()[after["m"][0].numpy()]).any() and not np.isnan(ol.e4m3_values()[after["v"][0].numpy()]).any()
+            assert torch.isfinite(after["ms"][0]).all() and torch.isfinite(after["vs"][0]).all()
+        assert (after["w"][0] - before["w"][0]).abs().max() <= 12 * LR
+    assert group.guards_kept()
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")], ids=str)
