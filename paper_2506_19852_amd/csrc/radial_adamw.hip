@@ -279,8 +279,9 @@ __device__ __forceinline__ uint32_t encode_four(f32x4 v, const uint32_t (&bits)[
     uint32_t codes = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      uint32_t code = random_code(y[e], kPositive ? bits[e] >> 16 : bits[e] & 0xffffu);
-      if (kPositive) code = max(code, min(__builtin_bit_cast(uint32_t, y[e]), 1u));  // a positive value keeps a positive code
+      const float one = y[e];  // (the bits of y[e] itself are those of y[0]: a bit cast of a vector's element takes the vector's address)
+      uint32_t code = random_code(one, kPositive ? bits[e] >> 16 : bits[e] & 0xffffu);
+      if (kPositive) code = max(code, min(__builtin_bit_cast(uint32_t, one), 1u));  // a positive value keeps a positive code
       codes |= code << 8 * e;
     }
     return codes;

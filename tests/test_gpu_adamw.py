@@ -175,6 +175,22 @@ def test_states_that_begin_as_zeros():
     assert not after["m"][0][:128].any() and not after["vs"][0][:1].any()
 
 
+@pytest.mark.parametrize("rounding", ["nearest", "random"])
+def test_values_without_a_gradient_among_others_stay_zeros(rounding):
+    group = Group([8192, 300], coded=True)
+    for k in ("m", "v", "ms", "vs"):
+        for t in group.views[k]:
+            t.zero_()
+    for i, t in enumerate(group.views["g"]):
+        t[i::3] = 0
+    before = group.read()
+    group.step(step=1, rounding=rounding, seed=3)
+    after = group.read()
+    check(group, before, after, step=1, rounding=rounding, seed=3)
+    for i in range(2):
+        assert not after["v"][i][i::3].any() and not after["m"][i][i::3].any()
+
+
 def test_a_small_root_beside_a_large_one_is_not_lost():
     """The next step divides by the root: it is the smallest code at least, and the update stays below what that allows."""
     group = Group([128], coded=True, decay=0.0)
