@@ -303,6 +303,23 @@ def complexity_curve(frames_list, heads, args):
     print(json.dumps(summary))
 
 
+def _time_parts(parts, args):
+    """Mean milliseconds of each of the named calls over the steps, one behind the other."""
+    import torch
+    total = {name: 0.0 for name, _ in parts}
+    for step in range(args.warmup + args.steps):
+        marks = [torch.cuda.Event(enable_timing=True) for _ in range(len(parts) + 1)]
+        marks[0].record()
+        for (_, call), mark in zip(parts, marks[1:]):
+            call()
+            mark.record()
+        torch.cuda.synchronize()
+        if step >= args.warmup:
+            for i, (name, _) in enumerate(parts):
+                total[name] += marks[i].elapsed_time(marks[i + 1]) / args.steps
+    return total
+
+
 def layer_times(w, args):
     """Prints one JSON line: the attention half of a layer at workload w's sizes, hidden size H*D, with random weights: norm, projection of q, k, v,
     rotary positions, block-sparse attention, output projection, gated residual and norm; the projections in E4M3 with a scale for each 128 values."""
@@ -345,23 +362,91 @@ def layer_times(w, args):
         ("project_out", lambda: rl.radial_product_fp8(*act, *weights["out"], o.view(-1, C))),
         ("residual_norm", lambda: rl.radial_norm_fwd(x, r, z, y=o, gate=mod[:, :, 2], scale=mod[:, :, 3], shift=mod[:, :, 4])),
     ]
-    total = {name: 0.0 for name, _ in parts}
-    for step in range(args.warmup + args.steps):
-        marks = [torch.cuda.Event(enable_timing=True) for _ in range(len(parts) + 1)]
-        marks[0].record()
-        for (_, call), mark in zip(parts, marks[1:]):
-            call()
-            mark.record()
-        torch.cuda.synchronize()
-        if step >= args.warmup:
-            for i, (name, _) in enumerate(parts):
-                total[name] += marks[i].elapsed_time(marks[i + 1]) / args.steps
+    total = _time_parts(parts, args)
     mask.free()
     ms = sum(total.values())
     print(json.dumps({"metric": "attention half of a layer, forward", "value": round(ms, 3), "unit": "ms", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
                       "higher_is_better": False, "dtype": "bf16, projections E4M3 with a scale for each 128 values", "data": "synthetic",
                       "config": {"model": w.name, "global_batch": w.B, "seq_len": N, "hidden": C}, "ms": {n: round(t, 4) for n, t in total.items()},
                       "attention_share": round(total["attention"] / ms, 4)}))
+
+
+def layer_step_times(w, args):
+    """Prints one JSON line: a tuning step of the attention half of a layer at workload w's sizes: the forward of layer_times with its projections in 8-bit integers,
+    all gradients, their norm, an AdamW step with states in 8 bits on the projections' weights and biases, and the weights' new codes."""
+    import torch
+    from paper_2506_19852_amd import binding as rb
+    from paper_2506_19852_amd import layer as rl
+
+    dev, B, N, H, D = "cuda:0", w.B, w.N, w.H, w.D
+    C, M = H * D, w.B * w.N
+    g = torch.Generator(device=dev).manual_seed(w.seed & 0x7fffffff)
+
+    def rand(*shape, size=1.0, dtype=torch.bfloat16):
+        return torch.empty(shape, dtype=dtype, device=dev).normal_(0.0, size, generator=g)
+
+    def new(*shape, dtype=torch.bfloat16):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+    f32, u8 = torch.float32, torch.uint8
+    sizes = {"qkv": (3 * C, C), "out": (C, C)}
+    P = {}   # of each projection: weight and bias, their gradients and states, codes of the weight and its transpose
+    for name, (rows, cols) in sizes.items():
+        p = P[name] = {"weight": rand(rows, cols, size=cols ** -0.5, dtype=f32), "bias": torch.zeros(rows, device=dev), "dw": new(rows, cols, dtype=f32), "db": new(rows, dtype=f32),
+                       "codes": new(rows, -(-cols // 128) * 128, dtype=torch.int8), "scales": new(rows, dtype=f32), "codes_t": new(cols, -(-rows // 128) * 128, dtype=torch.int8),
+                       "scales_t": new(cols, dtype=f32), "fwd": new(rl.radial_linear_i8_fwd_workspace(M, rows, cols), dtype=u8),
+                       "bwd": new(rl.radial_linear_i8_bwd_workspace(M, rows, cols), dtype=u8), "quantise": new(rl.radial_quantize_rows_i8_workspace(rows, cols), dtype=u8)}
+        p["project"] = lambda x, y, p=p: rl.radial_linear_i8_fwd(x, p["codes"], p["scales"], y, p["fwd"], bias=p["bias"])
+        p["gradients"] = lambda dy, x, dx, p=p: rl.radial_linear_i8_bwd(dy, p["bwd"], x=x, wt_codes=p["codes_t"], wt_scales=p["scales_t"], dx=dx, dw=p["dw"], dbias=p["db"])
+        p["encode"] = lambda p=p: rl.radial_quantize_rows_i8(p["weight"], p["codes"], p["scales"], p["codes_t"], p["scales_t"], p["quantise"])
+        p["encode"]()
+    weights = [P[n][k] for n in P for k in ("weight", "bias")]
+    zeros = lambda block, dtype: [torch.zeros(-(-t.numel() // block), dtype=dtype, device=dev) for t in weights]  # noqa: E731
+    states = dict(firsts=zeros(1, u8), seconds=zeros(1, u8), first_scales=zeros(128, f32), second_scales=zeros(128, f32))
+    tensors = rl.adamw_tensors(weights, [P[n][k] for n in P for k in ("dw", "db")], **states, decay=[0.01, 0.0] * len(P))
+    plan = rl.radial_adamw_plan(tensors)
+    adamw_table = new(plan.table_bytes, dtype=u8)
+    rl.radial_adamw_table(tensors, plan, adamw_table)
+    norm, norm_ws = new(2, dtype=f32), new(rl.radial_grad_norm_workspace(plan), dtype=u8)
+    count = torch.zeros(1, dtype=torch.int64, device=dev)
+
+    x, dz, dr, mod = rand(B, N, C), rand(B, N, C, size=0.02), rand(B, N, C, size=0.02), rand(B, 1, 6, C, size=0.3, dtype=f32)
+    params = rl.rope_params([w.frames, w.grid_h, w.grid_w], [16, D // 2 - 8, D // 2 - 8])
+    table = new(rl.radial_rope_table_bytes(params) // 4, dtype=f32)
+    rl.radial_rope_table(params, table)
+    mask = rb.radial_mask_build(w.frames, w.tokens_per_frame, w.block, 1, rb.RADIAL_MASK_TRANSPOSE)
+    h, o, z, r, attn, dx, do, dattn, dh, da = (torch.empty_like(x) for _ in range(10))
+    qkv, dqkv = new(B, N, 3, H, D), new(B, N, 3, H, D)
+    q, k, dq, dk = (new(B, H, N, D) for _ in range(4))
+    lse, dmod = new(B, H, N, dtype=f32), torch.empty_like(mod)
+    norm_bwd_ws, attn_ws = new(rl.radial_norm_bwd_workspace(B, N, C), dtype=u8), new(rb.radial_attn_bwd_workspace(B, H, N, D, mask), dtype=u8)
+    flat, heads = (lambda t: t.view(M, -1)), (lambda t, i: t[:, :, i].transpose(1, 2))
+    by_head = lambda t: t.view(B, N, H, D).transpose(1, 2)  # noqa: E731
+    m = lambda t, i: t[:, :, i]  # noqa: E731
+    parts = [
+        ("norm", lambda: rl.radial_norm_fwd(x, None, h, scale=m(mod, 0), shift=m(mod, 1))),
+        ("project_qkv", lambda: P["qkv"]["project"](flat(h), flat(qkv))),
+        ("rotary", lambda: rl.radial_rope_fwd(params, table, heads(qkv, 0), q, heads(qkv, 1), k)),
+        ("attention", lambda: rb.radial_attn_fwd(q, k, heads(qkv, 2), by_head(attn), lse, mask, w.scale)),
+        ("project_out", lambda: P["out"]["project"](flat(attn), flat(o))),
+        ("residual_norm", lambda: rl.radial_norm_fwd(x, r, z, y=o, gate=m(mod, 2), scale=m(mod, 3), shift=m(mod, 4))),
+        ("residual_norm_bwd", lambda: rl.radial_norm_bwd(r, dz, dx, norm_bwd_ws, dr=dr, y=o, dy=do, gate=m(mod, 2), scale=m(mod, 3), dgate=m(dmod, 2), dscale=m(dmod, 3), dshift=m(dmod, 4))),
+        ("project_out_bwd", lambda: P["out"]["gradients"](flat(do), flat(attn), flat(dattn))),
+        ("attention_bwd", lambda: rb.radial_attn_bwd(q, k, heads(qkv, 2), by_head(attn), by_head(dattn), lse, dq, dk, heads(dqkv, 2), mask, w.scale, attn_ws)),
+        ("rotary_bwd", lambda: rl.radial_rope_bwd(params, table, dq, heads(dqkv, 0), dk, heads(dqkv, 1))),
+        ("project_qkv_bwd", lambda: P["qkv"]["gradients"](flat(dqkv), flat(h), flat(dh))),
+        ("norm_bwd", lambda: rl.radial_norm_bwd(x, dh, da, norm_bwd_ws, dr=dx, scale=m(mod, 0), dscale=m(dmod, 0), dshift=m(dmod, 1))),
+        ("grad_norm", lambda: rl.radial_grad_norm(plan, adamw_table, norm, norm_ws, max_norm=1.0)),
+        ("adamw", lambda: (count.add_(1), rl.radial_adamw_step(plan, adamw_table, lr=1e-4, step_at=count, factor=norm, rounding="random", seed=w.seed))),
+        ("encode_weights", lambda: [p["encode"]() for p in P.values()]),
+    ]
+    ms = _time_parts(parts, args)
+    mask.free()
+    total = sum(ms.values())
+    print(json.dumps({"metric": "tuning step of the attention half of a layer", "value": round(total, 3), "unit": "ms", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
+                      "higher_is_better": False, "dtype": "bf16, projections in 8-bit integers, float32 weights, AdamW states in 8 bits", "data": "synthetic",
+                      "config": {"model": w.name, "global_batch": B, "seq_len": N, "hidden": C, "weights": sum(t.numel() for t in weights)},
+                      "ms": {n: round(t, 4) for n, t in ms.items()}}))
 
 
 def main():
@@ -389,6 +474,8 @@ def main():
     ap.add_argument("--curve-heads", type=int, default=2)
     ap.add_argument("--layer", action="store_true",
                     help="instead of the benchmark line: the attention half of a layer at the workload's sizes, part by part")
+    ap.add_argument("--layer-step", action="store_true",
+                    help="instead of the benchmark line: a tuning step of the attention half of a layer, projections in 8-bit integers, part by part")
     ap.add_argument("--secondary", default="cfg2_wan480p,cfg4_hunyuan720p_4x,cfg5_wan480p_4x_bwd", metavar="W1,W2,...",
                     help="other workloads reported in the line's `secondary` array (kernel times only; 'none' to skip)")
     ap.add_argument("--secondary-launches", type=int, default=2)
@@ -415,6 +502,9 @@ def main():
     w = wl.WORKLOADS[args.workload]
     if args.layer:
         layer_times(w, args)
+        return
+    if args.layer_step:
+        layer_step_times(w, args)
         return
     width_num, width_den = (int(t) for t in args.width_scale.split("/"))
     dev = "cuda:0"

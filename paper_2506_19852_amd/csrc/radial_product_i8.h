@@ -55,6 +55,7 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 // more (off by half a unit and 2^-46 of the value); adding 1.5 * 2^23 rounds it to whole, ties to even.
 struct Code {
   float scale, inverse;
+  Code() = default;
   __device__ __forceinline__ explicit Code(uint32_t largest) {
     const float amax = __builtin_bit_cast(float, largest);
     scale = largest < kInfinityBits ? fmaxf(amax / kLargestCode, kSmallestCodeScale) : __builtin_nanf("");

@@ -79,11 +79,11 @@ __global__ void __launch_bounds__(256) quantize_rows_i8_kernel(Job a) {
 
 // First pass: largest magnitudes and sums of the columns of a slab of rows, and of each row of the 512 columns, where they are wanted: a wave takes every fourth row, a
 // lane eight columns.
-constexpr int kAtOnce = 8;  // rows of a wave under way
+constexpr int kLookWaves = 4, kAtOnce = 8;  // waves of a workgroup, rows of a wave under way
 template <class T>
-__global__ void __launch_bounds__(256) look_over_kernel(Jobs jobs) {
-  __shared__ uint32_t of_wave[4][512];
-  __shared__ float sum_of_wave[4][512];
+__global__ void __launch_bounds__(64 * kLookWaves) look_over_kernel(Jobs jobs) {
+  __shared__ uint32_t of_wave[kLookWaves][512];
+  __shared__ float sum_of_wave[kLookWaves][512];
   const bool second = (int32_t)blockIdx.x >= jobs.first_of_second;
   const Job& a = jobs.job[second];
   const int32_t id = blockIdx.x - (second ? jobs.first_of_second : 0);
@@ -93,11 +93,11 @@ __global__ void __launch_bounds__(256) look_over_kernel(Jobs jobs) {
   uint32_t largest[8] = {};
   float sum[8] = {};
   const T* x = (const T*)a.x + c;
-  for (int32_t r = first + wave; r < last; r += 4 * kAtOnce) {
+  for (int32_t r = first + wave; r < last; r += kLookWaves * kAtOnce) {
     Eight<T> e[kAtOnce];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
-      const int32_t row = r + 4 * i;
+      const int32_t row = r + kLookWaves * i;
       e[i].load_some(x + (int64_t)min(row, last - 1) * a.stride, row < last ? a.cols - c : 0);
     }
 #pragma unroll
@@ -113,8 +113,9 @@ __global__ void __launch_bounds__(256) look_over_kernel(Jobs jobs) {
         sum[j] += v[j];
       }
       if (a.codes) {
+        const int32_t row = r + kLookWaves * i;
         of_row = wave_max(of_row);
-        if (lane == 0 && r + 4 * i < last) a.of_rows[(int64_t)tile * a.rows + r + 4 * i] = of_row;
+        if (lane == 0 && row < last) a.of_rows[(int64_t)tile * a.rows + row] = of_row;
       }
     }
   }
@@ -124,11 +125,17 @@ __global__ void __launch_bounds__(256) look_over_kernel(Jobs jobs) {
     sum_of_wave[wave][lane * 8 + j] = sum[j];
   }
   __syncthreads();
-  const int32_t c0 = tile * 512;
-  for (int32_t i = threadIdx.x; i < 512 && c0 + i < a.cols; i += 256) {
-    const int64_t at = (int64_t)slab * a.cols + c0 + i;
-    a.of_cols[at] = max(max(of_wave[0][i], of_wave[1][i]), max(of_wave[2][i], of_wave[3][i]));
-    if (a.sums_t) a.sums[at] = (sum_of_wave[0][i] + sum_of_wave[1][i]) + (sum_of_wave[2][i] + sum_of_wave[3][i]);
+  for (int32_t i = threadIdx.x; i < 512 && tile * 512 + i < a.cols; i += 64 * kLookWaves) {
+    const int64_t at = (int64_t)slab * a.cols + tile * 512 + i;
+    uint32_t all = 0;
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kLookWaves; ++w) {
+      all = max(all, of_wave[w][i]);
+      total += sum_of_wave[w][i];
+    }
+    a.of_cols[at] = all;
+    if (a.sums_t) a.sums[at] = total;
   }
 }
 
@@ -168,7 +175,7 @@ template <class T>
 __global__ void __launch_bounds__(256) quantize_tiles_i8_kernel(Jobs jobs) {
   __shared__ __align__(16) u32x2 turned[kCodeGroup * 16];
   __shared__ uint32_t half[2][kCodeGroup];
-  __shared__ uint32_t largest_of_row[kCodeGroup];
+  __shared__ Code of_col[kCodeGroup], of_row[kCodeGroup];
   const bool second = (int32_t)blockIdx.x >= jobs.first_of_second;
   const Job& a = jobs.job[second];
   const int32_t id = blockIdx.x - (second ? jobs.first_of_second : 0);
@@ -179,14 +186,19 @@ __global__ void __launch_bounds__(256) quantize_tiles_i8_kernel(Jobs jobs) {
     const int32_t c = threadIdx.x & 127, part = threadIdx.x >> 7;
     half[part][c] = col0 + c < a.cols ? largest_of(a.of_cols + (int64_t)part * a.cols + col0 + c, 2 * (int64_t)a.cols, (a.slabs + 1 - part) / 2) : 0u;
     __syncthreads();
-    if (strip == 0 && part == 0 && col0 + c < a.cols) {
-      a.scales_t[col0 + c] = Code(max(half[0][c], half[1][c])).scale;
-      if (a.sums_t) put_sum(a, col0 + c);
+    if (part == 0) {
+      const Code code(max(half[0][c], half[1][c]));
+      of_col[c] = code;
+      if (strip == 0 && col0 + c < a.cols) {
+        a.scales_t[col0 + c] = code.scale;
+        if (a.sums_t) put_sum(a, col0 + c);
+      }
     }
+    __syncthreads();
   }
-  uint32_t of_col[8];
+  Code mine[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) of_col[j] = max(half[0][tc * 8 + j], half[1][tc * 8 + j]);
+  for (int j = 0; j < 8; ++j) mine[j] = of_col[tc * 8 + j];
   for (int32_t tile = first; tile < last; ++tile) {
     const int32_t row0 = tile * kCodeGroup, r0 = row0 + tr * 8;
     float v[8][8];
@@ -200,20 +212,21 @@ __global__ void __launch_bounds__(256) quantize_tiles_i8_kernel(Jobs jobs) {
     if (a.codes) {
       if (threadIdx.x < kCodeGroup) {
         const uint32_t largest = row0 + (int32_t)threadIdx.x < a.rows ? largest_of(a.of_rows + row0 + threadIdx.x, a.rows, a.wide_tiles) : 0u;
-        largest_of_row[threadIdx.x] = largest;
-        if (col0 == 0 && row0 + (int32_t)threadIdx.x < a.rows) a.scales[row0 + threadIdx.x] = Code(largest).scale;
+        const Code code(largest);
+        of_row[threadIdx.x] = code;
+        if (col0 == 0 && row0 + (int32_t)threadIdx.x < a.rows) a.scales[row0 + threadIdx.x] = code.scale;
       }
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const Code code(largest_of_row[tr * 8 + i]);
+        const Code code = of_row[tr * 8 + i];
         if (r0 + i < a.rows)
           *(u32x2*)(a.codes + (int64_t)(r0 + i) * a.pitch + c0) = u32x2{code.four(v[i][0], v[i][1], v[i][2], v[i][3]), code.four(v[i][4], v[i][5], v[i][6], v[i][7])};
       }
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const Code code(of_col[j]);
+      const Code& code = mine[j];
       turned[(tc * 8 + j) * 16 + (tr ^ tc)] = u32x2{code.four(v[0][j], v[1][j], v[2][j], v[3][j]), code.four(v[4][j], v[5][j], v[6][j], v[7][j])};
     }
     __syncthreads();
@@ -263,10 +276,10 @@ int launch_passes(const Job* job, int count, hipStream_t stream) {
     looks += (int64_t)job[i].wide_tiles * job[i].slabs;
   }
   if (count == 1) jobs.first_of_second = 0x7fffffff;
-  if (looks > kMostThreads / 256) return fail(RADIAL_ESHAPE, "x is too large for one launch");
+  if (looks > kMostThreads / (64 * kLookWaves)) return fail(RADIAL_ESHAPE, "x is too large for one launch");
   for (int i = 0; i < count; ++i) tiles += (int64_t)job[i].col_tiles * job[i].strips;
   if (tiles > kMostThreads / 256) return fail(RADIAL_ESHAPE, "x is too large for one launch");
-  look_over_kernel<T><<<dim3((unsigned)looks), dim3(256), 0, stream>>>(jobs);
+  look_over_kernel<T><<<dim3((unsigned)looks), dim3(64 * kLookWaves), 0, stream>>>(jobs);
   RADIAL_HIP_TRY(hipGetLastError());
   if (!job[0].codes_t) {
     put_sums_kernel<<<dim3((unsigned)(((int64_t)job[0].cols + 63) / 64)), dim3(64), 0, stream>>>(job[0]);
