@@ -220,7 +220,7 @@ RADIAL_API int radial_product_i8(int32_t M, int32_t N, int32_t K, const int8_t* 
 /* A projection y = x W^T + bias, x [M, K], W [N, K], in 8-bit integers: x is quantised by rows and multiplied.
  *   w_codes, w_scales : of W (radial_quantize_rows_i8 of W, after each update of it);
  *   workspace         : radial_linear_i8_fwd_workspace(M, N, K) bytes, 256-byte aligned, contents ignored and undefined afterwards.
- * The other arguments and the errors are those of the two calls above. */
+ * y shares no memory with x.  The other arguments and the errors are those of the two calls above. */
 RADIAL_API size_t radial_linear_i8_fwd_workspace(int32_t M, int32_t N, int32_t K);
 RADIAL_API int radial_linear_i8_fwd(int32_t M, int32_t N, int32_t K, const void* x, int32_t type, int64_t x_stride, const int8_t* w_codes,
                                     const float* w_scales, const float* bias, void* y, int32_t y_type, int64_t y_stride, void* workspace,
@@ -232,6 +232,7 @@ RADIAL_API int radial_linear_i8_fwd(int32_t M, int32_t N, int32_t K, const void*
  *   x, dw                   : the forward's x [M, K] of dy's type, and dw [N, K]; dw NULL: not wanted, then x is not read;
  *   dbias                   : device float [N], or NULL: not wanted;
  *   accumulate              : != 0: dw, which is float32, and dbias are added to;
+ *   outputs share no memory with dy and x;
  *   workspace               : radial_linear_i8_bwd_workspace(M, N, K) bytes, 256-byte aligned, contents ignored and undefined afterwards. */
 RADIAL_API size_t radial_linear_i8_bwd_workspace(int32_t M, int32_t N, int32_t K);
 RADIAL_API int radial_linear_i8_bwd(int32_t M, int32_t N, int32_t K, const void* dy, int32_t type, int64_t dy_stride, const void* x,

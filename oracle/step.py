@@ -44,12 +44,12 @@ def mixed(x):
     return x ^ (x >> np.uint64(16))
 
 
-def random_bits(seed, step, tensor, n):
-    """(bits of the first, of the second state) of the n values of a tensor."""
+def random_bits(seed, step, tensor, n, first=0):
+    """(bits of the first, of the second state) of n values of a tensor from `first` on, all on one side of each multiple of 2^32."""
     key = np.uint64(0)
-    for word in (seed & 0xFFFFFFFF, seed >> 32, step & 0xFFFFFFFF, tensor):
+    for word in (seed & 0xFFFFFFFF, seed >> 32, step & 0xFFFFFFFF, tensor) + ((first >> 32,) if first >> 32 else ()):
         key = mixed(key ^ np.uint64(word))
-    h = mixed(key ^ np.arange(n, dtype=np.uint64))
+    h = mixed(key ^ (np.arange(n, dtype=np.uint64) + np.uint64(first & 0xFFFFFFFF)))
     return (h & np.uint64(0xFFFF)).astype(np.int64), (h >> np.uint64(16)).astype(np.int64)
 
 

@@ -244,7 +244,7 @@ __device__ __forceinline__ uint32_t random_code(float y, uint32_t bits16) {
 }
 
 // Quotients and roots without the steps of the library functions that cover tiny and huge operands, and without those for the last bit where nothing hangs on it: 85 instructions
-// a value became 51, and 105 million bf16 weights with bf16 gradients and states in 8 bits took 200 us instead of 297.
+// a value became 55, and 105 million bf16 weights with bf16 gradients and states in 8 bits took 200 us instead of 297.
 //
 // a / 448: product with the inverse, and what it leaves once more.
 __device__ __forceinline__ float over_448(float a) {

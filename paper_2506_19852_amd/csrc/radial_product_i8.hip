@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) __attribute__
   const int lane = threadIdx.x & 63, wave_of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int part = kSplit == 1 ? 0 : wave_of_all / S::kWaves, wave = wave_of_all - part * S::kWaves;
   int32_t m0, n0;
-  tile_of(blockIdx.x, (a.M + S::kTileM - 1) / S::kTileM, (a.N + S::kTileN - 1) / S::kTileN, m0, n0);
+  tile_of<kBandI8>(blockIdx.x, (a.M + S::kTileM - 1) / S::kTileM, (a.N + S::kTileN - 1) / S::kTileN, m0, n0);
   m0 *= S::kTileM;
   n0 *= S::kTileN;
   const int8_t* a_base = a.a + m0 * a.a_row;
@@ -363,7 +363,7 @@ int launch_form(int form, const ProductArgs& a, hipStream_t stream) {
   switch (form) {
     case 0: return launch_tiles<2, 4, 8, 2, 1>(a, stream);
     case 1: return launch_tiles<2, 4, 6, 2, 1>(a, stream);
-    case 2: return launch_tiles<2, 2, 4, 2, 1>(a, stream);
+    case 2: return launch_tiles<4, 2, 2, 2, 1>(a, stream);
     case 3: return launch_tiles<4, 2, 2, 3, 1>(a, stream);
     case 4: return launch_tiles<2, 2, 3, 3, 1>(a, stream);
     case 5: return launch_tiles<4, 2, 1, 3, 1>(a, stream);

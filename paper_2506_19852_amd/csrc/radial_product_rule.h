@@ -75,10 +75,11 @@ inline ProductPlan plan_product(int32_t M, int32_t N, int32_t groups, const Tile
 inline int64_t pieces_of(int32_t n) { return ((int64_t)n + 15) / 16; }
 inline bool takes_pieces(int32_t M, int32_t N) { return M <= 16 || pieces_of(M) * pieces_of(N) <= kComputeUnits; }
 
-// Tile of a workgroup.  XCD x of 8 (workgroup id mod 8) gets a run of neighbouring tiles, in bands of 8 rows of tiles, column by column: the 32 that
+// Tile of a workgroup.  XCD x of 8 (workgroup id mod 8) gets a run of neighbouring tiles, in bands of kBand rows of tiles, column by column: the 32 that
 // it works on at a time are 8 x 4, whose codes it fetches into its L2 once.
+template <uint32_t kBand = 8>
 __host__ __device__ __forceinline__ void tile_of(uint32_t id, int32_t tiles_m, int32_t tiles_n, int32_t& m, int32_t& n) {
-  constexpr uint32_t kXcds = 8, kBand = 8;
+  constexpr uint32_t kXcds = 8;
   const uint32_t tiles = (uint32_t)tiles_m * tiles_n, each = tiles / kXcds, more = tiles % kXcds;
   const uint32_t xcd = id % kXcds, at = xcd * each + (xcd < more ? xcd : more) + id / kXcds;
   const uint32_t band = at / (kBand * tiles_n), in_band = at - band * kBand * tiles_n;

@@ -27,12 +27,15 @@ struct Jobs {
   int32_t first_of_second;  // workgroup
 };
 
-// Codes along the rows: a wave takes a row, a lane eight columns of every 512.  kPieces pieces of 512 stay in registers between the largest magnitude
-// and the codes; longer rows (kPieces 0) are read twice.
-template <class T, int kPieces>
+// Codes along the rows: kTeam waves take a row, a lane eight columns of every 512 kTeam.  kPieces pieces stay in registers between the largest magnitude
+// and the codes; longer rows (kPieces 0) are read twice.  Few rows take four waves each (512 x 4096: 4.5 us, with one 5.2).
+template <class T, int kPieces, int kTeam>
 __global__ void __launch_bounds__(256) quantize_rows_i8_kernel(Job a) {
-  const int32_t lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= a.rows) return;
+  __shared__ uint32_t of_wave[4];
+  constexpr int kStep = 512 * kTeam;
+  const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = kTeam == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+  if (row >= a.rows) return;  // kTeam 4: there is a row for each workgroup
+  const int32_t at = lane * 8 + (kTeam == 1 ? 0 : wave * 512);
   const T* x = (const T*)a.x + row * a.stride;
   const int32_t padded = a.col_tiles * kCodeGroup;
   int8_t* codes = a.codes + row * a.pitch;
@@ -48,18 +51,24 @@ __global__ void __launch_bounds__(256) quantize_rows_i8_kernel(Job a) {
   if constexpr (kPieces > 0) {
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
-      const int32_t c = p * 512 + lane * 8;
+      const int32_t c = p * kStep + at;
       held[p].load_some(x + c, a.cols - c);
     }
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) look(held[p]);
   } else {
-    for (int32_t c = lane * 8; c < a.cols; c += 512) {
+    for (int32_t c = at; c < a.cols; c += kStep) {
       held[0].load_some(x + c, a.cols - c);
       look(held[0]);
     }
   }
-  const Code code(wave_max(largest));
+  largest = wave_max(largest);
+  if constexpr (kTeam > 1) {
+    if (lane == 0) of_wave[wave] = largest;
+    __syncthreads();
+    largest = max(max(of_wave[0], of_wave[1]), max(of_wave[2], of_wave[3]));
+  }
+  const Code code(largest);
   auto put = [&](const Eight<T>& e, int32_t c) __attribute__((always_inline)) {
     float v[8];
     e.get(v);
@@ -67,14 +76,14 @@ __global__ void __launch_bounds__(256) quantize_rows_i8_kernel(Job a) {
   };
   if constexpr (kPieces > 0) {
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p) put(held[p], p * 512 + lane * 8);
+    for (int p = 0; p < kPieces; ++p) put(held[p], p * kStep + at);
   } else {
-    for (int32_t c = lane * 8; c < padded; c += 512) {
+    for (int32_t c = at; c < padded; c += kStep) {
       held[0].load_some(x + c, a.cols - c);
       put(held[0], c);
     }
   }
-  if (lane == 0) a.scales[row] = code.scale;
+  if (lane == 0 && (kTeam == 1 || wave == 0)) a.scales[row] = code.scale;
 }
 
 // First pass: largest magnitudes and sums of the columns of a slab of rows, and of each row of the 512 columns, where they are wanted: a wave takes every fourth row, a
@@ -151,21 +160,22 @@ __device__ __forceinline__ uint32_t largest_of(const uint32_t* p, int64_t step, 
   }
   return largest;
 }
-// The sum of a column over the slabs, in order, eight asked for at a time.
-__device__ __forceinline__ void put_sum(const Job& a, int32_t c) {
+// The sum of a column over every `step`th slab from `first` on, in order, eight asked for at a time.
+__device__ __forceinline__ float sum_of(const Job& a, int32_t c, int32_t first, int32_t step) {
   float all = 0.f;
-  for (int32_t s = 0; s < a.slabs; s += 8) {
+  for (int32_t s = first; s < a.slabs; s += 8 * step) {
     float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = a.sums[(int64_t)min(s + j, a.slabs - 1) * a.cols + c];
+    for (int j = 0; j < 8; ++j) v[j] = a.sums[(int64_t)min(s + j * step, a.slabs - 1) * a.cols + c];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) all += s + j < a.slabs ? v[j] : 0.f;
+    for (int j = 0; j < 8; ++j) all += s + j * step < a.slabs ? v[j] : 0.f;
   }
-  a.sums_t[c] = a.accumulate ? a.sums_t[c] + all : all;
+  return all;
 }
+__device__ __forceinline__ void put_sum(const Job& a, int32_t c, float sum) { a.sums_t[c] = a.accumulate ? a.sums_t[c] + sum : sum; }
 __global__ void __launch_bounds__(64) put_sums_kernel(Job a) {
   const int32_t c = blockIdx.x * 64 + threadIdx.x;
-  if (c < a.cols) put_sum(a, c);
+  if (c < a.cols) put_sum(a, c, sum_of(a, c, 0, 1));
 }
 
 // Second pass, by tiles of 128 x 128, a strip of them one below the other for each workgroup: the largest magnitudes of its rows and columns are put together, then a
@@ -175,6 +185,7 @@ template <class T>
 __global__ void __launch_bounds__(256) quantize_tiles_i8_kernel(Jobs jobs) {
   __shared__ __align__(16) u32x2 turned[kCodeGroup * 16];
   __shared__ uint32_t half[2][kCodeGroup];
+  __shared__ float half_sum[2][kCodeGroup];
   __shared__ Code of_col[kCodeGroup], of_row[kCodeGroup];
   const bool second = (int32_t)blockIdx.x >= jobs.first_of_second;
   const Job& a = jobs.job[second];
@@ -184,6 +195,8 @@ __global__ void __launch_bounds__(256) quantize_tiles_i8_kernel(Jobs jobs) {
   const int32_t tr = threadIdx.x >> 4, tc = threadIdx.x & 15, c0 = col0 + tc * 8;
   {
     const int32_t c = threadIdx.x & 127, part = threadIdx.x >> 7;
+    const bool sums = a.sums_t && strip == 0 && col0 + c < a.cols;
+    if (sums) half_sum[part][c] = sum_of(a, col0 + c, part, 2);
     half[part][c] = col0 + c < a.cols ? largest_of(a.of_cols + (int64_t)part * a.cols + col0 + c, 2 * (int64_t)a.cols, (a.slabs + 1 - part) / 2) : 0u;
     __syncthreads();
     if (part == 0) {
@@ -191,7 +204,7 @@ __global__ void __launch_bounds__(256) quantize_tiles_i8_kernel(Jobs jobs) {
       of_col[c] = code;
       if (strip == 0 && col0 + c < a.cols) {
         a.scales_t[col0 + c] = code.scale;
-        if (a.sums_t) put_sum(a, col0 + c);
+        if (sums) put_sum(a, col0 + c, half_sum[0][c] + half_sum[1][c]);
       }
     }
     __syncthreads();
@@ -241,26 +254,38 @@ __global__ void __launch_bounds__(256) quantize_tiles_i8_kernel(Jobs jobs) {
 }
 
 inline int32_t at_most(int64_t wanted, int64_t most) { return (int32_t)(wanted < most ? wanted : most); }
-// Slabs of the first pass: two workgroups for each compute unit, of 16 rows at least.
+// Slabs of the first pass: two workgroups for each compute unit, of 32 rows at least (the second pass reads a value of each slab).
 inline int32_t slabs_of(int32_t rows, int32_t cols) {
   const int64_t tiles = ((int64_t)cols + 511) / 512;
-  return at_most((512 + tiles - 1) / tiles, ((int64_t)rows + 15) / 16);
+  return at_most((512 + tiles - 1) / tiles, ((int64_t)rows + 31) / 32);
 }
 // Strips of the second: four workgroups for each compute unit, as long as there are tiles.
 inline int32_t strips_of(int32_t rows, int32_t cols) { return at_most((1024 + code_groups(cols) - 1) / code_groups(cols), code_groups(rows)); }
 
 template <class T>
 int launch_rows(const Job& a, hipStream_t stream) {
-  if (((int64_t)a.rows + 3) / 4 > kMostThreads / 256) return fail(RADIAL_ESHAPE, "x is too large for one launch");
-  const dim3 grid((unsigned)(((int64_t)a.rows + 3) / 4)), threads(256);
-  const int64_t pieces = ((int64_t)a.col_tiles * kCodeGroup + 511) / 512;
-  if (pieces <= 1) quantize_rows_i8_kernel<T, 1><<<grid, threads, 0, stream>>>(a);
-  else if (pieces <= 2) quantize_rows_i8_kernel<T, 2><<<grid, threads, 0, stream>>>(a);
-  else if (pieces <= 4) quantize_rows_i8_kernel<T, 4><<<grid, threads, 0, stream>>>(a);
-  else if (pieces <= 6) quantize_rows_i8_kernel<T, 6><<<grid, threads, 0, stream>>>(a);
-  else if (pieces <= 10) quantize_rows_i8_kernel<T, 10><<<grid, threads, 0, stream>>>(a);
-  else if (pieces <= 16) quantize_rows_i8_kernel<T, 16><<<grid, threads, 0, stream>>>(a);
-  else quantize_rows_i8_kernel<T, 0><<<grid, threads, 0, stream>>>(a);
+  const bool few = a.rows <= 2048;  // two rounds of four waves a row on the chip's compute units
+  const int64_t groups = few ? a.rows : ((int64_t)a.rows + 3) / 4;
+  if (groups > kMostThreads / 256) return fail(RADIAL_ESHAPE, "x is too large for one launch");
+  const dim3 grid((unsigned)groups), threads(256);
+  const int64_t pieces = ((int64_t)a.col_tiles * kCodeGroup + (few ? 2047 : 511)) / (few ? 2048 : 512);
+  if (few) {
+    if (pieces <= 1) quantize_rows_i8_kernel<T, 1, 4><<<grid, threads, 0, stream>>>(a);
+    else if (pieces <= 3) quantize_rows_i8_kernel<T, 3, 4><<<grid, threads, 0, stream>>>(a);
+    else quantize_rows_i8_kernel<T, 0, 4><<<grid, threads, 0, stream>>>(a);
+  } else if (pieces <= 2) {
+    quantize_rows_i8_kernel<T, 2, 1><<<grid, threads, 0, stream>>>(a);
+  } else if (pieces <= 4) {
+    quantize_rows_i8_kernel<T, 4, 1><<<grid, threads, 0, stream>>>(a);
+  } else if (pieces <= 6) {
+    quantize_rows_i8_kernel<T, 6, 1><<<grid, threads, 0, stream>>>(a);
+  } else if (pieces <= 10) {
+    quantize_rows_i8_kernel<T, 10, 1><<<grid, threads, 0, stream>>>(a);
+  } else if (pieces <= 16) {
+    quantize_rows_i8_kernel<T, 16, 1><<<grid, threads, 0, stream>>>(a);
+  } else {
+    quantize_rows_i8_kernel<T, 0, 1><<<grid, threads, 0, stream>>>(a);
+  }
   RADIAL_HIP_TRY(hipGetLastError());
   return RADIAL_OK;
 }

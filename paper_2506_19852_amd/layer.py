@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import ctypes
 import numbers
+import operator
 from ctypes import POINTER, byref, c_double, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 
 from . import binding
@@ -608,6 +609,7 @@ def radial_adamw_step(plan: radial_adamw_plan_info, table, *, lr: float = 0.0, s
     device = _device()
     if rounding not in _ROUNDINGS:
         raise ValueError(f"rounding must be one of {', '.join(_ROUNDINGS)}")
+    seed, step = operator.index(seed), operator.index(step)
     if not 0 <= seed < 1 << 64 or step >> 63:
         raise ValueError("seed must be below 2^64 and step below 2^63, neither negative")
     by = _vector(factor, "factor", 2, device)

@@ -389,3 +389,35 @@ def test_a_table_of_no_values():
     group.step(factor=group.norm)
     torch.cuda.synchronize()
     assert group.plan.pieces == 0 and to64(group.norm).tolist() == [0.0, 1.0] and group.guards_kept()
+
+
+def test_a_tensor_of_more_than_2_to_the_32_values():
+    """Values on both sides of 2^31 and 2^32 and at the end, with the bits of their own; 26 GB."""
+    n, big = (1 << 32) + 4500, dict(device=DEV)
+    w, g = torch.zeros(n, dtype=BF16, **big), torch.zeros(n, dtype=BF16, **big)
+    m, v = torch.zeros(n, dtype=torch.uint8, **big), torch.zeros(n, dtype=torch.uint8, **big)
+    ms, vs = (torch.zeros(-(-n // 128), **big) for _ in range(2))
+    tensors = rl.adamw_tensors([w], [g], [m], [v], first_scales=[ms], second_scales=[vs], decay=0.1)
+    plan = rl.radial_adamw_plan(tensors)
+    table = torch.empty(plan.table_bytes, dtype=torch.uint8, **big)
+    rl.radial_adamw_table(tensors, plan, table)
+    norm, work = torch.empty(2, **big), torch.empty(rl.radial_grad_norm_workspace(plan), dtype=torch.uint8, **big)
+    spans = [(0, 256), ((1 << 31) - 256, 256), (1 << 31, 256), ((1 << 32) - 256, 256), (1 << 32, 256), (n - 404, 404)]   # whole blocks; the last one is of 20 values
+    gen, total = np.random.default_rng(9), 0.0
+    for at, k in spans:
+        g[at:at + k] = torch.tensor(gen.normal(size=k) * 1e-3, device=DEV).to(BF16)
+        total += float((g[at:at + k].double() ** 2).sum())
+    rl.radial_grad_norm(plan, table, norm, work)
+    rl.radial_adamw_step(plan, table, lr=LR, step=3, rounding="random", seed=1 << 40)
+    torch.cuda.synchronize()
+    assert abs(float(norm[0]) - np.sqrt(total)) <= 2 * U32 * np.sqrt(total)
+    for at, k in spans:
+        x = g[at:at + k].float().cpu().numpy()
+        m1, v1 = os_.moments(x, np.zeros(k, np.float32), np.zeros(k, np.float32), BETA1, BETA2)
+        bits = os_.random_bits(1 << 40, 3, 0, k, at)
+        for got, scales, value, b, positive in ((m, ms, m1, bits[0], False), (v, vs, np.sqrt(v1), bits[1], True)):
+            codes, want = os_.encode(value, b, positive)
+            assert np.array_equal(got[at:at + k].cpu().numpy(), codes) and np.array_equal(scales[at // 128:-(-(at + k) // 128)].cpu().numpy(), want), at
+        want = os_.update(np.zeros(k), m1.astype(np.float64), v1.astype(np.float64), LR, 3, BETA1, BETA2, EPS, 0.1)
+        assert_within(w[at:at + k], want, HALF_STEP[BF16] * np.abs(want) * 1.01, f"w at {at}")
+    assert not m[256:(1 << 31) - 256].any() and not w[(1 << 31) + 256:(1 << 32) - 256].any() and int(m.count_nonzero()) <= sum(k for _, k in spans)

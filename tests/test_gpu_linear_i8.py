@@ -49,7 +49,7 @@ def spread_values(rows, cols, seed):
 # ---- codes --------------------------------------------------------------------------------------
 
 # a width of each number of pieces that a wave keeps, and beyond
-SHAPES = [(1, 1), (3, 200), (128, 128), (129, 127), (5, 1000), (257, 384), (40, 2048), (1000, 40), (2, 5120), (7, 2999), (3, 8192), (2, 8200), (4, 20001), (300, 513)]
+SHAPES = [(1, 1), (3, 200), (128, 128), (129, 127), (5, 1000), (257, 384), (40, 2048), (1000, 40), (2, 5120), (7, 2999), (3, 8192), (2, 8200), (4, 20001), (300, 513), (5, 2049), (6, 6144), (7, 6145), (2049, 900), (2050, 1500), (2051, 2050), (2052, 3000), (2053, 5000), (2054, 8000), (2055, 8193)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])

@@ -30,7 +30,7 @@ def kernels(tmp_path_factory):
     return out
 
 
-@pytest.mark.parametrize("source, count", [("radial_quantize_i8", 2 * 9 + 1), ("radial_product_i8", 10 + 1 + 6), ("radial_adamw", 5)])
+@pytest.mark.parametrize("source, count", [("radial_quantize_i8", 2 * (6 + 3 + 2) + 1), ("radial_product_i8", 10 + 1 + 6), ("radial_adamw", 5)])
 def test_no_scratch_memory(kernels, source, count):
     assert len(kernels[source]) == count and not any(size for size, _ in kernels[source].values()), {k: v[0] for k, v in kernels[source].items()}
 

@@ -53,3 +53,10 @@ def test_rows_left_over_are_behind_whole_tiles(rule):
 def test_large_products_take_large_tiles_and_few_rows_parts_of_the_groups(rule):
     large, few = rule(["form 32760 5120 40", "form 64 5120 40"])
     assert large[1:4] == [256, 256, 1] and few[1:3] == [32, 64] and few[3] > 1
+
+
+@pytest.mark.parametrize("shape", [(1, 1), (1, 20), (20, 1), (5, 3), (6, 6), (7, 5), (12, 7), (128, 20), (17, 33)], ids=str)
+def test_every_tile_is_taken_once(rule, shape):
+    (flat,) = rule([f"tiles {shape[0]} {shape[1]}"])
+    got = {(flat[i], flat[i + 1]) for i in range(0, len(flat), 2)}
+    assert len(flat) == 2 * shape[0] * shape[1] and got == {(m, n) for m in range(shape[0]) for n in range(shape[1])}

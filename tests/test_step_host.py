@@ -260,6 +260,16 @@ def test_step_marshalling(one_device):  # noqa: F811
             rl.radial_grad_norm(plan, a["table"], a["norm"], a["workspace"], stream=1)
 
 
+def test_numbers_of_numpy(one_device):  # noqa: F811
+    array = rl.adamw_tensors(**_lists(), decay=np.float32(0.5))
+    assert [e.decay for e in array] == [0.5, 0.5]
+    _, plan, _ = _plan(_tensor())
+    with pytest.raises(rb.RadialError, match="needed"):   # the last check before the launch
+        rl.radial_adamw_step(plan, _fake(U8, plan.table_bytes - 1), lr=np.float32(1e-3), step=np.int64(3), seed=np.int32(5), eps=np.float64(1e-8), stream=1)
+    with pytest.raises(TypeError):
+        rl.radial_adamw_step(plan, _fake(U8, plan.table_bytes), lr=1e-3, step=1.5, stream=1)
+
+
 # ---- the oracle itself --------------------------------------------------------------------------
 
 def test_codes_of_the_oracle():
