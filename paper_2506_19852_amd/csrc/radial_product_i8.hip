@@ -67,7 +67,7 @@ __device__ __forceinline__ void put(const ProductArgs& a, int32_t m, int32_t n, 
 }
 
 // Few rows, or few results: a workgroup of 8 waves takes 16 x 16 of C, each wave every 8th group, straight from memory (a lane's 32 bytes of a row, four
-// lanes a line); the parts meet in LDS.
+// lanes a line); the parts meet in LDS.  (1 x 5120 x 5120 7.7 us; two or four times the rows for a workgroup were slower: 64 x 5120 x 5120 22 to 24 us, in tiles of 32 x 64 8.5.)
 constexpr int kParts = 8;
 
 // The sums of the parts, scaled: wave 0 holds them, column n0 + 4 (lane / 16) on, row m.
@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(64 * kParts) product_i8_pieces_kernel(ProductA
 }
 
 // A projection of up to 4 rows of up to 8192 columns in one launch: every workgroup quantises the rows for itself, into LDS, while the first groups of its weights are under
-// way, and goes on as above.
+// way, and goes on as above.  Bound by reading W: 2 x 5120 x 5120 8.2 us, 3.2 TB/s, of which a launch is three to four (in two launches 4.8 + 8.6).
 constexpr int kFewRows = 4, kFewCols = 8192, kUnderWay = 5;
 template <class T, int kRows>
 __global__ void __launch_bounds__(64 * kParts) linear_i8_few_kernel(ProductArgs a, const T* x, int64_t stride, int32_t cols) {
@@ -181,6 +181,11 @@ __global__ void __launch_bounds__(64 * kParts) linear_i8_few_kernel(ProductArgs 
 
 // Many rows: a workgroup takes a tile of 16 kMTiles kWavesM x 64 kWavesN, stage by stage of one group (128 bytes of every row), which copies put into LDS
 // kStages - 1 stages ahead, straight from memory.  kSplit parts of the workgroup's waves take the groups in turn and add up their sums at the end.
+// 256 x 256 tiles, eight waves, two a SIMD: 32 760 x 5120 x 5120 660-690 us over boxes (2.5-2.6 POP/s; a large library product of whole numbers without scales takes 733-755), 8192^3 400
+// (2.75).  At 32 760 rows the matrix pipes are busy 54 % of the cycles at 2.2 GHz; with codes of zeros it takes 550 and 8192^3 318 (3.46 POP/s, 69 %): the board's power, then the reads of A from
+// beyond the last-level cache (a quarter of A's memory: 640).  What does not change the time: fragments read a stage ahead through rings of four and five
+// stages of 64 bytes (717 beside 700), four waves of 128 x 128 with a third fewer reads from LDS (750), A in blocks of 128 columns (708 beside 704).  Asking for lines of A three stages ahead
+// costs 50 us; tiles of 128 x 256, two workgroups a unit, 831.
 template <int kWavesM, int kWavesN, int kMTiles, int kStages, int kSplit>
 struct TileShape {
   static constexpr int kWaves = kWavesM * kWavesN;  // of one part of the groups

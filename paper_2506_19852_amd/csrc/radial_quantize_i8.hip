@@ -1,4 +1,7 @@
-// Codes of 8-bit integers for gfx950: a matrix with one float32 scale for each row, by rows, and by columns as the rows of its transpose.
+// Codes of 8-bit integers for gfx950: a matrix with one float32 scale for each row, by rows, and by columns as the rows of its transpose.  Bound by memory: a row's scale needs all of
+// the row, which stays in registers (32 760 x 5120 in bf16 91 us, 5.5 TB/s); a column's needs all of the column, so that columns take two passes over the matrix, the second
+// from the last-level cache as far as it goes (14 040 x 5120: columns 68 us, rows and columns 91; 5120 x 5120 32 and 43).  Within the gradients of a projection of that size the two
+// passes over both matrices take 230 us, the first from a cold cache at 3.1 TB/s.
 #include <math.h>
 
 #include "radial_layer_common.h"
