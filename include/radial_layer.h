@@ -306,7 +306,7 @@ typedef struct {
   int32_t rounding;             /* RADIAL_ROUND_*, of states in 8 bits                                              */
   const float* factor;          /* device, or NULL (1).  While it is not finite a step changes nothing at all       */
   const float* lr_at;           /* device, read in place of lr, or NULL                                              */
-  const int64_t* step_at;       /* device, read in place of step, or NULL: a captured step counts on in replays     */
+  const int64_t* step_at;       /* device, read in place of step (below 1: 1), or NULL: a captured step counts on in replays */
 } radial_adamw_params;
 
 /* One step for all tensors of the table.  Errors: EINVAL, ESHAPE (alignment), EHIP. */

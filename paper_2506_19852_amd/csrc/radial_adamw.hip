@@ -402,7 +402,8 @@ __global__ void __launch_bounds__(256) adamw_step_kernel(StepArgs a) {
   if (a.lr_at || a.step_at) {
     // from the device: 1 - beta^t as -(e^(t log beta) - 1), which keeps its digits where beta^t is near 1
     if (a.lr_at) lr = *a.lr_at;
-    const float step = (float)(a.step_at ? *a.step_at : a.step);
+    const int64_t counted = a.step_at ? *a.step_at : a.step;
+    const float step = (float)(counted > 1 ? counted : 1);
     by_first = lr / (a.beta1 > 0.f ? -expm1f(step * a.log_beta1) : 1.f);
     by_second = 1.f / sqrtf(a.beta2 > 0.f ? -expm1f(step * a.log_beta2) : 1.f);
     keep = 1.f - lr * t.decay;

@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(64 * kParts) linear_i8_few_kernel(ProductArgs 
 
 // Many rows: a workgroup takes a tile of 16 kMTiles kWavesM x 64 kWavesN, stage by stage of one group (128 bytes of every row), which copies put into LDS
 // kStages - 1 stages ahead, straight from memory.  kSplit parts of the workgroup's waves take the groups in turn and add up their sums at the end.
-// 256 x 256 tiles, eight waves, two a SIMD: 32 760 x 5120 x 5120 660-690 us over boxes (2.5-2.6 POP/s; a large library product of whole numbers without scales takes 733-755), 8192^3 400
+// 256 x 256 tiles, eight waves, two a SIMD: 32 760 x 5120 x 5120 660-690 us from board to board (2.5-2.6 POP/s; a large library product of whole numbers without scales takes 733-755), 8192^3 400
 // (2.75).  At 32 760 rows the matrix pipes are busy 54 % of the cycles at 2.2 GHz; with codes of zeros it takes 550 and 8192^3 318 (3.46 POP/s, 69 %): the board's power, then the reads of A from
 // beyond the last-level cache (a quarter of A's memory: 640).  What does not change the time: fragments read a stage ahead through rings of four and five
 // stages of 64 bytes (717 beside 700), four waves of 128 x 128 with a third fewer reads from LDS (750), A in blocks of 128 columns (708 beside 704).  Asking for lines of A three stages ahead

@@ -359,6 +359,21 @@ def test_step_and_rate_from_the_device_captured_and_replayed():
             lr.mul_(1.0)
 
 
+@pytest.mark.parametrize("coded", [False, True], ids=["f32", "8bit"])
+def test_rate_or_step_alone_from_the_device(coded):
+    """Each against the oracle; a number below 1 counts as 1; beta of 0 has no correction."""
+    lr = torch.tensor([2 * LR], device=DEV)
+    for number, betas in ((9, (BETA1, BETA2)), (0, (BETA1, BETA2)), (-5, (BETA1, BETA2)), (4, (0.0, 0.0)), (1 << 40, (BETA1, BETA2))):
+        t, how = torch.tensor([number], device=DEV), dict(beta1=betas[0], beta2=betas[1])
+        group = Group([300, 4100], coded=coded)
+        before = group.read()
+        group.step(step=0, step_at=t, **how)
+        check(group, before, group.read(), step=max(number, 1), more=6 * U32, **how)
+        before = group.read()
+        group.step(lr=0.0, lr_at=lr, step=3, **how)
+        check(group, before, group.read(), lr=float(lr), step=3, more=6 * U32, **how)
+
+
 def test_on_a_busy_stream_of_its_own():
     for by_argument in (True, False):
         group, eager = Group([9000]), Group([9000])

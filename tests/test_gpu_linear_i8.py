@@ -171,6 +171,10 @@ def test_longer_sums_are_added_in_parts(size):
     for at in range(0, K, 130944):
         most = most + os_.product(a[:, at:at + 130944], sa, b[:, at:at + 130944], sb)[1]
     assert_within(out, want, 6 * U32 * most, "parts")
+    # added to, with a bias, which counts once
+    before, bias = to64(out), np.linspace(-1e3, 1e3, N).astype(np.float32)
+    rl.radial_product_i8(*put_codes(a, sa), *put_codes(b, sb), out, bias=torch.tensor(bias, device=DEV), accumulate=True)
+    assert_within(out, before + want + bias, 10 * U32 * (most + np.abs(before) + np.abs(bias)), "parts added")
 
 
 def test_more_than_2_to_the_31_codes_and_results():
