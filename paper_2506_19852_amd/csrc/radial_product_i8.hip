@@ -66,6 +66,44 @@ __device__ __forceinline__ void put(const ProductArgs& a, int32_t m, int32_t n, 
   }
 }
 
+// A wave's float32 results of one row fragment, 16 rows of 64 columns that are all inside: lane l has row l%16, columns 16 (l/16) .. + 15.  Pieces of 16 bytes change lanes, so that
+// each store writes 64 neighbouring bytes of a row and not every fourth piece of it: the gradients of 14 040 x 5120 x 5120 take 848 us instead of 859, 1237 x 1961 x 1001
+// 13.4 instead of 14.4.  (bf16 results, which are every second piece, gained nothing from the like.)
+__device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
+  const auto sw = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  const uint32_t first = sw[0], second = sw[1];
+  a = first;
+  b = second;
+}
+__device__ __forceinline__ void swap_rows(uint32_t& a, uint32_t& b) {
+  const auto sw = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  const uint32_t first = sw[0], second = sw[1];
+  a = first;
+  b = second;
+}
+__device__ __forceinline__ void put_fragment(const ProductArgs& a, int32_t m, int32_t n_of_wave, int32_t q, const float (&y)[16]) {
+  uint32_t piece[4][4];  // piece t of a lane: columns 16 q + 4 t on; after the swaps columns 16 t + 4 q on
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) piece[t][e] = __builtin_bit_cast(uint32_t, y[4 * t + e]);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    swap_halves(piece[0][e], piece[2][e]);
+    swap_halves(piece[1][e], piece[3][e]);
+    swap_rows(piece[0][e], piece[1][e]);
+    swap_rows(piece[2][e], piece[3][e]);
+  }
+  if (m >= a.M) return;
+  float* out = (float*)a.out + m * a.out_stride + n_of_wave + 4 * q;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    f32x4 v = __builtin_bit_cast(f32x4, u32x4{piece[t][0], piece[t][1], piece[t][2], piece[t][3]});
+    if (a.accumulate) v += *(const f32x4_any*)(out + 16 * t);
+    *(f32x4_any*)(out + 16 * t) = v;
+  }
+}
+
 // Few rows, or few results: a workgroup of 8 waves takes 16 x 16 of C, each wave every 8th group, straight from memory (a lane's 32 bytes of a row, four
 // lanes a line); the parts meet in LDS.  (1 x 5120 x 5120 7.7 us; two or four times the rows for a workgroup were slower: 64 x 5120 x 5120 22 to 24 us, in tiles of 32 x 64 8.5.)
 constexpr int kParts = 8;
@@ -331,6 +369,7 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) __attribute__
         for (int t = 0; t < S::kNTiles; ++t) sum[i][t] += *place(from_part, i, t);
   }
   const int32_t n = n0 + wn * 64 + q * 16;
+  const bool whole = a.out_type == RADIAL_F32 && n0 + wn * 64 + 64 <= a.N;
   float sb[16], bias[16];
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
@@ -341,12 +380,12 @@ __global__ void __launch_bounds__(64 * kWavesM * kWavesN * kSplit) __attribute__
 #pragma unroll
   for (int i = 0; i < kMTiles; ++i) {
     const int32_t m = m0 + (wm * kMTiles + i) * 16 + l16;
-    if (m >= a.M) continue;
-    const float sa = a.sa[m];
+    const float sa = a.sa[min(m, a.M - 1)];
     float y[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) y[e] = result(sum[i][e >> 2][e & 3], sa * sb[e], bias[e]);
-    put(a, m, n, y, a.N - n);
+    if (whole) put_fragment(a, m, n0 + wn * 64, q, y);
+    else if (m < a.M) put(a, m, n, y, a.N - n);
   }
 }
 
