@@ -1,7 +1,7 @@
 // Codes of 8-bit integers for gfx950: a matrix with one float32 scale for each row, by rows, and by columns as the rows of its transpose.  Bound by memory: a row's scale needs all of
 // the row, which stays in registers (32 760 x 5120 in bf16 91 us, 5.5 TB/s); a column's needs all of the column, so that columns take two passes over the matrix, the second
-// from the last-level cache as far as it goes (14 040 x 5120: columns 68 us, rows and columns 91; 5120 x 5120 32 and 43).  Within the gradients of a projection of that size the two
-// passes over both matrices take 230 us, the first from a cold cache at 3.1 TB/s.
+// from the last-level cache as far as it goes (14 040 x 5120: columns 60 us, rows and columns 79; 5120 x 5120 28 and 39).  Within the gradients of a projection of that size the two
+// passes over both matrices take some 190 us, the first from a cold cache.
 #include <math.h>
 
 #include "radial_layer_common.h"
@@ -257,13 +257,15 @@ __global__ void __launch_bounds__(256) quantize_tiles_i8_kernel(Jobs jobs) {
 }
 
 inline int32_t at_most(int64_t wanted, int64_t most) { return (int32_t)(wanted < most ? wanted : most); }
-// Slabs of the first pass: two workgroups for each compute unit, of 32 rows at least (the second pass reads a value of each slab).
+// Slabs of the first pass: up to two workgroups for each compute unit, of 32 rows at least (the second pass reads a value of each slab).  (14 040 x 5120: 520 workgroups, eight too many,
+// cost 4 us; three for each are alike.)
 inline int32_t slabs_of(int32_t rows, int32_t cols) {
   const int64_t tiles = ((int64_t)cols + 511) / 512;
-  return at_most((512 + tiles - 1) / tiles, ((int64_t)rows + 31) / 32);
+  return at_most(tiles < 512 ? 512 / tiles : 1, ((int64_t)rows + 31) / 32);
 }
-// Strips of the second: four workgroups for each compute unit, as long as there are tiles.
-inline int32_t strips_of(int32_t rows, int32_t cols) { return at_most((1024 + code_groups(cols) - 1) / code_groups(cols), code_groups(rows)); }
+// Strips of the second: up to three workgroups for each compute unit, which all fit at once, as long as there are tiles.  (14 040 x 5120: columns 64 us, with both orientations 84;
+// with 1040 workgroups, one round and a third, 67 and 90; 32 760 x 5120 both 228 and 251.)
+inline int32_t strips_of(int32_t rows, int32_t cols) { return at_most(code_groups(cols) < 768 ? 768 / code_groups(cols) : 1, code_groups(rows)); }
 
 template <class T>
 int launch_rows(const Job& a, hipStream_t stream) {
@@ -337,7 +339,7 @@ Job job_of(const QuantI8& q, char* workspace) {
 }
 
 // Two matrices share their launches up to this many bytes.  Beyond, each goes through both passes before the next, so that the second pass finds what the first has
-// read in the last-level cache: two of 14 040 x 5120 in bf16 168 us, in shared launches 180; 1001 x 333 and 1001 x 2049 24 us, one after the other 33.
+// read in the last-level cache: two of 14 040 x 5120 in bf16 168 us, in shared launches 180 (both as first built); 1001 x 333 and 1001 x 2049 24 us, one after the other 33.
 constexpr int64_t kShared = 128LL << 20;
 
 template <class T>
