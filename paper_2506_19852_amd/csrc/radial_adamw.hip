@@ -287,9 +287,12 @@ __device__ __forceinline__ uint32_t encode_four(f32x4 v, const uint32_t (&bits)[
     return codes;
   }
   if (kPositive) {
-    // a positive value keeps a positive code: its least is half of the smallest and a little, 0 stays 0
+    // a positive value keeps a positive code: it is the smallest code's value at least; 0 stays 0 and NaN NaN
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = fmaxf(y[e], fminf(y[e] * 0x1p100f, 0x1p-9f));
+    for (int e = 0; e < 4; ++e) {
+      const float least = fminf(y[e] * 0x1p100f, 0x1p-9f);
+      y[e] = y[e] < least ? least : y[e];
+    }
   }
   return nearest_codes(y);
 }

@@ -246,16 +246,22 @@ def test_gradients_that_are_not_finite_change_nothing_behind_their_norm(bad):
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for k in before for a, b in zip(before[k], after[k]))
 
 
-def test_a_gradient_of_nan_without_a_norm_stays_in_its_value_or_block():
-    for coded in (False, True):
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")], ids=str)
+def test_a_gradient_that_is_not_finite_without_a_norm_stays_in_its_value_or_block(bad):
+    for coded, rounding in ((False, "nearest"), (True, "nearest"), (True, "random")):
         group = Group([600], coded=coded)
-        group.views["g"][0][300] = float("nan")
-        group.step()
+        group.views["g"][0][300] = bad
+        group.step(rounding=rounding)
         after = group.read()
         w = after["w"][0]
         assert w.isnan().sum() == 1 and w[300].isnan()
         if coded:
-            assert np.isnan(ol.e4m3_values()[after["m"][0].numpy()]).sum() == 1 and torch.isfinite(after["ms"][0]).all()
+            m, v = (np.isnan(ol.e4m3_values()[after[k][0].numpy()]) for k in ("m", "v"))
+            assert v[300] and v.sum() == 1 and torch.isfinite(after["vs"][0]).all()
+            assert m[300] and (m.sum() == 1 if np.isnan(bad) else m[256:384].all() and m.sum() == 128)
+            assert torch.isfinite(after["ms"][0]).sum() == (5 if np.isnan(bad) else 4)
+        else:
+            assert not torch.isfinite(after["m"][0][300]) and not torch.isfinite(after["v"][0][300]) and torch.isfinite(after["v"][0]).sum() == 599
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
