@@ -250,8 +250,8 @@ RADIAL_API int radial_linear_i8_bwd(int32_t M, int32_t N, int32_t K, const void*
  * States in 8 bits: m and sqrt(v) are held as E4M3 codes (as in radial.h) with a float32 scale for each block of 128 values of
  * the tensor, the last block the rest: scale = amax/448, code = E4M3(m (448/amax)), all 0 where amax is below 2^-100.  (sqrt(v) spans half of
  * the powers of two that v does.)  Otherwise a positive sqrt(v) never becomes 0, but the smallest code: what a step divides by is not lost
- * beside larger neighbours.  A NaN, and an infinite sqrt(v), has the code of NaN and does not enter amax; an infinite m makes its block's first state NaN.  Codes and
- * scales begin as zeros.  Rounding to nearest keeps a slowly changing state where it is (beta2 = 0.999 moves sqrt(v) by less than half
+ * beside larger neighbours.  A NaN, and an infinite sqrt(v), has the code of NaN and does not enter amax; a step divides by infinity there, as it does with
+ * float32 states, so that a weight whose v overflowed only decays.  An infinite m makes its block's first state NaN.  Codes and scales begin as zeros.  Rounding to nearest keeps a slowly changing state where it is (beta2 = 0.999 moves sqrt(v) by less than half
  * a step of its code, 3 to 6 %, unless a gradient is 8 times it); RADIAL_ROUND_RANDOM rounds up with the probability of what is left over, so
  * that a state is right on average: the magnitude's code is floor(y + u), y in steps of the code, u = (16 bits)/2^16.  The bits of
  * value i of tensor j are the low (m) and the high half (sqrt(v)) of h(h(k ^ j) ^ i), k = h(h(h(seed) ^ seed/2^32) ^ t) by 32-bit words,

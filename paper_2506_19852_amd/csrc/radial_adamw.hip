@@ -259,7 +259,8 @@ __device__ __forceinline__ float of_448(float a) {
   return __builtin_fmaf(__builtin_fmaf(-q, t, kScaled), r, q);
 }
 // sqrt(v): v / sqrt(v), and half of what its square leaves over that root.  Positive for every positive v, and rounded to nearest for normal numbers but for some
-// one in 2^22 next to a border.
+// one in 2^22 next to a border.  NaN for an infinite v, whose code in the state is that of NaN; what divides by the root takes NaN for infinity, now and when the code is read
+// again: m over it is 0, as it is with states in float32.  (A NaN in v without one in m has no other origin.)
 __device__ __forceinline__ float root_of(float v) {
   const float y = __builtin_amdgcn_rsqf(fmaxf(v, 0x1p-126f)), s = v * y;
   return __builtin_fmaf(__builtin_fmaf(-s, s, v), 0.5f * y, s);
@@ -353,7 +354,9 @@ __device__ __forceinline__ void step_piece(const StepArgs& a, const Tensor& t, P
       m[j][e] = m[j][e] * a.beta1 + x * a.of_grad1;
       v[j][e] = v[j][e] * a.beta2 + x * x * a.of_grad2;
       root[e] = kCoded ? root_of(v[j][e]) : sqrtf(v[j][e]);
-      w[j][e] = w[j][e] * keep - by_first * (m[j][e] * __builtin_amdgcn_rcpf(root[e] * by_second + a.eps));
+      float divisor = root[e] * by_second + a.eps;
+      if constexpr (kCoded) divisor = fminf(divisor, __builtin_inff());  // a root that is NaN counts as infinite
+      w[j][e] = w[j][e] * keep - by_first * (m[j][e] * __builtin_amdgcn_rcpf(divisor));
     }
     if (some) {
       store_four<kWhole>(weight, at, w[j], count);

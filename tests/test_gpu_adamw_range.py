@@ -1,0 +1,53 @@
+"""AdamW where float32 is left or nearly so, against the oracle (run with -m gpu).
+
+Bounds.  u = 2^-24.  m and v are float32 operations one by one, whose bits numpy gives; from them on, in 64 bits: the root u, its product with a constant 2u, the sum with eps u; the inverse one unit,
+2u; the products with m and with c, and c's own rounding, 3u: c m/d is off by 9u of itself (12u are allowed).  The decay's share of the weight is off by 2u of itself, the sum and the difference by u each."""
+import numpy as np
+import pytest
+import torch
+
+from layer_util import DEV, U32, assert_within
+from oracle import layer as ol
+from oracle import step as os_
+from test_gpu_adamw import BETA1, BETA2, BF16, EPS, F32, LR, Group, check
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("states", ["f32", "8bit", "random"])
+@pytest.mark.parametrize("grad", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", [2e19, 1e20, 3e38], ids=str)
+def test_a_gradient_whose_square_overflows_leaves_its_weight_but_for_the_decay(size, grad, states):
+    """v is infinite, and m over its root 0: the weight is not lost, nor in the next step.  A code of the root says NaN, in its value alone."""
+    group = Group([300, 5000], grad=grad, coded=states != "f32", copy=True)
+    large = [torch.arange(300) % 7 == 3, torch.arange(5000) > 4990]
+    for g, at in zip(group.views["g"], large):
+        g[at.to(DEV)] = size
+        g[at.to(DEV).nonzero()[0]] = -size
+    before = group.read()
+    group.step(rounding="random" if states == "random" else "nearest", seed=4)
+    after = group.read()
+    for i, at in enumerate(large):
+        w, got = before["w"][i].double().numpy(), after["w"][i].double().numpy()
+        want = w * (1 - LR * group.decay)
+        assert_within(got[at], want[at], 2 * U32 * (np.abs(w) + np.abs(want))[at], "w")
+        assert np.isfinite(got).all() and (got != want)[~at].any()
+        assert torch.equal(after["c"][i], after["w"][i].to(BF16))
+        if group.coded:
+            v = ol.e4m3_values()[after["v"][i].numpy()]
+            assert np.array_equal(np.isnan(v), at.numpy()) and torch.isfinite(after["vs"][i]).all() and torch.isfinite(after["ms"][i]).all()
+            assert not np.isnan(ol.e4m3_values()[after["m"][i].numpy()]).any()
+        else:
+            assert np.array_equal(np.isinf(after["v"][i].numpy()), at.numpy())
+    # and stays where it is
+    for g, at in zip(group.views["g"], large):
+        g[at.to(DEV)] = 1e-3
+    group.step(step=8)
+    again = group.read()
+    for i, at in enumerate(large):
+        w = after["w"][i].double().numpy()
+        want = w * (1 - LR * group.decay)
+        got = again["w"][i].double().numpy()
+        assert_within(got[at], want[at], 2 * U32 * (np.abs(w) + np.abs(want))[at], "w of the next step")
+        assert np.isfinite(got).all()
+    assert group.guards_kept()
