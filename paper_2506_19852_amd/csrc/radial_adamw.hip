@@ -258,12 +258,15 @@ __device__ __forceinline__ float of_448(float a) {
   const float t = a * 0x1p-9f, first = __builtin_amdgcn_rcpf(t), r = __builtin_fmaf(__builtin_fmaf(-t, first, 1.f), first, first), q = kScaled * r;
   return __builtin_fmaf(__builtin_fmaf(-q, t, kScaled), r, q);
 }
-// sqrt(v): v / sqrt(v), and half of what its square leaves over that root.  Positive for every positive v, and rounded to nearest for normal numbers but for some
-// one in 2^22 next to a border.  NaN for an infinite v, whose code in the state is that of NaN; what divides by the root takes NaN for infinity, now and when the code is read
-// again: m over it is 0, as it is with states in float32.  (A NaN in v without one in m has no other origin.)
+// sqrt(v), rounded to nearest: v / sqrt(v) and 1 / (2 sqrt(v)), both corrected once by what their product leaves of 1/2, and the root by what its square leaves of v.  Where that would leave the
+// normal numbers, below 2^-96, 2^64 v takes v's place.  NaN for an infinite v, whose code in the state is that of NaN; what divides by the root takes NaN for infinity, now and when the code is
+// read again: m over it is 0, as it is with states in float32.  (A NaN in v without one in m has no other origin.)
 __device__ __forceinline__ float root_of(float v) {
-  const float y = __builtin_amdgcn_rsqf(fmaxf(v, 0x1p-126f)), s = v * y;
-  return __builtin_fmaf(__builtin_fmaf(-s, s, v), 0.5f * y, s);
+  const bool small = v < 0x1p-96f;
+  const float x = small ? v * 0x1p64f : v, y = __builtin_amdgcn_rsqf(fmaxf(x, 0x1p-126f)), s = x * y, half = 0.5f * y;
+  const float left = __builtin_fmaf(-half, s, 0.5f), root = __builtin_fmaf(s, left, s);
+  const float nearest = __builtin_fmaf(__builtin_fmaf(-root, root, x), __builtin_fmaf(half, left, half), root);
+  return small ? nearest * 0x1p-32f : nearest;
 }
 
 // Codes and scale of a block's values: 32 lanes, four each.

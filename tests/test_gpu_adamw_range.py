@@ -14,6 +14,36 @@ from test_gpu_adamw import BETA1, BETA2, BF16, EPS, F32, LR, Group, check
 pytestmark = pytest.mark.gpu
 
 
+def zero_states(group):
+    for k in ("m", "v", "ms", "vs"):
+        for t in group.views.get(k, ()):
+            t.zero_()
+
+
+def check_from_moments(group, before, after, step, eps, rounding="nearest", seed=0):
+    """One tensor: codes and scales equal, weights from the float32 moments."""
+    g = before["g"][0].float().numpy()
+    if group.coded:
+        m0, r0 = (os_.decode(before[k][0].numpy(), before[k + "s"][0].numpy(), np.float32) for k in ("m", "v"))
+        v0 = r0 * r0
+    else:
+        m0, v0 = before["m"][0].numpy(), before["v"][0].numpy()
+    m, v = os_.moments(g, m0, v0, BETA1, BETA2)
+    assert m.dtype == v.dtype == np.float32 and np.isfinite(v).all()
+    if group.coded:
+        bits = os_.random_bits(seed, step, 0, len(g)) if rounding == "random" else (None, None)
+        for name, value, b, positive in (("m", m, bits[0], False), ("v", np.sqrt(v), bits[1], True)):
+            codes, scales = os_.encode(value, b, positive)
+            assert np.array_equal(after[name + "s"][0].numpy(), scales), name
+            assert np.array_equal(after[name][0].numpy(), codes), (name, (after[name][0].numpy() != codes).sum())
+    else:
+        assert np.array_equal(after["m"][0].numpy(), m) and np.array_equal(after["v"][0].numpy(), v)
+    w, m, v = before["w"][0].double().numpy(), m.astype(np.float64), v.astype(np.float64)
+    c, d = LR / (1 - BETA1 ** step), np.sqrt(v / (1 - BETA2 ** step)) + eps
+    want = w * (1 - LR * group.decay) - c * m / d
+    assert_within(after["w"][0].double().numpy(), want, 12 * U32 * c * np.abs(m) / d + 2 * U32 * (np.abs(w) + np.abs(want)), "w")
+
+
 @pytest.mark.parametrize("states", ["f32", "8bit", "random"])
 @pytest.mark.parametrize("grad", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("size", [2e19, 1e20, 3e38], ids=str)
@@ -50,4 +80,19 @@ def test_a_gradient_whose_square_overflows_leaves_its_weight_but_for_the_decay(s
         got = again["w"][i].double().numpy()
         assert_within(got[at], want[at], 2 * U32 * (np.abs(w) + np.abs(want))[at], "w of the next step")
         assert np.isfinite(got).all()
+    assert group.guards_kept()
+
+
+@pytest.mark.parametrize("states", ["f32", "8bit", "random"])
+@pytest.mark.parametrize("eps", [1e-8, 1e-20, 1e-30, 2e-38], ids=str)
+@pytest.mark.parametrize("size", [1e-14, 1e-16, 1e-17, 1e-18, 1e-19, 1e-20, 1e-21], ids=str)
+def test_gradients_whose_squares_are_hardly_there(size, eps, states):
+    """v below the normal numbers of float32, down to its smallest and to nothing: its root is that of the v there is.  Two steps, the second from the states of the first."""
+    group, rounding = Group([300], coded=states != "f32"), "random" if states == "random" else "nearest"
+    zero_states(group)
+    group.views["g"][0].copy_(torch.linspace(-size, size, 300))
+    for step in (1, 2):
+        before = group.read()
+        group.step(step=step, eps=eps, rounding=rounding, seed=11)
+        check_from_moments(group, before, group.read(), step, eps, rounding, 11)
     assert group.guards_kept()
