@@ -291,12 +291,9 @@ __device__ __forceinline__ uint32_t encode_four(f32x4 v, const uint32_t (&bits)[
     return codes;
   }
   if (kPositive) {
-    // a positive value keeps a positive code: it is the smallest code's value at least; 0 stays 0 and NaN NaN
+    // a positive value keeps a positive code: it is the smallest code's value at least; 0 stays 0 and NaN NaN.  (From the smallest root, 2^-74.5, beside the largest, 2^64, y is 2^-129.7: positive.)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float least = fminf(y[e] * 0x1p100f, 0x1p-9f);
-      y[e] = y[e] < least ? least : y[e];
-    }
+    for (int e = 0; e < 4; ++e) y[e] = y[e] > 0.f ? fmaxf(y[e], 0x1p-9f) : y[e];
   }
   return nearest_codes(y);
 }

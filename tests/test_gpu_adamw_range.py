@@ -96,3 +96,20 @@ def test_gradients_whose_squares_are_hardly_there(size, eps, states):
         group.step(step=step, eps=eps, rounding=rounding, seed=11)
         check_from_moments(group, before, group.read(), step, eps, rounding, 11)
     assert group.guards_kept()
+
+
+@pytest.mark.parametrize("rounding", ["nearest", "random"])
+@pytest.mark.parametrize("largest", [1e4, 1e12, 1e18, 1.5e19], ids=str)
+def test_the_smallest_root_of_a_block_keeps_the_smallest_code(largest, rounding):
+    """Beside a root up to 2^138 times as large, too: only what is nothing becomes 0."""
+    group = Group([256], coded=True)
+    zero_states(group)
+    group.views["g"][0].copy_(torch.tensor(np.geomspace(1e-21, 1e-10, 256)))
+    group.views["g"][0][5] = group.views["g"][0][200] = largest
+    group.views["g"][0][9] = 0
+    before = group.read()
+    group.step(step=1, rounding=rounding, seed=12)
+    after = group.read()
+    codes = after["v"][0].numpy()
+    assert codes[9] == 0 and (np.delete(codes, 9) >= 1).all()
+    check_from_moments(group, before, after, 1, EPS, rounding, 12)
