@@ -113,3 +113,44 @@ def test_the_smallest_root_of_a_block_keeps_the_smallest_code(largest, rounding)
     codes = after["v"][0].numpy()
     assert codes[9] == 0 and (np.delete(codes, 9) >= 1).all()
     check_from_moments(group, before, after, 1, EPS, rounding, 12)
+
+
+@pytest.mark.parametrize("from_device", [False, True], ids=["host", "device"])
+@pytest.mark.parametrize("states", ["f32", "8bit"])
+@pytest.mark.parametrize("by", [1e-6, 1e-7, 1e-8, 2e-9], ids=str)
+def test_a_small_decay_is_right_on_average(by, states, from_device):
+    """Weights of [1/2, 1) whose last bit is 2^-24, updates many times that: a decay of lr decay = `by` is lost in each but not in their mean.  The difference's rounding is spread evenly over 2^-24, a variance of
+    2^-48/12, and what is rounded before it 4u of the update and of the decay; five standard deviations."""
+    n, lr = 1 << 20, 1e-4
+    group = Group([n], coded=states == "8bit", decay=by / lr)
+    group.views["w"][0].copy_(torch.linspace(0.5, 1.0, n + 1)[:-1])
+    before = group.read()
+    if from_device:
+        group.step(lr=0.0, lr_at=torch.tensor([lr], device=DEV), step=1000)
+        lr = float(np.float32(lr))
+    else:
+        group.step(lr=lr, step=1000)
+    after = group.read()
+    g = before["g"][0].numpy()
+    if group.coded:
+        m0, r0 = (os_.decode(before[k][0].numpy(), before[k + "s"][0].numpy(), np.float32) for k in ("m", "v"))
+        m, v = os_.moments(g, m0, r0 * r0, BETA1, BETA2)
+    else:
+        m, v = os_.moments(g, before["m"][0].numpy(), before["v"][0].numpy(), BETA1, BETA2)
+    w = before["w"][0].double().numpy()
+    want = os_.update(w, m.astype(np.float64), v.astype(np.float64), lr, 1000, BETA1, BETA2, EPS, by / lr if not from_device else float(np.float32(by / 1e-4)))
+    moved, update = after["w"][0].double().numpy() - w, want - w + by * w
+    share = (moved - update).mean() / -(by * w).mean()   # of the decay
+    off = 5 * 2.0 ** -24 / np.sqrt(12 * n) + (4 + 12 * from_device) * U32 * (np.abs(update).mean() + by)
+    assert np.abs(update).mean() > 2.0 ** -17 and off < 0.1 * by
+    assert abs((after["w"][0].double().numpy() - want).mean()) <= off, share
+
+
+@pytest.mark.parametrize("decay", [0.0, 0.1])
+def test_weights_that_are_not_finite_stay_what_they_are(decay):
+    group = Group([300], decay=decay)
+    inf = float("inf")
+    group.views["w"][0][:3] = torch.tensor([inf, -inf, float("nan")])
+    group.step()
+    w = group.read()["w"][0]
+    assert w[0] == inf and w[1] == -inf and w[2].isnan() and torch.isfinite(w[3:]).all()
