@@ -302,7 +302,7 @@ __device__ __forceinline__ uint32_t encode_four(f32x4 v, const uint32_t (&bits)[
 // The step of a workgroup's piece: a wave takes 1024 neighbouring values, a lane four of every 256 (so that 32 lanes are one block of 128).  Products
 // and sums are rounded one by one, as the formula is written: a state's codes then do not depend on how a compiler joins them.
 template <class W, class G, bool kCoded, bool kRandom, bool kWhole>
-__device__ __forceinline__ void step_piece(const StepArgs& a, const Tensor& t, Piece piece, int32_t left, float factor, float by_decay, float by_first, float by_second) {
+__device__ __forceinline__ void step_piece(const StepArgs& a, const Tensor& t, Piece piece, int32_t left, float factor, float by_decay, float by_first, float by_second, int64_t step) {
 #pragma clang fp contract(off)
   const int64_t first = (int64_t)piece.index * kPiece;
   const uint32_t lane_at = (threadIdx.x >> 6) * 1024 + (threadIdx.x & 63) * 4;
@@ -332,7 +332,6 @@ __device__ __forceinline__ void step_piece(const StepArgs& a, const Tensor& t, P
   }
   uint32_t key = 0;
   if constexpr (kRandom) {
-    const int64_t step = a.step_at ? *a.step_at : a.step;
     key = mixed(mixed(mixed((uint32_t)a.seed) ^ (uint32_t)(a.seed >> 32)) ^ (uint32_t)step);
     key = mixed(key ^ (uint32_t)piece.tensor);
     const uint32_t far = (uint32_t)(first >> 32);
@@ -408,14 +407,15 @@ __global__ void __launch_bounds__(256) adamw_step_kernel(StepArgs a) {
   const Tensor t = ((const Tensor*)a.table)[piece.tensor];
   const float factor = a.factor ? *a.factor : 1.f;
   if (!(fabsf(factor) < __builtin_inff())) return;
+  int64_t step = a.step_at ? *a.step_at : a.step;
+  step = step > 1 ? step : 1;  // of the corrections and of the random bits
   float lr = a.lr, by_first = a.by_first, by_second = a.by_second, by_decay;
   if (a.lr_at || a.step_at) {
     // from the device: 1 - beta^t as -(e^(t log beta) - 1), which keeps its digits where beta^t is near 1
     if (a.lr_at) lr = *a.lr_at;
-    const int64_t counted = a.step_at ? *a.step_at : a.step;
-    const float step = (float)(counted > 1 ? counted : 1);
-    by_first = lr / (a.beta1 > 0.f ? -expm1f(step * a.log_beta1) : 1.f);
-    by_second = 1.f / sqrtf(a.beta2 > 0.f ? -expm1f(step * a.log_beta2) : 1.f);
+    const float counted = (float)step;
+    by_first = lr / (a.beta1 > 0.f ? -expm1f(counted * a.log_beta1) : 1.f);
+    by_second = 1.f / sqrtf(a.beta2 > 0.f ? -expm1f(counted * a.log_beta2) : 1.f);
     by_decay = lr * t.decay;
   } else {
     by_decay = (float)(a.lr_wide * (double)t.decay);
@@ -423,8 +423,8 @@ __global__ void __launch_bounds__(256) adamw_step_kernel(StepArgs a) {
   const int32_t left = left_of(t, (int64_t)piece.index * kPiece);
   auto go = [&](auto types) __attribute__((always_inline)) {
     using S = decltype(types);
-    if (left == kPiece) step_piece<typename S::W, typename S::G, S::kCoded, S::kRandomly, true>(a, t, piece, left, factor, by_decay, by_first, by_second);
-    else step_piece<typename S::W, typename S::G, S::kCoded, S::kRandomly, false>(a, t, piece, left, factor, by_decay, by_first, by_second);
+    if (left == kPiece) step_piece<typename S::W, typename S::G, S::kCoded, S::kRandomly, true>(a, t, piece, left, factor, by_decay, by_first, by_second, step);
+    else step_piece<typename S::W, typename S::G, S::kCoded, S::kRandomly, false>(a, t, piece, left, factor, by_decay, by_first, by_second, step);
   };
   switch (t.kind) {
     case 0: return go(step_of<__bf16, __bf16, false, false>{});

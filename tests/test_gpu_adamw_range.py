@@ -1,4 +1,5 @@
-"""AdamW where float32 is left or nearly so, against the oracle (run with -m gpu).
+"""AdamW where float32 is left or nearly so: gradients whose squares overflow or lie below the normal numbers, states of one block that are far apart, decays far below a weight's last
+bit, numbers of steps below 1 (run with -m gpu).
 
 Bounds.  u = 2^-24.  m and v are float32 operations one by one, whose bits numpy gives; from them on, in 64 bits: the root u, its product with a constant 2u, the sum with eps u; the inverse one unit,
 2u; the products with m and with c, and c's own rounding, 3u: c m/d is off by 9u of itself (12u are allowed).  The decay's share of the weight is off by 2u of itself, the sum and the difference by u each."""
@@ -154,3 +155,12 @@ def test_weights_that_are_not_finite_stay_what_they_are(decay):
     group.step()
     w = group.read()["w"][0]
     assert w[0] == inf and w[1] == -inf and w[2].isnan() and torch.isfinite(w[3:]).all()
+
+
+@pytest.mark.parametrize("number", [1, 0, -5, -(1 << 40)], ids=str)
+def test_a_number_below_1_draws_the_bits_of_the_first_step(number):
+    t = torch.tensor([number], device=DEV)
+    group = Group([300, 4100], coded=True)
+    before = group.read()
+    group.step(step=0, step_at=t, rounding="random", seed=21)
+    check(group, before, group.read(), step=1, rounding="random", seed=21, more=6 * U32)
