@@ -598,17 +598,21 @@ def _one(t, name, dtype, device):
     return t.data_ptr()
 
 
-def radial_adamw_step(plan: radial_adamw_plan_info, table, *, lr: float = 0.0, step: int = 0, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+def radial_adamw_step(plan: radial_adamw_plan_info, table, *, lr: float | None = None, step: int = 0, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                       factor=None, lr_at=None, step_at=None, rounding="nearest", seed: int = 0, stream=None):
     """One AdamW step over the table's tensors, in place.
 
-    step: 1, 2, ..., or step_at, a CUDA int64 tensor of one value that is read when the step runs; lr, or lr_at (float32) likewise; factor: radial_grad_norm's norm
+    step: 1, 2, ..., or step_at, a CUDA int64 tensor of one value that is read when the step runs; lr, or lr_at (float32) likewise (one of them is needed); factor: radial_grad_norm's norm
     (float32 [2], of which the second value multiplies the gradients; while it is not finite nothing is changed); rounding: "nearest" or "random" (by seed and
     step), of states in 8 bits."""
     lib = _lib or load()
     device = _device()
     if rounding not in _ROUNDINGS:
         raise ValueError(f"rounding must be one of {', '.join(_ROUNDINGS)}")
+    if lr is None:
+        if lr_at is None:
+            raise ValueError("lr or lr_at must be given")
+        lr = 0.0
     seed, step = operator.index(seed), operator.index(step)
     if not 0 <= seed < 1 << 64 or step >> 63:
         raise ValueError("seed must be below 2^64 and step below 2^63, neither negative")

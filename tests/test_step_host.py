@@ -270,6 +270,17 @@ def test_numbers_of_numpy(one_device):  # noqa: F811
         rl.radial_adamw_step(plan, _fake(U8, plan.table_bytes), lr=1e-3, step=1.5, stream=1)
 
 
+def test_a_step_without_a_rate_is_refused(one_device):  # noqa: F811
+    """It would move the states and leave the weights, and report success."""
+    _, plan, _ = _plan(_tensor())
+    small = _fake(U8, plan.table_bytes - 1)   # the last check before the launch
+    with pytest.raises(ValueError, match="lr or lr_at"):
+        rl.radial_adamw_step(plan, small, step=1, stream=1)
+    for how in (dict(lr=0.0), dict(lr=1e-3), dict(lr_at=_fake(T32, 1)), dict(lr=1e-3, lr_at=_fake(T32, 1))):
+        with pytest.raises(rb.RadialError, match="needed"):
+            rl.radial_adamw_step(plan, small, step=1, stream=1, **how)
+
+
 # ---- the oracle itself --------------------------------------------------------------------------
 
 def test_codes_of_the_oracle():
