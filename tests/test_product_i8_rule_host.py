@@ -7,6 +7,7 @@ import pytest
 
 from paper_2506_19852_amd import build as hip_build
 from test_gpu_linear_i8 import SIZES
+from test_gpu_linear_i8_long import LONG
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -60,3 +61,9 @@ def test_every_tile_is_taken_once(rule, shape):
     (flat,) = rule([f"tiles {shape[0]} {shape[1]}"])
     got = {(flat[i], flat[i + 1]) for i in range(0, len(flat), 2)}
     assert len(flat) == 2 * shape[0] * shape[1] and got == {(m, n) for m in range(shape[0]) for n in range(shape[1])}
+
+
+def test_long_gradients_leave_rows_over_in_either_product(rule):
+    _, _, dx = _of(rule, [(m, k, n) for m, n, k in LONG])
+    _, _, dw = _of(rule, [(n, k, m) for m, n, k in LONG])
+    assert [p[4] < m for p, (m, _, _) in zip(dx, LONG)] == [True, False] and [p[4] < n for p, (_, n, _) in zip(dw, LONG)] == [False, True]
