@@ -210,7 +210,7 @@ RADIAL_API int radial_quantize_rows_i8(int32_t rows, int32_t cols, const void* x
  *   accumulate : != 0: out, which is float32, <- out + the result.
  * With X, W and the gradient dY of Y = X W^T:  Y: (X, W); dX: (dY, W transposed); dW: (dY transposed, X transposed).
  * Up to K = 131 071 the sum is exact, for codes of -128 too.  A longer one is taken in parts of 130 944 columns that are added
- * in float32, so that out has to be float32.  Products of two scales have to be finite in float32.
+ * in float32, so that out has to be float32.  Products of two scales have to be finite in float32, and lose digits below 2^-126.
  * Errors: EINVAL (NULL, sizes < 1, types, accumulate), EUNSUPPORTED (K above 131 071 with bf16), ESHAPE (stride, alignment, M or
  * N above 2^29, K above 2^23), EHIP. */
 RADIAL_API int radial_product_i8(int32_t M, int32_t N, int32_t K, const int8_t* a_codes, const float* a_scales, const int8_t* b_codes,
@@ -227,7 +227,7 @@ RADIAL_API int radial_linear_i8_fwd(int32_t M, int32_t N, int32_t K, const void*
                                     size_t workspace_bytes, void* hip_stream);
 
 /* Its gradients from dy [M, N]: dx = dy W with dy quantised by rows, dw = dy^T x with dy and x quantised by columns, and
- * dbias = the column sums of dy, which are not quantised (the rounding to codes is passed over, as if it were not there).
+ * dbias = the column sums of dy in float32, not quantised (the rounding to codes is passed over, as if it were not there).
  *   wt_codes, wt_scales, dx : of W transposed (codes_t of W), and dx [M, K]; dx NULL: not wanted, then the codes are not read;
  *   x, dw                   : the forward's x [M, K] of dy's type, and dw [N, K]; dw NULL: not wanted, then x is not read;
  *   dbias                   : device float [N], or NULL: not wanted;
@@ -251,8 +251,8 @@ RADIAL_API int radial_linear_i8_bwd(int32_t M, int32_t N, int32_t K, const void*
  * the tensor, the last block the rest: scale = amax/448, code = E4M3(m (448/amax)), all 0 where amax is below 2^-100.  (sqrt(v) spans half of
  * the powers of two that v does.)  Otherwise a positive sqrt(v) never becomes 0, but the smallest code: what a step divides by is not lost
  * beside larger neighbours.  A NaN, and an infinite sqrt(v), has the code of NaN and does not enter amax; a step divides by infinity there, as it does with
- * float32 states, so that a weight whose v overflowed only decays.  An infinite m makes its block's first state NaN.  Codes and scales begin as zeros.  Rounding to nearest keeps a slowly changing state where it is (beta2 = 0.999 moves sqrt(v) by less than half
- * a step of its code, 3 to 6 %, unless a gradient is 8 times it); RADIAL_ROUND_RANDOM rounds up with the probability of what is left over, so
+ * float32 states, so that a weight whose v overflowed only decays.  An infinite m makes its block's first state NaN.  Codes and scales begin as zeros.
+ * Rounding to nearest keeps a slowly changing state where it is (beta2 = 0.999 moves sqrt(v) by less than half a step of its code, 3 to 6 %, unless a gradient is 8 times it); RADIAL_ROUND_RANDOM rounds up with the probability of what is left over, so
  * that a state is right on average: the magnitude's code is floor(y + u), y in steps of the code, u = (16 bits)/2^16.  The bits of
  * value i of tensor j are the low (m) and the high half (sqrt(v)) of h(h(k ^ j) ^ i), k = h(h(h(seed) ^ seed/2^32) ^ t) by 32-bit words,
  * h(x): x ^= x >> 16; x *= 0x9E3779B1; x ^= x >> 15; x *= 0x6A09E667; x ^= x >> 16  (for i from 2^32 on h(h(k ^ j) ^ i/2^32) takes h(k ^ j)'s place). */
@@ -286,7 +286,8 @@ typedef struct {
 RADIAL_API int radial_adamw_plan(const radial_adamw_tensor* tensors, int32_t count, radial_adamw_plan_info* plan);
 
 /* Fills the table (device, 16-byte aligned, table_bytes of at least plan->table_bytes) for the calls below, which only read it.  It
- * holds the tensors' addresses: they stay where they are as long as it is used, and nothing that is written overlaps anything else. */
+ * holds the tensors' addresses, those of the gradients too: they stay where they are as long as it is used (gradients that are allocated for each
+ * step need a table for each step, one launch for every 32 tensors), and nothing that is written overlaps anything else. */
 RADIAL_API int radial_adamw_table(const radial_adamw_tensor* tensors, const radial_adamw_plan_info* plan, void* table, size_t table_bytes, void* hip_stream);
 
 /* Bytes of device workspace radial_grad_norm needs (0 on invalid arguments). */
@@ -304,7 +305,8 @@ typedef struct {
   int64_t step;                 /* t >= 1                                                                            */
   uint64_t seed;                /* of RADIAL_ROUND_RANDOM                                                            */
   int32_t rounding;             /* RADIAL_ROUND_*, of states in 8 bits                                              */
-  const float* factor;          /* device, or NULL (1).  While it is not finite a step changes nothing at all       */
+  const float* factor;          /* device, or NULL (1).  While it is not finite a step changes nothing at all (a    */
+                                /*   number that the caller has counted on at step_at stays counted)                */
   const float* lr_at;           /* device, read in place of lr, or NULL                                              */
   const int64_t* step_at;       /* device, read in place of step (below 1: 1), or NULL: a captured step counts on in replays */
 } radial_adamw_params;

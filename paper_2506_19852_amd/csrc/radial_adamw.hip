@@ -45,7 +45,7 @@ __host__ __device__ __forceinline__ const Piece* pieces_of_table(const void* tab
 
 // ---- table ------------------------------------------------------------------------------------------
 
-constexpr int kTensorsAtOnce = 32;  // arguments of a launch, 2.6 KB
+constexpr int kTensorsAtOnce = 32;  // arguments of a launch, 2.4 KB
 struct TableArgs {
   void* table;
   int32_t count, first;
@@ -244,8 +244,9 @@ __device__ __forceinline__ uint32_t random_code(float y, uint32_t bits16) {
   return (y == y ? code : 0x7fu) | (u >> 31) << 7;
 }
 
-// Quotients and roots without the steps of the library functions that cover tiny and huge operands, and without those for the last bit where nothing hangs on it: 85 instructions
-// a value became 55, and 105 million bf16 weights with bf16 gradients and states in 8 bits took 200 us instead of 297.
+// Quotients and roots without the steps of the library functions that cover operands which do not occur here: 60 instructions a value where those took 85, and 105 million bf16 weights with bf16
+// gradients and states in 8 bits 196 us instead of 297.  The three below are rounded to nearest, for every significand and with the instruction's result off by a unit either way, so that the codes
+// are those of float32 arithmetic; the weights' quotient is the product with v_rcp_f32's inverse, a unit off, which only moves the update by 2^-23 of itself.
 //
 // a / 448: product with the inverse, and what it leaves once more.
 __device__ __forceinline__ float over_448(float a) {

@@ -75,8 +75,8 @@ inline ProductPlan plan_product(int32_t M, int32_t N, int32_t groups, const Tile
 inline int64_t pieces_of(int32_t n) { return ((int64_t)n + 15) / 16; }
 inline bool takes_pieces(int32_t M, int32_t N) { return M <= 16 || pieces_of(M) * pieces_of(N) <= kComputeUnits; }
 
-// Tile of a workgroup.  XCD x of 8 (workgroup id mod 8) gets a run of neighbouring tiles, in bands of kBand rows of tiles, column by column: the 32 that
-// it works on at a time are 8 x 4, whose codes it fetches into its L2 once.
+// Tile of a workgroup.  XCD x of 8 (workgroup id mod 8) gets a run of neighbouring tiles, in bands of kBand rows of tiles, column by column: of the 32 that
+// it works on at a time 8 share a column with kBand 8 (8 x 4) and 6 with 6, and their codes are fetched into its L2 once.
 template <uint32_t kBand = 8>
 __host__ __device__ __forceinline__ void tile_of(uint32_t id, int32_t tiles_m, int32_t tiles_n, int32_t& m, int32_t& n) {
   constexpr uint32_t kXcds = 8;

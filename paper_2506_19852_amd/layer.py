@@ -512,7 +512,7 @@ def adamw_tensors(weights, grads, firsts, seconds, *, first_scales=None, second_
 
     weights, grads: bf16 or float32; firsts, seconds: float32 states, or uint8 codes with float32 first_scales and second_scales [ceil(n/128)]; copies:
     bf16, each gets its weight rounded (an entry may be None); decay: one number, or one for each tensor.  Nothing that a step writes may overlap another tensor.
-    The array holds addresses: the caller keeps the tensors."""
+    The array and the table made of it hold addresses: the caller keeps the tensors, and makes both again when one moves (gradients that are freed after each step do)."""
     _lib or load()
     device, count = _device(), len(weights)
 
